@@ -454,6 +454,163 @@ agnes_status agnes_sage_forward(agnes_batch* batch, const agnes_sage_model* mode
 agnes_status agnes_sage_forward_noalloc(agnes_batch* batch, const agnes_sage_model* model, float* out,
                                         void* hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a training or serving step beside the hyperbatch path: rows of a
+ * learned table for the sampled nodes and their gradient, the loss against a
+ * teacher's top logits, and 4-bit products for a frozen model.
+ *
+ * Shared conventions: every pointer is device memory of the current device
+ * unless said otherwise; every call enqueues on hip_stream and returns without
+ * waiting; it keeps nothing between calls, so calls on different streams do
+ * not disturb each other.  A call that needs scratch memory takes it from its
+ * caller: `workspace` (device, 256-byte aligned) of at least the bytes that
+ * its *_bytes function returns for the same sizes, in use until the call's work
+ * on hip_stream is done.  The calls allocate nothing and may be captured in a HIP
+ * graph.  Results are the same on every run: sums have a fixed order.
+ * ------------------------------------------------------------------------- */
+
+/* A row-major matrix: element (i, j) is data[i * stride + j] (stride in
+ * elements, not bytes).  An input's rows may overlap (stride >= 0; 0 = one row
+ * for all); an output needs stride >= cols.  data needs only its element
+ * type's own alignment; it may be NULL when rows * cols is 0. */
+typedef struct {
+    void* data;
+    int64_t rows;
+    int64_t cols;
+    int64_t stride;
+    agnes_dtype dtype;   /* AGNES_FLOAT32, AGNES_FLOAT16 or AGNES_BFLOAT16 */
+} agnes_matrix;
+
+/* Embedding lookup: out row i = scale * table row ids[i], computed in float32
+ * and rounded once to out's type.  ids: [out->rows] of ids_dtype (AGNES_INT32
+ * or AGNES_INT64).  An id outside [0, table->rows) names no row (padding): its
+ * output row is zero.  out->cols must be table->cols; table->rows < 2^31 - 1.
+ * Errors: INVALID. */
+agnes_status agnes_embedding_lookup(const agnes_matrix* table, const void* ids, agnes_dtype ids_dtype, float scale,
+                                    const agnes_matrix* out, void* hip_stream);
+
+/* Gradient of the lookup: row v of the table receives
+ *     scale * sum of grad_out row i over the i with ids[i] = v, ascending in i,
+ * summed in float32 and rounded once; padding ids add nothing.  The ids are
+ * sorted (stably) and each run of equal ids is summed; long runs are summed in
+ * pieces of fixed length that are then added in order.
+ * n = grad_out->rows < 2^31, num_rows < 2^31 - 1.
+ *
+ * agnes_embedding_grad writes the whole gradient, grad_table [num_rows][dim]:
+ * rows that no id names become zero.  With accumulate != 0 the sums are added
+ * (in float32, rounded once) to what grad_table holds, and other rows stay as
+ * they are.
+ *
+ * agnes_embedding_grad_rows writes the named rows alone: row_ids[r] (int32) is
+ * the r-th distinct id in ascending order and row r of rows its gradient, for
+ * r < min(count, rows->rows); the remaining row_ids are -1 and the remaining
+ * rows are left as they are.  *count (int64) receives the number of distinct ids,
+ * also when it is more than rows->rows (agnes_stats.distinct_rows for a
+ * batch's node list).
+ * Errors: INVALID (also a workspace that is too small), RANGE. */
+agnes_status agnes_embedding_grad_bytes(int64_t n, int64_t num_rows, int64_t dim, uint64_t* bytes);
+agnes_status agnes_embedding_grad(const agnes_matrix* grad_out, const void* ids, agnes_dtype ids_dtype, float scale,
+                                  int32_t accumulate, const agnes_matrix* grad_table, void* workspace,
+                                  uint64_t workspace_bytes, void* hip_stream);
+agnes_status agnes_embedding_grad_rows(const agnes_matrix* grad_out, const void* ids, agnes_dtype ids_dtype,
+                                       float scale, int64_t num_rows, int32_t* row_ids, const agnes_matrix* rows,
+                                       int64_t* count, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* The same for a batch's node list: ids = the batch's nodes (minibatch-major,
+ * agnes_batch_view.nodes), n = node_off[H], table rows = the store's nodes.
+ * The call is ordered after the batch's gather on whatever stream that runs,
+ * and the next hyperbatch begun on the batch waits for it.  Errors: INVALID
+ * (also a batch without a finished hyperbatch). */
+agnes_status agnes_batch_embedding_lookup(agnes_batch* batch, const agnes_matrix* table, float scale,
+                                          const agnes_matrix* out, void* hip_stream);
+agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_matrix* grad_out, float scale,
+                                             int32_t* row_ids, const agnes_matrix* rows, int64_t* count,
+                                             void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits.  Row i has C = logits.cols student
+ * logits z, k = teacher.cols teacher logits t_1 .. t_k of the classes c_1 ..
+ * c_k, a label y and a weight w.  With q = softmax(z / T), and p = softmax(t / T)
+ * over the row's valid entries (0 <= c_e < C; others are padding):
+ *     L_i   = soft * T^2 * sum_e p_e (ln p_e - ln q[c_e])
+ *           + hard * (ln sum_j exp z_j - z_y)
+ *     loss  = w L_i,   grad = w dL_i / dz
+ * A row without valid entries has no first term, one whose label lies outside
+ * [0, C) no second term.  A class listed twice has the sum of its p.  Terms with
+ * p_e = 0 count as 0.  A row of weight 0 is skipped: loss 0, gradient 0,
+ * whatever its logits hold.  Logits may be -inf (masked classes: q = 0,
+ * gradient 0; a loss that asks for one is +inf); a row whose logits are all
+ * -inf has no q: its loss is +inf (0 if it has no term) and its gradient 0.  NaN or +inf
+ * logits make the row's loss and gradient NaN.  All arithmetic is float32; the
+ * gradient is rounded once to its type.
+ *   logits, teacher: matrices of equal rows; teacher.cols in [0, AGNES_DISTILL_MAX_K].
+ *   classes: index_dtype (AGNES_INT32 or AGNES_INT64) [rows], stride
+ *     classes_stride >= 0 elements.
+ *   labels: index_dtype [rows], or NULL (no second term).
+ *   weight: float32 [rows], or NULL (1).  The gradient of a loss that is
+ *     not a weighted sum: pass its row factors here to agnes_distill_grad.
+ *   temperature > 0, soft >= 0, hard >= 0, all finite.
+ * agnes_distill_loss: loss [rows] and, unless NULL, stats [rows][3] (the row's
+ *   largest logit m, sum exp((z - m) / T), sum exp(z - m)).
+ * agnes_distill_grad: the gradient from those statistics.
+ * agnes_distill_loss_grad: both in one pass over the logits.
+ * grad: the logits' shape, any type; it may be the logits' own memory (same
+ *   data, stride and type).  Errors: INVALID. */
+#define AGNES_DISTILL_MAX_K 1024
+typedef struct {
+    agnes_matrix logits;
+    agnes_matrix teacher;
+    const void* classes;
+    int64_t classes_stride;
+    agnes_dtype index_dtype;
+    const void* labels;
+    const float* weight;
+    float temperature;
+    float soft;
+    float hard;
+} agnes_distill;
+
+agnes_status agnes_distill_bytes(int64_t rows, int64_t classes, uint64_t* bytes);
+agnes_status agnes_distill_loss(const agnes_distill* d, float* loss, float* stats, void* workspace,
+                                uint64_t workspace_bytes, void* hip_stream);
+agnes_status agnes_distill_grad(const agnes_distill* d, const float* stats, const agnes_matrix* grad,
+                                void* hip_stream);
+agnes_status agnes_distill_loss_grad(const agnes_distill* d, float* loss, const agnes_matrix* grad, void* workspace,
+                                     uint64_t workspace_bytes, void* hip_stream);
+
+/* Microscaled 4-bit floating point (the MXFP4 format of the OCP Microscaling
+ * specification): a row of cols elements is cut into blocks of 32 (the last
+ * one padded with zeros); a block has one scale, 2^(code - 127) as a byte,
+ * and 32 elements of 4 bits (sign, two exponent bits, one mantissa bit:
+ * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6).
+ *   codes: [rows][16 * ceil(cols / 32)] bytes, element 2 i in the low four bits
+ *     of byte i; 16-byte aligned.   scales: [rows][ceil(cols / 32)] bytes.
+ * Quantisation: scale = 2^(floor(log2 max|x|) - 2), not below 2^-127; element =
+ * x / scale rounded to nearest, ties to the even code, magnitudes above 6 to 6.
+ * A block with an infinity or NaN has the scale code 255: all its
+ * values are NaN, and so is every product that takes part in it. */
+typedef struct {
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t rows;
+    int64_t cols;
+} agnes_mx4;
+
+/* x -> q and q -> x (equal shapes).  Errors: INVALID. */
+agnes_status agnes_mx4_quantize(const agnes_matrix* x, const agnes_mx4* q, void* hip_stream);
+agnes_status agnes_mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, void* hip_stream);
+
+/* out[M][N] = x[M][K] w[N][K]^T + bias, then max(., 0) with relu != 0 (NaN
+ * stays NaN): 4-bit operands, float32 sums, one rounding to out's type.  bias:
+ * float32 [N] or NULL.  agnes_mx4_linear quantises its float rows x first
+ * (into the workspace); w is laid out once by agnes_mx4_quantize.
+ * M, N, K < 2^31.  Errors: INVALID. */
+agnes_status agnes_mx4_product_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
+agnes_status agnes_mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, int32_t relu,
+                               const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+agnes_status agnes_mx4_linear_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
+agnes_status agnes_mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const float* bias, int32_t relu,
+                              const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
 /* Store facts: out[0] num_nodes, out[1] num_edges, out[2] topology blocks,
  * out[3] edges per topology block, out[4] feature blocks, out[5] rows per
  * feature block, out[6] row_bytes, out[7] device bytes held by the store. */

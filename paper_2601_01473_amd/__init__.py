@@ -8,6 +8,13 @@ torch streams, and copies of the outputs back to numpy.
     store = Store(offsets, indices, features, block_bytes=65536)
     batch = store.prepare(targets_int32_HxB, fanouts=[25, 10], seed=0)
     out = batch.to_host()          # per-minibatch nodes, per-hop CSR, features
+
+Operators of the step that follows (ops.py), on torch CUDA tensors: rows of a
+learned table for a batch's nodes and their gradient (embedding_lookup,
+embedding_grad, embedding_grad_rows, Batch.embedding, Batch.embedding_grad_rows),
+the loss against a teacher's top logits with its gradient (distill_loss,
+distill_grad, distill_loss_grad), and products with 4-bit weights
+(mx4_quantize, mx4_dequantize, mx4_linear).
 """
 from __future__ import annotations
 
@@ -24,6 +31,9 @@ from ._binding import agnes_hyperbatch_begin_device, agnes_hyperbatch_prepare_de
 from ._binding import agnes_store_info, agnes_store_object_table, agnes_store_set_option  # noqa: F401
 from ._binding import agnes_batch_tier_stats, agnes_build_blocks_staged, agnes_sage_forward  # noqa: F401
 from ._binding import agnes_build_blocks_cached, agnes_philox4x64_10, agnes_set_device_allocator  # noqa: F401
+from . import ops
+from .ops import Mx4, distill_grad, distill_loss, distill_loss_grad, embedding_grad  # noqa: F401
+from .ops import embedding_grad_rows, embedding_lookup, mx4_dequantize, mx4_linear, mx4_quantize  # noqa: F401
 
 _FEAT_DTYPES = {np.dtype(np.float32): B.AGNES_FLOAT32, np.dtype(np.float16): B.AGNES_FLOAT16}
 
@@ -291,6 +301,42 @@ class Batch:
         fn(self.handle, m, out.data_ptr(), _stream_handle(stream))
         self._sage_keep = (weights, biases, out)
         return out
+
+    def embedding(self, table: torch.Tensor, scale: float = 1.0, dtype: torch.dtype | None = None,
+                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """scale * table[nodes] for the batch's node list, one row per node in
+        the features' order (agnes_batch_embedding_lookup).  table: [num_nodes,
+        dim]; returns [rows, dim] of `dtype` (default: the table's)."""
+        m = ops._matrix(table, "table")
+        v = self.view()
+        rows = int(v.node_off[v.H])
+        with ops._on(stream, table, out):
+            if out is None:
+                out = torch.empty(rows, m.cols, dtype=dtype or table.dtype, device="cuda")
+            elif dtype is not None and out.dtype != dtype:
+                raise ValueError("out must be of the type asked for")
+            B.agnes_batch_embedding_lookup(self.handle, m, scale, ops._matrix(out, "out"), ops._handle(stream))
+        return out
+
+    def embedding_grad_rows(self, grad_out: torch.Tensor, max_rows: int | None = None, scale: float = 1.0,
+                            dtype: torch.dtype | None = None, stream=None):
+        """The gradient of embedding() as distinct rows (agnes_batch_embedding_grad_rows):
+        (row_ids int32, rows, count) as embedding_grad_rows returns them.
+        max_rows defaults to the batch's number of distinct nodes
+        (stats()["distinct_rows"], which waits for the batch)."""
+        if max_rows is None:
+            max_rows = self.stats()["distinct_rows"]
+        with ops._on(stream, grad_out):
+            g = ops._rows_of(grad_out)
+            m = ops._matrix(g, "grad_out")
+            row_ids = torch.empty(max_rows, dtype=torch.int32, device="cuda")
+            rows = torch.empty(max_rows, m.cols, dtype=dtype or grad_out.dtype, device="cuda")
+            count = torch.empty(1, dtype=torch.int64, device="cuda")
+            ws = ops._workspace(B.agnes_embedding_grad_bytes(m.rows, self.store.num_nodes, m.cols))
+            B.agnes_batch_embedding_grad_rows(self.handle, m, scale, row_ids.data_ptr(), ops._matrix(rows, "rows"),
+                                              count.data_ptr(), ops._ptr(ws), 0 if ws is None else ws.numel(),
+                                              ops._handle(stream))
+        return row_ids, rows, count
 
     def tier_stats(self) -> dict:
         """Staged-tier counters (all zero for HBM-resident features)."""

@@ -30,7 +30,11 @@ EXPORTED = ["agnes_build_blocks", "agnes_build_blocks_staged", "agnes_build_bloc
             "agnes_hyperbatch_prepare_device", "agnes_hyperbatch_begin", "agnes_hyperbatch_begin_device", "agnes_batch_finish", "agnes_batch_wait", "agnes_batch_view_get",
             "agnes_batch_stats", "agnes_batch_tier_stats", "agnes_store_set_option", "agnes_store_info",
             "agnes_store_object_table", "agnes_sage_forward", "agnes_sage_forward_noalloc", "agnes_philox4x64_10", "agnes_set_device_allocator", "agnes_free",
-            "agnes_last_error"]
+            "agnes_last_error", "agnes_embedding_lookup", "agnes_embedding_grad_bytes", "agnes_embedding_grad",
+            "agnes_embedding_grad_rows", "agnes_batch_embedding_lookup", "agnes_batch_embedding_grad_rows",
+            "agnes_distill_bytes", "agnes_distill_loss", "agnes_distill_grad", "agnes_distill_loss_grad",
+            "agnes_mx4_quantize", "agnes_mx4_dequantize", "agnes_mx4_product_bytes", "agnes_mx4_product",
+            "agnes_mx4_linear_bytes", "agnes_mx4_linear"]
 
 # void* alloc(uint64_t bytes, void* user); void release(void* ptr, uint64_t bytes, void* user)
 DEVICE_ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p)
@@ -81,6 +85,23 @@ class agnes_tier_stats(ctypes.Structure):
 class agnes_sage_model(ctypes.Structure):
     _fields_ = [("L", ctypes.c_int32), ("dims", ctypes.c_int32 * (AGNES_MAX_LAYERS + 1)),
                 ("weight", ctypes.c_void_p * AGNES_MAX_LAYERS), ("bias", ctypes.c_void_p * AGNES_MAX_LAYERS)]
+
+
+class agnes_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class agnes_distill(ctypes.Structure):
+    _fields_ = [("logits", agnes_matrix), ("teacher", agnes_matrix), ("classes", ctypes.c_void_p),
+                ("classes_stride", ctypes.c_int64), ("index_dtype", ctypes.c_int), ("labels", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("temperature", ctypes.c_float), ("soft", ctypes.c_float),
+                ("hard", ctypes.c_float)]
+
+
+class agnes_mx4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
 
 
 class AgnesError(RuntimeError):
@@ -143,6 +164,27 @@ def lib():
     L.agnes_philox4x64_10.argtypes = [vp, vp, i64, vp]
     L.agnes_set_device_allocator.restype = st
     L.agnes_set_device_allocator.argtypes = [DEVICE_ALLOC_FN, DEVICE_FREE_FN, vp]
+    mat, mx, dis, f32, u64p = (ctypes.POINTER(agnes_matrix), ctypes.POINTER(agnes_mx4),
+                               ctypes.POINTER(agnes_distill), ctypes.c_float, ctypes.POINTER(u64))
+    for name, args in (
+            ("agnes_embedding_lookup", [mat, vp, st, f32, mat, vp]),
+            ("agnes_embedding_grad_bytes", [i64, i64, i64, u64p]),
+            ("agnes_embedding_grad", [mat, vp, st, f32, i32, mat, vp, u64, vp]),
+            ("agnes_embedding_grad_rows", [mat, vp, st, f32, i64, vp, mat, vp, vp, u64, vp]),
+            ("agnes_batch_embedding_lookup", [vp, mat, f32, mat, vp]),
+            ("agnes_batch_embedding_grad_rows", [vp, mat, f32, vp, mat, vp, vp, u64, vp]),
+            ("agnes_distill_bytes", [i64, i64, u64p]),
+            ("agnes_distill_loss", [dis, vp, vp, vp, u64, vp]),
+            ("agnes_distill_grad", [dis, vp, mat, vp]),
+            ("agnes_distill_loss_grad", [dis, vp, mat, vp, u64, vp]),
+            ("agnes_mx4_quantize", [mat, mx, vp]),
+            ("agnes_mx4_dequantize", [mx, mat, vp]),
+            ("agnes_mx4_product_bytes", [i64, i64, i64, u64p]),
+            ("agnes_mx4_product", [mx, mx, vp, i32, mat, vp, u64, vp]),
+            ("agnes_mx4_linear_bytes", [i64, i64, i64, u64p]),
+            ("agnes_mx4_linear", [mat, mx, vp, i32, mat, vp, u64, vp])):
+        getattr(L, name).restype = st
+        getattr(L, name).argtypes = args
     L.agnes_free.restype = None
     L.agnes_free.argtypes = [vp]
     L.agnes_last_error.restype = ctypes.c_char_p
@@ -294,3 +336,89 @@ def agnes_free(handle: int | None) -> None:
 
 def agnes_last_error() -> str:
     return lib().agnes_last_error().decode(errors="replace")
+
+
+# Operators: structures by reference, device pointers as integers (None = NULL).
+
+def _bytes(fn, *sizes) -> int:
+    n = ctypes.c_uint64()
+    check(fn(*sizes, ctypes.byref(n)))
+    return n.value
+
+
+def agnes_embedding_lookup(table: agnes_matrix, ids, ids_dtype: int, scale: float, out: agnes_matrix,
+                           stream: int = 0) -> None:
+    check(lib().agnes_embedding_lookup(ctypes.byref(table), ids, ids_dtype, scale, ctypes.byref(out), stream))
+
+
+def agnes_embedding_grad_bytes(n: int, num_rows: int, dim: int) -> int:
+    return _bytes(lib().agnes_embedding_grad_bytes, n, num_rows, dim)
+
+
+def agnes_embedding_grad(grad_out: agnes_matrix, ids, ids_dtype: int, scale: float, accumulate: int,
+                         grad_table: agnes_matrix, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_embedding_grad(ctypes.byref(grad_out), ids, ids_dtype, scale, accumulate,
+                                     ctypes.byref(grad_table), workspace, workspace_bytes, stream))
+
+
+def agnes_embedding_grad_rows(grad_out: agnes_matrix, ids, ids_dtype: int, scale: float, num_rows: int, row_ids,
+                              rows: agnes_matrix, count, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_embedding_grad_rows(ctypes.byref(grad_out), ids, ids_dtype, scale, num_rows, row_ids,
+                                          ctypes.byref(rows), count, workspace, workspace_bytes, stream))
+
+
+def agnes_batch_embedding_lookup(batch: int, table: agnes_matrix, scale: float, out: agnes_matrix,
+                                 stream: int = 0) -> None:
+    check(lib().agnes_batch_embedding_lookup(batch, ctypes.byref(table), scale, ctypes.byref(out), stream))
+
+
+def agnes_batch_embedding_grad_rows(batch: int, grad_out: agnes_matrix, scale: float, row_ids, rows: agnes_matrix,
+                                    count, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_batch_embedding_grad_rows(batch, ctypes.byref(grad_out), scale, row_ids, ctypes.byref(rows),
+                                                count, workspace, workspace_bytes, stream))
+
+
+def agnes_distill_bytes(rows: int, classes: int) -> int:
+    return _bytes(lib().agnes_distill_bytes, rows, classes)
+
+
+def agnes_distill_loss(d: agnes_distill, loss, stats, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_distill_loss(ctypes.byref(d), loss, stats, workspace, workspace_bytes, stream))
+
+
+def agnes_distill_grad(d: agnes_distill, stats, grad: agnes_matrix, stream: int = 0) -> None:
+    check(lib().agnes_distill_grad(ctypes.byref(d), stats, ctypes.byref(grad), stream))
+
+
+def agnes_distill_loss_grad(d: agnes_distill, loss, grad: agnes_matrix, workspace, workspace_bytes: int,
+                            stream: int = 0) -> None:
+    check(lib().agnes_distill_loss_grad(ctypes.byref(d), loss, ctypes.byref(grad), workspace, workspace_bytes,
+                                        stream))
+
+
+def agnes_mx4_quantize(x: agnes_matrix, q: agnes_mx4, stream: int = 0) -> None:
+    check(lib().agnes_mx4_quantize(ctypes.byref(x), ctypes.byref(q), stream))
+
+
+def agnes_mx4_dequantize(q: agnes_mx4, x: agnes_matrix, stream: int = 0) -> None:
+    check(lib().agnes_mx4_dequantize(ctypes.byref(q), ctypes.byref(x), stream))
+
+
+def agnes_mx4_product_bytes(M: int, N: int, K: int) -> int:
+    return _bytes(lib().agnes_mx4_product_bytes, M, N, K)
+
+
+def agnes_mx4_product(x: agnes_mx4, w: agnes_mx4, bias, relu: int, out: agnes_matrix, workspace,
+                      workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_mx4_product(ctypes.byref(x), ctypes.byref(w), bias, relu, ctypes.byref(out), workspace,
+                                  workspace_bytes, stream))
+
+
+def agnes_mx4_linear_bytes(M: int, N: int, K: int) -> int:
+    return _bytes(lib().agnes_mx4_linear_bytes, M, N, K)
+
+
+def agnes_mx4_linear(x: agnes_matrix, w: agnes_mx4, bias, relu: int, out: agnes_matrix, workspace,
+                     workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_mx4_linear(ctypes.byref(x), ctypes.byref(w), bias, relu, ctypes.byref(out), workspace,
+                                 workspace_bytes, stream))

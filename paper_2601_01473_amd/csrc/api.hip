@@ -8,6 +8,7 @@
 #include <rocprofiler-sdk-roctx/roctx.h>
 
 #include "bucket.hpp"
+#include "ops.hpp"
 #include "runtime.hpp"
 
 namespace agnes {
@@ -72,6 +73,28 @@ static Store* as_store(void* p) {
     Store* s = static_cast<Store*>(p);
     AGNES_REQUIRE(s && s->magic == kStoreMagic, AGNES_ERR_INVALID, "not a store handle");
     return s;
+}
+
+void check_matrix(const agnes_matrix* m, bool output, const char* name) {
+    const std::string n(name);
+    AGNES_REQUIRE(m, AGNES_ERR_INVALID, n + " must not be NULL");
+    AGNES_REQUIRE(is_float(m->dtype), AGNES_ERR_INVALID, n + " must be float32, float16 or bfloat16");
+    AGNES_REQUIRE(m->rows >= 0 && m->cols >= 0 && m->rows < ((int64_t)1 << 31) && m->cols < ((int64_t)1 << 31),
+                  AGNES_ERR_INVALID, n + ": rows and cols must be in [0, 2^31)");
+    if (m->rows == 0 || m->cols == 0) return;
+    AGNES_REQUIRE(m->stride >= (output && m->rows > 1 ? m->cols : 0) && m->stride < ((int64_t)1 << 31),
+                  AGNES_ERR_INVALID,
+                  n + (output ? ": the stride must be in [cols, 2^31)" : ": the stride must be in [0, 2^31)"));
+    AGNES_REQUIRE(m->data, AGNES_ERR_INVALID, n + ".data must not be NULL");
+    AGNES_REQUIRE(((uintptr_t)m->data & (elem_size(m->dtype) - 1)) == 0, AGNES_ERR_INVALID,
+                  n + ".data is not aligned to its element type");
+}
+
+void check_workspace(const void* ws, uint64_t have, uint64_t need) {
+    if (need == 0) return;
+    AGNES_REQUIRE(ws && ((uintptr_t)ws & 255) == 0, AGNES_ERR_INVALID, "the workspace must be 256-byte aligned");
+    AGNES_REQUIRE(have >= need, AGNES_ERR_INVALID, "the workspace has " + std::to_string(have) + " bytes of " +
+                                                       std::to_string(need));
 }
 
 }  // namespace agnes
@@ -388,6 +411,113 @@ agnes_status agnes_set_device_allocator(agnes_device_alloc_fn alloc, agnes_devic
         a.alloc = alloc;
         a.release = release;
         a.user = alloc ? user : nullptr;
+    });
+}
+
+agnes_status agnes_embedding_lookup(const agnes_matrix* table, const void* ids, agnes_dtype ids_dtype, float scale,
+                                    const agnes_matrix* out, void* hip_stream) {
+    return guarded([&] { embedding_lookup(table, ids, ids_dtype, scale, out, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_embedding_grad_bytes(int64_t n, int64_t num_rows, int64_t dim, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = embedding_grad_bytes(n, num_rows, dim);
+    });
+}
+
+agnes_status agnes_embedding_grad(const agnes_matrix* grad_out, const void* ids, agnes_dtype ids_dtype, float scale,
+                                  int32_t accumulate, const agnes_matrix* grad_table, void* workspace,
+                                  uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        embedding_grad(grad_out, ids, ids_dtype, scale, accumulate != 0, grad_table, workspace, workspace_bytes,
+                       (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_embedding_grad_rows(const agnes_matrix* grad_out, const void* ids, agnes_dtype ids_dtype,
+                                       float scale, int64_t num_rows, int32_t* row_ids, const agnes_matrix* rows,
+                                       int64_t* count, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        embedding_grad_rows(grad_out, ids, ids_dtype, scale, num_rows, row_ids, rows, count, workspace,
+                            workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_batch_embedding_lookup(agnes_batch* batch, const agnes_matrix* table, float scale,
+                                          const agnes_matrix* out, void* hip_stream) {
+    return guarded([&] { batch_embedding_lookup(*as_batch(batch), table, scale, out, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_matrix* grad_out, float scale,
+                                             int32_t* row_ids, const agnes_matrix* rows, int64_t* count,
+                                             void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        batch_embedding_grad_rows(*as_batch(batch), grad_out, scale, row_ids, rows, count, workspace, workspace_bytes,
+                                  (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_distill_bytes(int64_t rows, int64_t classes, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = distill_bytes(rows, classes);
+    });
+}
+
+agnes_status agnes_distill_loss(const agnes_distill* d, float* loss, float* stats, void* workspace,
+                                uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        distill_loss(d, loss, stats, nullptr, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_distill_grad(const agnes_distill* d, const float* stats, const agnes_matrix* grad,
+                                void* hip_stream) {
+    return guarded([&] { distill_grad(d, stats, grad, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_distill_loss_grad(const agnes_distill* d, float* loss, const agnes_matrix* grad, void* workspace,
+                                     uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        AGNES_REQUIRE(grad, AGNES_ERR_INVALID, "grad must not be NULL");
+        distill_loss(d, loss, nullptr, grad, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_mx4_quantize(const agnes_matrix* x, const agnes_mx4* q, void* hip_stream) {
+    return guarded([&] { mx4_quantize(x, q, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, void* hip_stream) {
+    return guarded([&] { mx4_dequantize(q, x, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_mx4_product_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = mx4_product_bytes(M, N, K);
+    });
+}
+
+agnes_status agnes_mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, int32_t relu,
+                               const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        mx4_product(x, w, bias, relu != 0, out, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_mx4_linear_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = mx4_linear_bytes(M, N, K);
+    });
+}
+
+agnes_status agnes_mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const float* bias, int32_t relu,
+                              const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        mx4_linear(x, w, bias, relu != 0, out, workspace, workspace_bytes, (hipStream_t)hip_stream);
     });
 }
 

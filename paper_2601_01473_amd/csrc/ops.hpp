@@ -1,0 +1,98 @@
+// What the operator kernels (embed.hip, distill.hip, mx4.hip) share: element
+// types, vector accesses at element alignment, argument checks and the host
+// entry points that api.hip wraps.
+#pragma once
+
+#include "device.hpp"
+#include "runtime.hpp"
+
+namespace agnes {
+
+// ----------------------------------------------------------------- elements
+
+// float, _Float16 and __bf16 convert to and from float with single
+// instructions; conversions to 16 bits round to nearest, ties to even, and keep
+// NaN and infinities.
+template <typename T> __device__ __forceinline__ float to_float(T x) { return (float)x; }
+template <typename T> __device__ __forceinline__ T from_float(float x) { return (T)x; }
+
+// E consecutive elements, loaded or stored at element alignment: rows of any
+// length and stride start anywhere, and the memory system takes wide accesses
+// at any address.
+template <typename T, int E> struct Vec {
+    typedef T type __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    static __device__ __forceinline__ void load(const T* p, float (&x)[E]) {
+        const type v = *(const type*)p;
+#pragma unroll
+        for (int q = 0; q < E; q++) x[q] = (float)v[q];
+    }
+    static __device__ __forceinline__ void store(T* p, const float (&x)[E]) {
+        type v;
+#pragma unroll
+        for (int q = 0; q < E; q++) v[q] = (T)x[q];
+        *(type*)p = v;
+    }
+};
+
+// ----------------------------------------------------------------- host side
+
+inline size_t elem_size(agnes_dtype t) { return t == AGNES_FLOAT32 ? 4 : 2; }
+inline bool is_float(agnes_dtype t) { return t == AGNES_FLOAT32 || t == AGNES_FLOAT16 || t == AGNES_BFLOAT16; }
+inline bool is_index(agnes_dtype t) { return t == AGNES_INT32 || t == AGNES_INT64; }
+
+// Calls f with a value of the element type.
+template <typename F> void with_float(agnes_dtype t, F&& f) {
+    if (t == AGNES_FLOAT32) f(float{});
+    else if (t == AGNES_FLOAT16) f(_Float16{});
+    else f(__bf16{});
+}
+template <typename F> void with_index(agnes_dtype t, F&& f) {
+    if (t == AGNES_INT64) f(int64_t{});
+    else f(int32_t{});
+}
+
+void check_matrix(const agnes_matrix* m, bool output, const char* name);
+void check_workspace(const void* ws, uint64_t have, uint64_t need);
+
+// Parts of a caller's workspace, each aligned to 256 bytes.
+struct Carve {
+    char* base;
+    size_t used = 0;
+    explicit Carve(void* p) : base((char*)p) {}
+    template <typename T> T* take(int64_t n) {
+        T* p = (T*)(base + used);
+        used += ((size_t)n * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// ----------------------------------------------------------------- entry points
+
+void embedding_lookup(const agnes_matrix* table, const void* ids, agnes_dtype ids_dtype, float scale,
+                      const agnes_matrix* out, hipStream_t st);
+uint64_t embedding_grad_bytes(int64_t n, int64_t num_rows, int64_t dim);
+void embedding_grad(const agnes_matrix* grad_out, const void* ids, agnes_dtype ids_dtype, float scale,
+                    bool accumulate, const agnes_matrix* grad_table, void* ws, uint64_t ws_bytes, hipStream_t st);
+void embedding_grad_rows(const agnes_matrix* grad_out, const void* ids, agnes_dtype ids_dtype, float scale,
+                         int64_t num_rows, int32_t* row_ids, const agnes_matrix* rows, int64_t* count, void* ws,
+                         uint64_t ws_bytes, hipStream_t st);
+void batch_embedding_lookup(Batch& b, const agnes_matrix* table, float scale, const agnes_matrix* out,
+                            hipStream_t st);
+void batch_embedding_grad_rows(Batch& b, const agnes_matrix* grad_out, float scale, int32_t* row_ids,
+                               const agnes_matrix* rows, int64_t* count, void* ws, uint64_t ws_bytes, hipStream_t st);
+
+uint64_t distill_bytes(int64_t rows, int64_t classes);
+void distill_loss(const agnes_distill* d, float* loss, float* stats, const agnes_matrix* grad, void* ws,
+                  uint64_t ws_bytes, hipStream_t st);
+void distill_grad(const agnes_distill* d, const float* stats, const agnes_matrix* grad, hipStream_t st);
+
+void mx4_quantize(const agnes_matrix* x, const agnes_mx4* q, hipStream_t st);
+void mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, hipStream_t st);
+uint64_t mx4_product_bytes(int64_t M, int64_t N, int64_t K);
+void mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, bool relu, const agnes_matrix* out,
+                 void* ws, uint64_t ws_bytes, hipStream_t st);
+uint64_t mx4_linear_bytes(int64_t M, int64_t N, int64_t K);
+void mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const float* bias, bool relu, const agnes_matrix* out,
+                void* ws, uint64_t ws_bytes, hipStream_t st);
+
+}  // namespace agnes

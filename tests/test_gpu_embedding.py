@@ -1,0 +1,332 @@
+"""Embedding lookup and its gradient on the GPU against the definition in 64 bits (tests/operators_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+from tests import operators_ref as ref
+from tests.graphs import distinct_targets, features, random_graph
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def ag():
+    import paper_2601_01473_amd as m
+    return m
+
+
+def make_ids(n, V, skew, dtype, seed, padding=True):
+    g = torch.Generator().manual_seed(seed)
+    i = (V * torch.rand(n, generator=g, dtype=torch.float64) ** skew).long().clamp(max=max(V - 1, 0))
+    if padding and n > 3:
+        i[::5] = -1
+        i[3::17] = V
+        i[4::19] = torch.iinfo(dtype).min
+        i[1::23] = torch.iinfo(dtype).max
+    return i.to(dtype).cuda()
+
+
+def normal(shape, dtype, seed):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+SIZES = [(1, 1, 1), (7, 3, 5), (100, 64, 33), (1000, 75, 777), (50, 257, 300), (4000, 128, 5000), (3, 1024, 130),
+         (65, 1537, 129), (30000, 8, 20000), (2000, 2, 9000)]
+
+
+# ----------------------------------------------------------------- lookup
+
+@pytest.mark.parametrize("V,D,n", SIZES)
+@pytest.mark.parametrize("tin,tout,tid", [(F32, F32, torch.int32), (F32, BF16, torch.int64), (BF16, BF16, torch.int32),
+                                          (F16, F32, torch.int32), (BF16, F16, torch.int64)])
+def test_lookup(ag, V, D, n, tin, tout, tid):
+    table, ids = normal((V, D), tin, 1), make_ids(n, V, 1.5, tid, 2)
+    got = ag.embedding_lookup(table, ids, scale=3.3, dtype=tout)
+    ref.within(got, *ref.lookup(table, ids, 3.3), "lookup")
+
+
+@pytest.mark.parametrize("tin", [F32, F16, BF16])
+@pytest.mark.parametrize("tout", [F32, F16, BF16])
+def test_lookup_every_pair_of_types(ag, tin, tout):
+    table, ids = normal((40, 21), tin, 3), make_ids(90, 40, 1.0, torch.int32, 4)
+    ref.within(ag.embedding_lookup(table, ids, scale=0.5, dtype=tout), *ref.lookup(table, ids, 0.5))
+
+
+def test_lookup_strides_offsets_and_shapes(ag):
+    big = normal((60, 50), BF16, 5)
+    table = big[3:43, 5:42]                                   # rows start at odd places, 50 elements apart
+    ids = make_ids(24, 40, 1.0, torch.int32, 6).view(2, 3, 4)
+    got = ag.embedding_lookup(table, ids, scale=2.0)
+    assert got.shape == (2, 3, 4, 37)
+    ref.within(got.view(-1, 37), *ref.lookup(table, ids, 2.0))
+    out = torch.full((24, 64), 7.0, device="cuda", dtype=F32)
+    ag.embedding_lookup(table, ids.view(-1), out=out[:, 11:48])
+    ref.within(out[:, 11:48], *ref.lookup(table, ids, 1.0))
+    assert bool((out[:, :11] == 7).all()) and bool((out[:, 48:] == 7).all())
+    # transposed ids, one row for all table rows
+    ids2 = make_ids(24, 40, 1.0, torch.int64, 7).view(4, 6).t()
+    one = normal((1, 9), F32, 8).expand(40, 9)
+    ref.within(ag.embedding_lookup(one, ids2).view(-1, 9), *ref.lookup(one, ids2, 1.0))
+
+
+def test_lookup_empty(ag):
+    table = normal((5, 4), F32, 1)
+    assert ag.embedding_lookup(table, torch.empty(0, dtype=torch.int32, device="cuda")).shape == (0, 4)
+    assert ag.embedding_lookup(table[:, :0], torch.zeros(3, dtype=torch.int32, device="cuda")).shape == (3, 0)
+    got = ag.embedding_lookup(table[:0], torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert bool((got == 0).all())                             # a table without rows: every id is padding
+
+
+def test_lookup_keeps_infinities_and_ignores_rows_not_named(ag):
+    table = torch.full((4, 5), float("nan"), device="cuda")
+    table[1] = torch.tensor([1.0, float("inf"), -float("inf"), 0.0, float("nan")])
+    got = ag.embedding_lookup(table, torch.tensor([1, -1], dtype=torch.int32, device="cuda"), scale=2.0, dtype=BF16)
+    assert got[0, :4].tolist() == [2.0, float("inf"), -float("inf"), 0.0] and bool(got[0, 4].isnan())
+    assert bool((got[1] == 0).all())
+
+
+def test_lookup_offsets_past_32_bits(ag):
+    V, D = 1_050_000, 2100                                    # 2.2e9 elements, 4.4 GB
+    table = torch.empty(V, D, dtype=BF16, device="cuda")
+    ids = torch.tensor([0, 1_022_613, 1_022_614, V - 1, 511_305], dtype=torch.int32, device="cuda")
+    table[ids.long()] = normal((5, D), BF16, 9)
+    got = ag.embedding_lookup(table, ids, scale=1.0)
+    assert torch.equal(got, table[ids.long()])
+
+
+# ----------------------------------------------------------------- gradient
+
+def check_dense(ag, g, ids, V, scale=1.5, dtype=None):
+    got = ag.embedding_grad(g, ids, V, scale=scale, dtype=dtype)
+    names, rows, err = ref.grad(g, ids, V, scale)
+    want, e = torch.zeros(V, g.shape[-1], dtype=torch.float64), torch.zeros(V, g.shape[-1], dtype=torch.float64)
+    want[names], e[names] = rows, err
+    ref.within(got, want, e, "dense gradient")
+    return got
+
+
+def check_rows(ag, g, ids, V, scale=1.5, dtype=None, max_rows=None):
+    row_ids, rows, count = ag.embedding_grad_rows(g, ids, V, max_rows, scale=scale, dtype=dtype)
+    names, want, err = ref.grad(g, ids, V, scale)
+    assert int(count) == len(names)
+    m = min(len(names), len(row_ids))
+    assert torch.equal(row_ids[:m].cpu().long(), names[:m])
+    assert bool((row_ids[m:] == -1).all())
+    ref.within(rows[:m], want[:m], err[:m], "gradient rows")
+    return row_ids, rows, count
+
+
+@pytest.mark.parametrize("V,D,n", SIZES + [(1 << 21, 3, 4000), (100, 40, 30000), (70000, 65, 40000)])
+@pytest.mark.parametrize("tin,tout,tid,skew", [(F32, F32, torch.int32, 1.0), (BF16, BF16, torch.int64, 4.0),
+                                               (BF16, F32, torch.int32, 2.0)])
+def test_grad(ag, V, D, n, tin, tout, tid, skew):
+    g, ids = normal((n, D), tin, 11), make_ids(n, V, skew, tid, 12)
+    if V * D < 1 << 24:
+        check_dense(ag, g, ids, V, dtype=tout)
+    check_rows(ag, g, ids, V, dtype=tout)
+
+
+@pytest.mark.parametrize("tin", [F32, F16, BF16])
+@pytest.mark.parametrize("tout", [F32, F16, BF16])
+def test_grad_every_pair_of_types(ag, tin, tout):
+    g, ids = normal((500, 19), tin, 13), make_ids(500, 60, 2.0, torch.int32, 14)
+    check_dense(ag, g, ids, 60, dtype=tout)
+    check_rows(ag, g, ids, 60, dtype=tout)
+
+
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 64, 1000, 4095, 4096, 4097, 70001])
+@pytest.mark.parametrize("D", [4, 96])
+def test_grad_of_one_id(ag, n, D):
+    """Every position names the same row: the longest run there can be."""
+    g = normal((n, D), F32, 15)
+    ids = torch.full((n,), 2, dtype=torch.int32, device="cuda")
+    check_dense(ag, g, ids, 4)
+    check_rows(ag, g, ids, 4)
+
+
+@pytest.mark.parametrize("n", [1, 40, 5000])
+def test_grad_of_padding_alone(ag, n):
+    g = torch.full((n, 7), float("nan"), device="cuda")
+    ids = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    assert bool((ag.embedding_grad(g, ids, 11) == 0).all())
+    row_ids, rows, count = ag.embedding_grad_rows(g, ids, 11)
+    assert int(count) == 0 and bool((row_ids == -1).all())
+
+
+def test_grad_ignores_what_padding_rows_hold(ag):
+    g, ids = normal((6000, 20), BF16, 16), make_ids(6000, 100, 2.0, torch.int32, 17)
+    clean = check_dense(ag, torch.where(((ids >= 0) & (ids < 100))[:, None], g, 0), ids, 100)
+    g[(ids < 0) | (ids >= 100)] = float("nan")
+    assert torch.equal(ag.embedding_grad(g, ids, 100, scale=1.5), clean)
+
+
+def test_grad_long_and_short_runs_mixed(ag):
+    """Runs that begin and end at, before and behind every boundary a split of the sorted list could have."""
+    lengths = [1, 1, 31, 33, 63, 1, 64, 65, 127, 2, 129, 1, 1, 4000, 3, 5, 2500, 32, 32, 32, 1, 700, 8, 8, 8, 8, 16]
+    ids = torch.repeat_interleave(torch.arange(len(lengths)), torch.tensor(lengths))
+    perm = torch.randperm(len(ids), generator=torch.Generator().manual_seed(1))
+    for D in (5, 64, 600):
+        g = normal((len(ids), D), F32, 18)
+        check_dense(ag, g, ids[perm].int().cuda(), len(lengths) + 2)
+        check_rows(ag, g, ids[perm].cuda(), 1 << 20)
+
+
+def test_grad_rows_with_less_room_than_ids(ag):
+    for n in (300, 9000):
+        g, ids = normal((n, 10), F32, 19), make_ids(n, 200, 1.0, torch.int32, 20)
+        check_rows(ag, g, ids, 200, max_rows=7)
+        check_rows(ag, g, ids, 200, max_rows=0)
+        check_rows(ag, g, ids, 200, max_rows=1000)
+
+
+def test_grad_accumulates(ag):
+    for n, V in ((50, 80), (7000, 300)):
+        g, ids = normal((n, 33), BF16, 21), make_ids(n, V, 2.0, torch.int32, 22)
+        for dtype in (F32, BF16):
+            out = normal((V, 33), dtype, 23)
+            before = out.clone()
+            ag.embedding_grad(g, ids, V, scale=0.25, out=out, accumulate=True)
+            names, rows, err = ref.grad(g, ids, V, 0.25)
+            want = before.cpu().double()
+            e = torch.zeros_like(want)
+            e[names] = err + ref.U * (want[names].abs() + rows.abs() + err)
+            want[names] += rows
+            ref.within(out, want, e, "accumulated")
+            untouched = torch.ones(V, dtype=torch.bool)
+            untouched[names] = False
+            assert torch.equal(out.cpu()[untouched], before.cpu()[untouched])
+
+
+def test_grad_strides(ag):
+    ids = make_ids(700, 90, 2.0, torch.int32, 24)
+    wide = normal((700, 100), BF16, 25)
+    check_dense(ag, wide[:, 3:80], ids, 90)
+    check_rows(ag, normal((1, 40), F32, 26).expand(700, 40), ids, 90)          # one row for all, stride 0
+    got = ag.embedding_grad(torch.ones((), device="cuda").expand(700, 6), ids, 90)   # a sum's gradient: both strides 0
+    count = torch.bincount(ids[(ids >= 0) & (ids < 90)].long(), minlength=90)
+    assert torch.equal(got, count[:, None].float().expand(90, 6))
+    out = torch.full((90, 50), 9.0, device="cuda")
+    ag.embedding_grad(wide[:, :40], ids, 90, out=out[:, 5:45])
+    assert bool((out[:, :5] == 9).all()) and bool((out[:, 45:] == 9).all())
+    names, rows, err = ref.grad(wide[:, :40], ids, 90, 1.0)
+    want, e = torch.zeros(90, 40, dtype=torch.float64), torch.zeros(90, 40, dtype=torch.float64)
+    want[names], e[names] = rows, err
+    ref.within(out[:, 5:45], want, e)
+
+
+def test_grad_empty(ag):
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert bool((ag.embedding_grad(torch.empty(0, 5, device="cuda"), none, 3) == 0).all())
+    row_ids, rows, count = ag.embedding_grad_rows(torch.empty(0, 5, device="cuda"), none, 3, 2)
+    assert int(count) == 0 and bool((row_ids == -1).all())
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    assert ag.embedding_grad(torch.ones(4, 0, device="cuda"), ids, 3).shape == (3, 0)
+    row_ids, rows, count = ag.embedding_grad_rows(torch.ones(4, 0, device="cuda"), ids, 3, 2)
+    assert int(count) == 1 and row_ids.tolist() == [0, -1]
+    assert ag.embedding_grad(torch.ones(4, 2, device="cuda"), ids, 0).shape == (0, 2)
+
+
+def test_grad_infinities_stay_in_their_row(ag):
+    g = normal((5000, 9), F32, 27)
+    ids = make_ids(5000, 40, 1.0, torch.int32, 28, padding=False)
+    g[17] = float("inf")
+    got = ag.embedding_grad(g, ids, 40)
+    row = int(ids[17])
+    assert bool(torch.isinf(got[row]).all())
+    rest = torch.arange(40, device="cuda") != row
+    assert bool(torch.isfinite(got[rest]).all())
+
+
+def test_grad_is_the_lookups_transpose(ag):
+    """<lookup(E + dE) - lookup(E), G> = <dE, grad(G)>: the lookup is linear, so differences are exact up to rounding."""
+    V, D, n = 300, 24, 5000
+    E, dE, G = normal((V, D), F32, 29), normal((V, D), F32, 30), normal((n, D), F32, 31)
+    ids = make_ids(n, V, 2.0, torch.int32, 32)
+    diff = ag.embedding_lookup(E + dE, ids, scale=2.0).double() - ag.embedding_lookup(E, ids, scale=2.0).double()
+    a = float((diff * G.double()).sum())
+    b = float((dE.double() * ag.embedding_grad(G, ids, V, scale=2.0).double()).sum())
+    size = float((ag.embedding_lookup(dE.abs() + 2 * E.abs(), ids, scale=2.0).double() * G.abs().double()).sum())
+    assert abs(a - b) <= 4 * (n + 4) * ref.U * size
+
+
+def test_grad_same_bits_every_time(ag):
+    g, ids = normal((30000, 64), F32, 33), make_ids(30000, 500, 5.0, torch.int32, 34)
+    first = ag.embedding_grad(g, ids, 500)
+    for _ in range(3):
+        assert torch.equal(ag.embedding_grad(g, ids, 500), first)
+    row_ids, rows, count = ag.embedding_grad_rows(g, ids.long().where(ids < 500, -1), 500)
+    m = int(count)
+    assert torch.equal(rows[:m], first[row_ids[:m].long()])
+
+
+def test_grad_on_another_stream_and_in_a_graph(ag):
+    g, ids = normal((9000, 40), F32, 35), make_ids(9000, 800, 3.0, torch.int32, 36)
+    want = ag.embedding_grad(g, ids, 800)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = ag.embedding_grad(g, ids, 800, stream=side)
+    look = ag.embedding_lookup(g, ids, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(look, ag.embedding_lookup(g, ids))
+    for n in (9000, 500):
+        gs, is_ = g[:n].clone(), ids[:n].clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dense = ag.embedding_grad(gs, is_, 800)
+            row_ids, rows, count = ag.embedding_grad_rows(gs, is_, 800)
+        for k in range(3):
+            gs.copy_(normal((n, 40), F32, 40 + k))
+            is_.copy_(make_ids(n, 800, 2.0 + k, torch.int32, 50 + k))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(dense, ag.embedding_grad(gs, is_, 800))
+            r2, w2, c2 = ag.embedding_grad_rows(gs, is_, 800)
+            m = int(c2)
+            assert int(count) == m and torch.equal(row_ids, r2) and torch.equal(rows[:m], w2[:m])
+
+
+def test_grad_offsets_past_32_bits(ag):
+    V, D, n = 1_050_000, 2100, 5000
+    g = normal((n, D), F32, 37)
+    ids = make_ids(n, 40, 1.0, torch.int32, 38, padding=False)
+    ids = torch.where(ids < 20, ids, V - 1 - ids)
+    out = torch.full((V, D), 5.0, dtype=BF16, device="cuda")
+    ag.embedding_grad(g, ids, V, out=out)
+    names, rows, err = ref.grad(g, ids, V, 1.0)
+    ref.within(out[names.cuda()], rows, err)
+    out[names.cuda()] = 0
+    assert not bool(out.any())
+
+
+# ----------------------------------------------------------------- a batch's nodes
+
+def test_batch_embedding(ag):
+    off, idx = random_graph(3000, 9, seed=1, hubs=3, hub_deg=900)
+    store = ag.Store(off, idx, features(3000, 16, 2), 256)
+    table = normal((3000, 40), F32, 41)
+    batch, side = None, torch.cuda.Stream()
+    for step in range(3):
+        batch = store.prepare(distinct_targets(3000, 5, 30, step), [6, 4], seed=step, batch=batch)
+        nodes = torch.from_numpy(np.concatenate([m["nodes"] for m in batch.to_host(features=False)]))
+        got = batch.embedding(table, scale=2.0, dtype=BF16)
+        ref.within(got, *ref.lookup(table, nodes, 2.0))
+        g = normal((len(nodes), 40), BF16, 42 + step)
+        torch.cuda.synchronize()
+        row_ids, rows, count = batch.embedding_grad_rows(g, scale=2.0, dtype=F32, stream=side)
+        names, want, err = ref.grad(g, nodes, 3000, 2.0)
+        side.synchronize()
+        assert int(count) == len(names) == len(row_ids) == batch.stats()["distinct_rows"]
+        assert torch.equal(row_ids.cpu().long(), names)
+        ref.within(rows, want, err)
+    with pytest.raises(ag.AgnesError):
+        batch.embedding(table[:2999])
+    with pytest.raises(ag.AgnesError):
+        batch.embedding(table, out=torch.empty(3, 40, device="cuda"))
+    with pytest.raises(ag.AgnesError):
+        batch.embedding_grad_rows(torch.empty(3, 40, device="cuda"))
+    batch.close()
+    store.close()

@@ -1,0 +1,202 @@
+"""What the operators refuse, on the host: every bad argument is an error before any device work (the device pointers
+here are never read).  The wrappers' refusals of tensors need CUDA tensors and are marked so."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2601_01473_amd as ag
+from paper_2601_01473_amd import _binding as B
+
+P = 1 << 20                       # an address that is never used
+BIG = 1 << 40
+
+
+def mat(rows=4, cols=8, stride=None, dtype=B.AGNES_FLOAT32, data=P):
+    return B.agnes_matrix(data, rows, cols, cols if stride is None else stride, dtype)
+
+
+def mx(rows=4, cols=64, codes=P, scales=P):
+    return B.agnes_mx4(codes, scales, rows, cols)
+
+
+def refused(call, *words):
+    with pytest.raises(B.AgnesError) as e:
+        call()
+    assert e.value.status == B.AGNES_ERR_INVALID, e.value
+    for w in words:
+        assert w in str(e.value), (w, str(e.value))
+
+
+BAD_MATRICES = [(dict(dtype=B.AGNES_INT32), "float32, float16 or bfloat16"), (dict(dtype=99), "float32"),
+                (dict(rows=-1), "rows and cols"), (dict(cols=1 << 31), "rows and cols"), (dict(data=None), "NULL"),
+                (dict(stride=-1), "stride"), (dict(stride=1 << 31), "stride"), (dict(data=P + 2), "aligned")]
+
+
+@pytest.mark.parametrize("bad,word", BAD_MATRICES)
+def test_bad_matrices(bad, word):
+    out = mat(3, bad.get("cols", 8))
+    refused(lambda: B.agnes_embedding_lookup(mat(**bad), P, B.AGNES_INT32, 1.0, out), "table", word)
+    refused(lambda: B.agnes_mx4_quantize(mat(**bad), mx()), "x", word)
+    refused(lambda: B.agnes_embedding_grad(mat(**bad), P, B.AGNES_INT32, 1.0, 0, mat(), P, BIG), "grad_out", word)
+
+
+def test_null_structures():
+    lib = B.lib()
+    assert lib.agnes_embedding_lookup(None, None, B.AGNES_INT32, 1.0, None, None) == B.AGNES_ERR_INVALID
+    assert "table" in ag.agnes_last_error()
+    assert lib.agnes_embedding_grad(None, None, B.AGNES_INT32, 1.0, 0, None, None, 0, None) == B.AGNES_ERR_INVALID
+    assert lib.agnes_embedding_grad_rows(None, None, B.AGNES_INT32, 1.0, 3, None, None, None, None, 0, None) == 1
+    assert lib.agnes_distill_loss(None, None, None, None, 0, None) == 1
+    assert lib.agnes_distill_grad(None, None, None, None) == 1
+    assert lib.agnes_distill_loss_grad(None, None, None, None, 0, None) == 1
+    assert lib.agnes_mx4_quantize(None, None, None) == 1
+    assert lib.agnes_mx4_dequantize(None, None, None) == 1
+    assert lib.agnes_mx4_product(None, None, None, 0, None, None, 0, None) == 1
+    assert lib.agnes_mx4_linear(None, None, None, 0, None, None, 0, None) == 1
+    for f, n in ((lib.agnes_embedding_grad_bytes, 3), (lib.agnes_mx4_product_bytes, 3), (lib.agnes_mx4_linear_bytes, 3),
+                 (lib.agnes_distill_bytes, 2)):
+        assert f(*[1] * n, None) == B.AGNES_ERR_INVALID
+
+
+def test_lookup_arguments():
+    call = lambda t=mat(), i=P, d=B.AGNES_INT32, o=mat(3): B.agnes_embedding_lookup(t, i, d, 1.0, o)   # noqa: E731
+    refused(lambda: call(d=B.AGNES_FLOAT32), "int32 or int64")
+    refused(lambda: call(i=None), "ids")
+    refused(lambda: call(o=mat(3, 9)), "columns")
+    refused(lambda: call(o=mat(3, stride=7)), "stride")
+    refused(lambda: call(o=mat(3, stride=0)), "stride")
+    refused(lambda: call(t=mat(rows=(1 << 31) - 1)), "2^31 - 1")
+
+
+def test_grad_arguments():
+    def dense(g=mat(), i=P, d=B.AGNES_INT32, o=mat(6), ws=P, n=BIG):
+        B.agnes_embedding_grad(g, i, d, 1.0, 0, o, ws, n)
+
+    def rows(g=mat(), i=P, V=6, ids=P, o=mat(3), count=P, ws=P, n=BIG):
+        B.agnes_embedding_grad_rows(g, i, B.AGNES_INT32, 1.0, V, ids, o, count, ws, n)
+    refused(lambda: dense(d=B.AGNES_BFLOAT16), "int32 or int64")
+    refused(lambda: dense(i=None), "ids")
+    refused(lambda: dense(o=mat(6, 7)), "columns")
+    refused(lambda: dense(o=mat(6, stride=3)), "stride")
+    need = B.agnes_embedding_grad_bytes(4, 6, 8)
+    refused(lambda: dense(n=need - 1), "workspace", str(need))
+    refused(lambda: dense(ws=None), "workspace")
+    refused(lambda: dense(ws=P + 128), "aligned")
+    refused(lambda: rows(count=None), "count")
+    refused(lambda: rows(ids=None), "row_ids")
+    refused(lambda: rows(V=-1), "rows")
+    refused(lambda: rows(V=(1 << 31) - 1), "2^31 - 1")
+    refused(lambda: rows(n=need - 1), "workspace")
+    refused(lambda: B.agnes_embedding_grad_bytes(4, -1, 8))
+    refused(lambda: B.agnes_embedding_grad_bytes(4, 6, -8))
+    with pytest.raises(B.AgnesError) as e:
+        B.agnes_embedding_grad_bytes(1 << 31, 6, 8)
+    assert e.value.status == B.AGNES_ERR_RANGE
+
+
+def test_batch_calls_need_a_batch():
+    bogus = (ctypes.c_uint32 * 4)()
+    h = ctypes.cast(bogus, ctypes.c_void_p).value
+    refused(lambda: B.agnes_batch_embedding_lookup(h, mat(), 1.0, mat()), "batch")
+    refused(lambda: B.agnes_batch_embedding_grad_rows(h, mat(), 1.0, P, mat(), P, P, BIG), "batch")
+
+
+def dis(z=None, t=None, classes=P, cstride=3, index=B.AGNES_INT32, labels=None, weight=None, T=1.0, soft=1.0, hard=0.0):
+    return B.agnes_distill(z or mat(4, 9), t or mat(4, 3), classes, cstride, index, labels, weight, T, soft, hard)
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(z=mat(4, 0)), "at least one class"), (dict(t=mat(5, 3)), "equal rows"), (dict(t=mat(4, 1025)), "1024"),
+    (dict(z=mat(4, 9, dtype=B.AGNES_INT64)), "logits"), (dict(t=mat(4, 3, data=None)), "teacher"),
+    (dict(index=B.AGNES_FLOAT16), "int32 or int64"), (dict(classes=None), "classes"), (dict(cstride=-1), "classes_stride"),
+    (dict(T=0.0), "temperature"), (dict(T=-1.0), "temperature"), (dict(T=float("nan")), "temperature"),
+    (dict(T=float("inf")), "temperature"), (dict(T=1e-45), "temperature"), (dict(soft=-0.5), "soft"),
+    (dict(hard=float("nan")), "hard"), (dict(soft=float("inf")), "soft")])
+def test_distill_descriptor(kw, word):
+    d = dis(**kw)
+    refused(lambda: B.agnes_distill_loss(d, P, P, P, BIG), word)
+    refused(lambda: B.agnes_distill_grad(d, P, mat(4, 9)), word)
+    refused(lambda: B.agnes_distill_loss_grad(d, P, mat(4, 9), P, BIG), word)
+
+
+def test_distill_outputs():
+    d = dis()
+    refused(lambda: B.agnes_distill_loss(d, None, P, P, BIG), "loss")
+    refused(lambda: B.agnes_distill_loss_grad(d, None, mat(4, 9), P, BIG), "loss")
+    refused(lambda: B.agnes_distill_grad(d, None, mat(4, 9)), "stats")
+    for g, word in ((mat(4, 8), "shape"), (mat(5, 9), "shape"), (mat(4, 9, stride=8), "stride"),
+                    (mat(4, 9, dtype=B.AGNES_FLOAT16), "share"), (mat(4, 9, stride=10), "share"),
+                    (mat(4, 9, data=None), "grad")):
+        refused(lambda: B.agnes_distill_grad(d, P, g), word)
+        refused(lambda: B.agnes_distill_loss_grad(d, P, g, P, BIG), word)
+    refused(lambda: B.agnes_distill_bytes(-1, 4))
+    refused(lambda: B.agnes_distill_bytes(4, 1 << 31))
+    need = B.agnes_distill_bytes(1, 1 << 20)
+    if need:
+        one = dis(z=mat(1, 1 << 20), t=mat(1, 3))
+        refused(lambda: B.agnes_distill_loss(one, P, P, P, need - 1), "workspace")
+
+
+def test_mx4_arguments():
+    x = mat(4, 64)
+    for q, word in ((mx(5), "equal shapes"), (mx(4, 65), "equal shapes"), (mx(codes=None), "NULL"),
+                    (mx(scales=None), "NULL"), (mx(codes=P + 8), "16-byte"), (mx(rows=-1), "rows and cols")):
+        refused(lambda: B.agnes_mx4_quantize(x, q), word)
+        refused(lambda: B.agnes_mx4_dequantize(q, x), word)
+    out = mat(4, 7)
+
+    def product(a=mx(4), w=mx(7), o=out, ws=P, n=BIG):
+        B.agnes_mx4_product(a, w, None, 0, o, ws, n)
+
+    def linear(a=x, w=mx(7), o=out, ws=P, n=BIG):
+        B.agnes_mx4_linear(a, w, None, 0, o, ws, n)
+    refused(lambda: product(w=mx(7, 96)), "equal columns")
+    refused(lambda: linear(w=mx(7, 96)), "equal columns")
+    refused(lambda: product(o=mat(5, 7)), "out")
+    refused(lambda: linear(o=mat(4, 8)), "out")
+    refused(lambda: linear(o=mat(4, 7, stride=6)), "stride")
+    need = B.agnes_mx4_linear_bytes(4, 7, 64)
+    assert need >= 4 * 34
+    refused(lambda: linear(n=need - 1), "workspace")
+    refused(lambda: linear(ws=None), "workspace")
+    refused(lambda: B.agnes_mx4_product_bytes(1, -1, 1))
+    refused(lambda: B.agnes_mx4_linear_bytes(1, 1, 1 << 31))
+
+
+def test_host_tensors_are_refused():
+    x, i = torch.zeros(3, 4), torch.zeros(3, dtype=torch.int32)
+    for call in (lambda: ag.embedding_lookup(x, i), lambda: ag.embedding_grad(x, i, 5),
+                 lambda: ag.embedding_grad_rows(x, i, 5), lambda: ag.mx4_quantize(x),
+                 lambda: ag.distill_loss(x, x, i), lambda: ag.distill_loss_grad(x, x, i)):
+        with pytest.raises(TypeError):
+            call()
+
+
+@pytest.mark.gpu
+def test_tensors_of_the_wrong_kind_are_refused():
+    x, i = torch.zeros(6, 4, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    c = torch.zeros(6, 4, dtype=torch.int32, device="cuda")
+    q = ag.mx4_quantize(x)
+    types = [lambda: ag.embedding_lookup(x.double(), i), lambda: ag.embedding_lookup(x, i.float()),
+             lambda: ag.embedding_lookup(x, i, out=torch.zeros(6, 4)), lambda: ag.mx4_quantize(x.int()),
+             lambda: ag.distill_loss(x, x, x)]
+    values = [lambda: ag.embedding_lookup(x[0], i), lambda: ag.embedding_lookup(x.t(), i),
+              lambda: ag.embedding_lookup(x, i, out=x[:5]), lambda: ag.embedding_lookup(x, i, dtype=torch.float16, out=x),
+              lambda: ag.embedding_grad(x, i[:5], 9), lambda: ag.embedding_grad(x, i, 9, accumulate=True),
+              lambda: ag.embedding_grad(x, i, 9, out=x), lambda: ag.distill_loss(x, x, c[:, :3]),
+              lambda: ag.distill_loss(x, x, c, labels=i[:5]), lambda: ag.distill_loss(x, x, c, labels=i.long()),
+              lambda: ag.distill_loss(x, x, c, weight=i.float()[:5]), lambda: ag.distill_loss(x, x, c, weight=i),
+              lambda: ag.distill_loss_grad(x, x, c, out=x[:5]), lambda: ag.distill_grad(x, x, c, x[:, :3]),
+              lambda: ag.mx4_dequantize(q._replace(cols=40)), lambda: ag.mx4_linear(x, q, bias=x[0]),
+              lambda: ag.mx4_linear(x, q, out=x)]
+    for call in types:
+        with pytest.raises(TypeError):
+            call()
+    for call in values:
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ag.AgnesError):
+        ag.mx4_linear(x[:, :3], q)
+    with pytest.raises(ag.AgnesError):
+        ag.distill_loss(x, x, c, temperature=0.0)
