@@ -535,7 +535,8 @@ agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_mat
  *           + hard * (ln sum_j exp z_j - z_y)
  *     loss  = w L_i,   grad = w dL_i / dz
  * A row without valid entries has no first term, one whose label lies outside
- * [0, C) no second term.  A class listed twice has the sum of its p.  Terms with
+ * [0, C) no second term; teacher logits of -inf have p = 0 (and a row with no
+ * other has no first term).  A class listed twice has the sum of its p.  Terms with
  * p_e = 0 count as 0.  A row of weight 0 is skipped: loss 0, gradient 0,
  * whatever its logits hold.  Logits may be -inf (masked classes: q = 0,
  * gradient 0; a loss that asks for one is +inf); a row whose logits are all
@@ -549,9 +550,11 @@ agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_mat
  *   weight: float32 [rows], or NULL (1).  The gradient of a loss that is
  *     not a weighted sum: pass its row factors here to agnes_distill_grad.
  *   temperature > 0, soft >= 0, hard >= 0, all finite.
- * agnes_distill_loss: loss [rows] and, unless NULL, stats [rows][3] (the row's
- *   largest logit m, sum exp((z - m) / T), sum exp(z - m)).
- * agnes_distill_grad: the gradient from those statistics.
+ * agnes_distill_loss: loss [rows] and, unless NULL, stats [rows][3]: the row's
+ *   largest logit m, sum exp((z - m) / T) and, where there is a second term,
+ *   sum exp(z - m); zeros for a row of weight 0.
+ * agnes_distill_grad: the gradient from those statistics, for the same
+ *   descriptor (weights may differ in rows whose weight was not 0).
  * agnes_distill_loss_grad: both in one pass over the logits.
  * grad: the logits' shape, any type; it may be the logits' own memory (same
  *   data, stride and type).  Errors: INVALID. */

@@ -5,6 +5,16 @@
 //   loss   = w [ a T^2 sum_e p_e (ln p_e - ln q_{c_e}) + b (ln S_1 - (z_y - m)) ]
 //   grad_j = w [ a T (P q_j - sum_{c_e = j} p_e) + b (exp(z_j - m) / S_1 - [j = y]) ]
 // p is the softmax of the row's valid teacher logits, P = 1 if there are any.
+//
+// A row of logits is read once, stays in registers between its sums and its
+// gradient, and its gradient is written once; the classes that the teacher or
+// the label names get their values in a second store behind the row's.
+// Variants, by the number of 16-byte pieces of a row:
+//   up to 256      some lanes of a wave per row (a whole wave from 33 pieces on)
+//   up to 16384    a workgroup of 256 to 1024 threads per row
+//   above, or above 1024 with too few rows to fill the chip: the row is split
+//     over workgroups; a first launch leaves each part's maximum and sums, a
+//     second one joins them and writes the gradient (a second read of the row).
 #include <algorithm>
 #include <cmath>
 
@@ -12,155 +22,652 @@
 
 namespace agnes {
 
+constexpr float kLog2e = 1.44269504088896340736f;
+
 // The descriptor as the kernels take it.
 struct DistillArgs {
+    const void* z;
+    const void* t;
     const void* classes;
     const void* labels;
     const float* weight;
-    int64_t zstride, tstride, cstride;
+    const float* stats_in;         // the rows' statistics, or NULL: from the logits
+    float* loss;
+    float* stats;
+    void* grad;
+    int64_t zstride, tstride, cstride, gstride;
     int64_t rows;
     int32_t C, k;
-    float inv_t, soft, hard;       // 1 / T, a, b
-    float temp;
+    agnes_dtype ttype, gtype;
+    bool wide;                     // 64-bit classes and labels
+    bool nt;                       // gradient past the caches
+    float temp, inv_t, soft, hard; // T, 1 / T, a, b
+    float ct;                      // log2(e) / T: exp(x / T) = 2^(x ct)
 };
 
-__device__ __forceinline__ float block_max(float x, float* lds) {
-    for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, kWave));
-    __syncthreads();
-    if (lane_id() == 0) lds[wave_id()] = x;
-    __syncthreads();
-    float r = lds[0];
-    for (int w = 1; w < kWavesPerBlock; w++) r = fmaxf(r, lds[w]);
-    return r;
+__device__ __forceinline__ float load_any(const void* p, agnes_dtype t, int64_t i) {
+    if (t == AGNES_FLOAT32) return ((const float*)p)[i];
+    if (t == AGNES_FLOAT16) return (float)((const _Float16*)p)[i];
+    return (float)((const __bf16*)p)[i];
+}
+__device__ __forceinline__ void store_any(void* p, agnes_dtype t, int64_t i, float x) {
+    if (t == AGNES_FLOAT32) ((float*)p)[i] = x;
+    else if (t == AGNES_FLOAT16) ((_Float16*)p)[i] = (_Float16)x;
+    else ((__bf16*)p)[i] = (__bf16)x;
+}
+__device__ __forceinline__ int64_t load_index(const void* p, bool wide, int64_t i) {
+    return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i];
 }
 
-__device__ __forceinline__ float block_sum(float x, float* lds) {
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, kWave);
-    __syncthreads();
-    if (lane_id() == 0) lds[wave_id()] = x;
-    __syncthreads();
-    float r = lds[0];
-    for (int w = 1; w < kWavesPerBlock; w++) r += lds[w];
-    return r;
+// E elements at column c of the row whose first element is p[at].
+template <int E, typename T>
+__device__ __forceinline__ void store_typed(T* p, int64_t c, int64_t C, const float (&x)[E], bool nt) {
+    if (c + E <= C) {
+        Vec<T, E>::store(p + c, x, nt);
+    } else {
+#pragma unroll
+        for (int q = 0; q < E; q++)
+            if (c + q < C) p[c + q] = (T)x[q];
+    }
+}
+template <int E>
+__device__ __forceinline__ void store_grad(const DistillArgs& a, int64_t at, int64_t c, const float (&x)[E]) {
+    if (a.gtype == AGNES_FLOAT32) store_typed<E>((float*)a.grad + at, c, a.C, x, a.nt);
+    else if (a.gtype == AGNES_FLOAT16) store_typed<E>((_Float16*)a.grad + at, c, a.C, x, a.nt);
+    else store_typed<E>((__bf16*)a.grad + at, c, a.C, x, a.nt);
 }
 
-// One workgroup per row, three passes over it: maximum, sums, gradient.
-// stats_in: take the row's statistics from there.
-template <typename T, typename TT, typename TG, typename IdT>
-__global__ __launch_bounds__(kBlock) void k_distill(const T* z, const TT* __restrict__ t, DistillArgs a,
-                                                    const float* __restrict__ stats_in, float* __restrict__ loss,
-                                                    float* __restrict__ stats, TG* grad, int64_t gstride) {
-    __shared__ float lds[kWavesPerBlock];
-    __shared__ int32_t cls[AGNES_DISTILL_MAX_K];
-    __shared__ float prob[AGNES_DISTILL_MAX_K];
-    const int64_t r = blockIdx.x;
-    const T* zr = z + r * a.zstride;
-    TG* gr = grad + r * gstride;
-    const int C = a.C, tid = threadIdx.x;
+// Lanes [g L, (g + 1) L) of a wave reduce among themselves.
+__device__ __forceinline__ float lanes_max(float x, int L) {
+    for (int d = 1; d < L; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, kWave));
+    return x;
+}
+__device__ __forceinline__ float lanes_sum(float x, int L) {
+    for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d, kWave);
+    return x;
+}
+
+// 2^x with results below 2^-126 as 0.
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// How exp(d) follows from exp(d / T): kOne: not needed, or the same (T = 1);
+// kTwo: an exponential of its own; kSquare: its square (T = 2), a quarter of
+// the time of the exponential.
+enum { kOne = 0, kTwo = 1, kSquare = 2 };
+
+template <int MODE> __device__ __forceinline__ float plain_exp(float d, float et) {
+    if (MODE == kTwo) return pow2(d * kLog2e);
+    if (MODE == kSquare) return et * et;
+    return et;
+}
+
+// Maximum and sums of part of a row, relative to that maximum.
+struct Sums {
+    float m, st, s1;
+};
+
+// Adds E logits (-inf where there are none), none above s.m.  A NaN or +inf
+// logit makes the sums NaN, and with them everything that follows; where all
+// logits so far are -inf (or NaN, which a maximum passes over) the base is 0.
+template <int MODE, int E, typename Raw> __device__ __forceinline__ void add_piece(Sums& s, const Raw& v, float ct) {
+    const float base = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll
+    for (int q = 0; q < E; q++) {
+        const float d = (float)v[q] - base;
+        const float e = pow2(d * ct);
+        s.st += e;
+        if (MODE != kOne) s.s1 += plain_exp<MODE>(d, e);
+    }
+}
+
+// Brings sums to the maximum m of a larger part.
+template <int MODE> __device__ __forceinline__ void rebase(Sums& s, float m, float ct) {
+    if (m == -INFINITY) return;                  // the sums are 0 (or NaN)
+    const float d = s.m - m;
+    s.st *= pow2(d * ct);
+    if (MODE != kOne) s.s1 *= pow2(d * kLog2e);
+    s.m = m;
+}
+
+template <int MODE> __device__ __forceinline__ Sums lanes_join(Sums s, int L, float ct) {
+    rebase<MODE>(s, lanes_max(s.m, L), ct);
+    s.st = lanes_sum(s.st, L);
+    s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, L);
+    return s;
+}
+
+// Every logit is -inf.
+__device__ __forceinline__ bool no_logits(const Sums& s) { return s.m == -INFINITY && s.st == 0.f; }
+
+// A row's piece, -inf behind the last logit.
+template <typename T, int E>
+__device__ __forceinline__ typename Vec<T, E>::type logits_piece(const T* row, int64_t c, int64_t C) {
+    if (c + E <= C) return Vec<T, E>::raw(row + c);
+    typename Vec<T, E>::type v;
+#pragma unroll
+    for (int q = 0; q < E; q++) v[q] = c + q < C ? row[c + q] : (T)-INFINITY;
+    return v;
+}
+
+// Makes the compiler take the piece from its packed registers again: it would
+// otherwise keep the logits' float32 values from the maximum to the gradient,
+// twice the registers, and spill.
+template <typename Raw> __device__ __forceinline__ void keep_packed(Raw& v) {
+    uint4 w;
+    static_assert(sizeof(Raw) == sizeof(w), "a 16-byte piece");
+    __builtin_memcpy(&w, &v, 16);
+    asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w));
+    __builtin_memcpy(&v, &w, 16);
+}
+
+// What the teacher and the label ask of a row: the factors of q_j and of
+// exp(z_j - m) / S_1 in the gradient before the division by the sums.
+struct Terms {
+    bool some, named;
+    int64_t y;
+    float w, ca, cb;
+};
+
+// The teacher's distribution over lanes gl = 0 .. L - 1, entries e = gl, gl + L, ...:
+// classes (-1: padding) to cls, probabilities to prob.  Every lane gets the terms.
+__device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float w, int gl, int L, int32_t* cls,
+                                         float* prob) {
+    float tm = -INFINITY;
+    for (int e = gl; e < a.k; e += L) {
+        const int64_t c = load_index(a.classes, a.wide, r * a.cstride + e);
+        const bool ok = c >= 0 && c < a.C;
+        const float x = ok ? load_any(a.t, a.ttype, r * a.tstride + e) * a.inv_t : -INFINITY;
+        cls[e] = ok ? (int32_t)c : -1;
+        prob[e] = x;
+        tm = x != x ? INFINITY : fmaxf(tm, x);   // NaN: as +inf, which makes the sum NaN
+    }
+    tm = lanes_max(tm, L);
+    Terms q;
+    q.w = w;
+    q.some = a.soft > 0.f && tm != -INFINITY;
+    float ts = 0.f;
+    for (int e = gl; e < a.k; e += L) {
+        const float p = q.some ? pow2((prob[e] - tm) * kLog2e) : 0.f;
+        prob[e] = p;
+        ts += p;
+    }
+    ts = lanes_sum(ts, L);
+    if (q.some) {
+        const float inv = 1.f / ts;
+        for (int e = gl; e < a.k; e += L) prob[e] *= inv;
+    }
+    q.y = a.labels ? load_index(a.labels, a.wide, r) : -1;
+    q.named = a.hard > 0.f && q.y >= 0 && q.y < a.C;
+    q.ca = q.some ? w * a.soft * a.temp : 0.f;
+    q.cb = q.named ? w * a.hard : 0.f;
+    return q;
+}
+
+// sum_e p_e (ln p_e - ln q_{c_e}) over the lanes, from z_{c_e} in zc.
+__device__ __forceinline__ float divergence(const DistillArgs& a, const Sums& s, const float* prob, const float* zc,
+                                            int gl, int L) {
+    const float lt = logf(s.st);
+    float part = 0.f;
+    for (int e = gl; e < a.k; e += L) {
+        const float p = prob[e];
+        if (p != 0.f) part += p * (logf(p) - ((zc[e] - s.m) * a.inv_t - lt));
+    }
+    return lanes_sum(part, L);
+}
+
+// dy = z_y - m.
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Terms& q, const Sums& s, float div, float dy) {
+    if (no_logits(s)) return q.some || q.named ? q.w * INFINITY : 0.f;
+    float L = q.some ? a.soft * a.temp * a.temp * div : 0.f;
+    if (q.named) L += a.hard * (logf(s.s1) - dy);
+    return q.w * L;
+}
+
+// The gradient of logits [c, c + E), without the teacher's and the label's part.
+template <int MODE, int E, typename Raw>
+__device__ __forceinline__ void grad_piece(const DistillArgs& a, const Raw& v, const Sums& s, float ka, float kb,
+                                           float (&x)[E]) {
+#pragma unroll
+    for (int q = 0; q < E; q++) {
+        const float d = (float)v[q] - s.m;
+        const float e = pow2(d * a.ct);
+        x[q] = ka * e;
+        if (MODE != kOne) x[q] += kb * plain_exp<MODE>(d, e);
+    }
+}
+
+// The factors of exp((z - m) / T) and exp(z - m) in the gradient; with one
+// exponential, of T = 1 or of a single term, their sum in ka.  A term that is
+// not asked for has the factor 0, whatever its sum holds.
+template <int MODE> __device__ __forceinline__ void factors(const Terms& q, const Sums& s, float& ka, float& kb) {
+    ka = q.some ? q.ca / s.st : 0.f;
+    kb = q.named ? q.cb / s.s1 : 0.f;
+    if (MODE == kOne) {
+        ka += kb;
+        kb = 0.f;
+    }
+}
+
+// The gradient of class c, named by the teacher with the total probability p.
+template <int MODE>
+__device__ __forceinline__ float grad_named(const DistillArgs& a, const Terms& q, const Sums& s, float ka, float kb,
+                                            float z, int64_t c, float p) {
+    const float d = z - s.m;
+    const float e = pow2(d * a.ct);
+    float x = ka * e;
+    if (MODE != kOne) x += kb * plain_exp<MODE>(d, e);
+    if (q.some) x -= q.ca * p;
+    if (q.named && c == q.y) x -= q.cb;
+    return x;
+}
+
+// Orders the lanes' LDS accesses within their wave.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The total probability of class c: of all entries that list it, in their order.
+__device__ __forceinline__ float listed(const int32_t* cls, const float* prob, int k, int32_t c) {
+    float p = 0.f;
+    for (int e = 0; e < k; e++)
+        if (cls[e] == c) p += prob[e];
+    return p;
+}
+
+// Stores the gradient of the classes in [lo, hi) that the teacher lists or the
+// label names, by lanes gl = 0 .. L - 1 of one wave.  A class listed twice is stored
+// twice, with the same value.
+template <int MODE>
+__device__ __forceinline__ void store_named(const DistillArgs& a, const Terms& q, const Sums& s, float ka, float kb,
+                                            const int32_t* cls, const float* prob, const float* zc, float zy,
+                                            int64_t at, int gl, int L, int64_t lo, int64_t hi) {
+    wave_sync();                                 // cls and prob of the other lanes
+    if (q.some) {
+        for (int e0 = 0; e0 < a.k; e0 += L) {
+            const int e = e0 + gl;
+            const int32_t c = e < a.k ? cls[e] : -1;
+            bool again = true;
+            if (a.k <= kWave && L == kWave) {
+                // all entries are in this wave: is any class in two lanes?
+                uint64_t same = __ballot(c >= 0);
+                for (int b = 0; b < 31 && (a.C >> b); b++) {
+                    const uint64_t m = __ballot((c >> b) & 1);
+                    same &= ((c >> b) & 1) ? m : ~m;
+                }
+                again = __ballot(c >= 0 && (same & (same - 1))) != 0;
+            }
+            if (c < 0 || c < lo || c >= hi) continue;
+            const float p = again ? listed(cls, prob, a.k, c) : prob[e];
+            store_any(a.grad, a.gtype, at + c, grad_named<MODE>(a, q, s, ka, kb, zc[e], c, p));
+        }
+    }
+    if (q.named && gl == 0 && q.y >= lo && q.y < hi) {
+        const float p = q.some ? listed(cls, prob, a.k, (int32_t)q.y) : 0.f;
+        store_any(a.grad, a.gtype, at + q.y, grad_named<MODE>(a, q, s, ka, kb, zy, q.y, p));
+    }
+}
+
+// ----------------------------------------------------------------- lanes of a wave per row
+
+// L lanes per row, P pieces per lane (P > 1: L = 64).  Up to kLaneEntries
+// teacher entries.
+constexpr int kLaneEntries = 64;
+constexpr int kLanesMin = 8;
+
+template <typename T, int P, int MODE>
+__global__ __launch_bounds__(kBlock) void k_distill_lanes(DistillArgs a, int L) {
+    constexpr int E = 16 / (int)sizeof(T);
+    typedef typename Vec<T, E>::type Raw;
+    __shared__ int32_t cls_all[kBlock / kLanesMin * kLaneEntries];
+    __shared__ float prob_all[kBlock / kLanesMin * kLaneEntries];
+    __shared__ float zc_all[kBlock / kLanesMin * kLaneEntries];
+    const int g = threadIdx.x / L, gl = threadIdx.x % L;
+    const int64_t r = (int64_t)blockIdx.x * (kBlock / L) + g;
+    if (r >= a.rows) return;                     // whole groups; nothing below crosses a group
+    int32_t* cls = cls_all + g * kLaneEntries;
+    float* prob = prob_all + g * kLaneEntries;
+    float* zc = zc_all + g * kLaneEntries;
+    const T* zr = (const T*)a.z + r * a.zstride;
+    const int64_t at = r * a.gstride;
     const float w = a.weight ? a.weight[r] : 1.f;
     if (w == 0.f) {
-        if (tid == 0 && loss) loss[r] = 0.f;
-        if (tid == 0 && stats) stats[3 * r] = stats[3 * r + 1] = stats[3 * r + 2] = 0.f;
-        if (grad)
-            for (int64_t j = tid; j < C; j += kBlock) gr[j] = from_float<TG>(0.f);
+        if (gl == 0 && a.loss) a.loss[r] = 0.f;
+        if (gl == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
+        if (a.grad) {
+            const float zero[E] = {};
+            for (int i = 0; i < P; i++) {
+                const int64_t c = (int64_t)(gl + i * L) * E;
+                if (c < a.C) store_grad<E>(a, at, c, zero);
+            }
+        }
         return;
     }
-    // the teacher's distribution
-    float tm = -INFINITY;
-    for (int e = tid; e < a.k; e += kBlock) {
-        const int64_t c = (int64_t)((const IdT*)a.classes)[r * a.cstride + e];
-        const bool ok = c >= 0 && c < C;
-        const float x = ok ? to_float(t[r * a.tstride + e]) * a.inv_t : -INFINITY;
-        cls[e] = ok ? (int)c : -1;
-        prob[e] = x;
-        tm = x > tm || x != x ? x : tm;
-    }
-    const bool tnan = block_sum(tm != tm ? 1.f : 0.f, lds) > 0.f;
-    tm = tnan ? NAN : block_max(tm, lds);
-    const bool some = !(tm == -INFINITY) && a.soft > 0.f;
-    float ts = 0.f;
-    if (some)
-        for (int e = tid; e < a.k; e += kBlock) ts += expf(prob[e] - tm);
-    ts = block_sum(ts, lds);
-    const int64_t y = a.labels ? (int64_t)((const IdT*)a.labels)[r] : -1;
-    const bool named = y >= 0 && y < C && a.hard > 0.f;
-    // the student's statistics
-    float m, st, s1;
-    if (stats_in) {
-        m = stats_in[3 * r];
-        st = stats_in[3 * r + 1];
-        s1 = stats_in[3 * r + 2];
+    Raw v[P];
+#pragma unroll
+    for (int i = 0; i < P; i++) v[i] = logits_piece<T, E>(zr, (int64_t)(gl + i * L) * E, a.C);
+    const Terms q = teacher(a, r, w, gl, L, cls, prob);
+    for (int e = gl; e < a.k; e += L) zc[e] = cls[e] >= 0 ? (float)zr[cls[e]] : 0.f;
+    const float zy = q.named ? (float)zr[q.y] : 0.f;
+    Sums s{-INFINITY, 0.f, 0.f};
+    if (a.stats_in) {
+        s = Sums{a.stats_in[3 * r], a.stats_in[3 * r + 1], a.stats_in[3 * r + 2]};
     } else {
-        float x = -INFINITY, bad = 0.f;
-        for (int64_t j = tid; j < C; j += kBlock) {
-            const float v = to_float(zr[j]);
-            if (v != v) bad = 1.f;
-            x = fmaxf(x, v);
+#pragma unroll
+        for (int i = 0; i < P; i++)
+#pragma unroll
+            for (int x = 0; x < E; x++) s.m = fmaxf(s.m, (float)v[i][x]);
+        s.m = lanes_max(s.m, L);
+#pragma unroll
+        for (int i = 0; i < P; i++) add_piece<MODE, E>(s, v[i], a.ct);
+        s.st = lanes_sum(s.st, L);
+        s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, L);
+    }
+    if (a.loss) {
+        const float div = q.some ? divergence(a, s, prob, zc, gl, L) : 0.f;
+        if (gl == 0) a.loss[r] = row_loss(a, q, s, div, zy - s.m);
+    }
+    if (gl == 0 && a.stats) {
+        a.stats[3 * r] = s.m;
+        a.stats[3 * r + 1] = s.st;
+        a.stats[3 * r + 2] = s.s1;
+    }
+    if (!a.grad) return;
+    const bool empty = no_logits(s);
+    float ka, kb;
+    factors<MODE>(q, s, ka, kb);
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        const int64_t c = (int64_t)(gl + i * L) * E;
+        float x[E] = {};
+        if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
+        if (c < a.C) store_grad<E>(a, at, c, x);
+    }
+    if (!empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, gl, L, 0, a.C);
+}
+
+// ----------------------------------------------------------------- a workgroup per row
+
+template <typename T, int THREADS, int P, int MODE>
+__global__ __launch_bounds__(THREADS) void k_distill_block(DistillArgs a) {
+    constexpr int E = 16 / (int)sizeof(T), WAVES = THREADS / kWave;
+    typedef typename Vec<T, E>::type Raw;
+    __shared__ int32_t cls[AGNES_DISTILL_MAX_K];
+    __shared__ float prob[AGNES_DISTILL_MAX_K];
+    __shared__ float zc[AGNES_DISTILL_MAX_K];
+    __shared__ Sums red[WAVES];
+    __shared__ Terms terms;
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
+    const int64_t r = blockIdx.x;
+    const T* zr = (const T*)a.z + r * a.zstride;
+    const int64_t at = r * a.gstride;
+    const float w = a.weight ? a.weight[r] : 1.f;
+    if (w == 0.f) {
+        if (tid == 0 && a.loss) a.loss[r] = 0.f;
+        if (tid == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
+        if (a.grad) {
+            const float zero[E] = {};
+            for (int64_t c = (int64_t)tid * E; c < a.C; c += THREADS * E) store_grad<E>(a, at, c, zero);
         }
-        m = block_sum(bad, lds) > 0.f ? NAN : block_max(x, lds);
-        float u = 0.f, v = 0.f;
-        if (m != -INFINITY)
-            for (int64_t j = tid; j < C; j += kBlock) {
-                const float d = to_float(zr[j]) - m;
-                u += expf(d * a.inv_t);
-                v += expf(d);
+        return;
+    }
+    Raw v[P];
+#pragma unroll
+    for (int i = 0; i < P; i++) v[i] = logits_piece<T, E>(zr, (int64_t)(tid + i * THREADS) * E, a.C);
+    Terms q{};
+    float zy = 0.f;
+    if (wave == 0) {
+        q = teacher(a, r, w, lane, kWave, cls, prob);
+        for (int e = lane; e < a.k; e += kWave) zc[e] = cls[e] >= 0 ? (float)zr[cls[e]] : 0.f;
+        zy = q.named ? (float)zr[q.y] : 0.f;
+        if (lane == 0) terms = q;
+    }
+    Sums s{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < P; i++)
+#pragma unroll
+        for (int x = 0; x < E; x++) s.m = fmaxf(s.m, (float)v[i][x]);
+    s.m = lanes_max(s.m, kWave);
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        keep_packed(v[i]);
+        add_piece<MODE, E>(s, v[i], a.ct);
+    }
+    s.st = lanes_sum(s.st, kWave);
+    s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, kWave);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();                             // also: the named logits have been read
+    s = lane < WAVES ? red[lane] : Sums{-INFINITY, 0.f, 0.f};
+    s = lanes_join<MODE>(s, kWave, a.ct);
+    q = terms;
+    if (wave == 0) {
+        if (a.loss) {
+            const float div = q.some ? divergence(a, s, prob, zc, lane, kWave) : 0.f;
+            if (lane == 0) a.loss[r] = row_loss(a, q, s, div, zy - s.m);
+        }
+        if (lane == 0 && a.stats) {
+            a.stats[3 * r] = s.m;
+            a.stats[3 * r + 1] = s.st;
+            a.stats[3 * r + 2] = s.s1;
+        }
+    }
+    if (!a.grad) return;
+    const bool empty = no_logits(s);
+    float ka, kb;
+    factors<MODE>(q, s, ka, kb);
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        const int64_t c = (int64_t)(tid + i * THREADS) * E;
+        float x[E] = {};
+        keep_packed(v[i]);
+        if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
+        if (c < a.C) store_grad<E>(a, at, c, x);
+    }
+    __syncthreads();                             // the row's values are stored before the named classes'
+    if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, kWave, 0, a.C);
+}
+
+// ----------------------------------------------------------------- a row over several workgroups
+
+// Part of a row: its maximum and sums, and of the classes that lie in it the
+// teacher's probability and sum_e p_e (z_{c_e} - m), and z_y - m.
+struct Part {
+    Sums s;
+    float mass, cross, label;
+    float pad[2];
+};
+
+constexpr int kPartThreads = 256;
+
+// blockIdx: (part, row).  A part is `span` logits, a multiple of a piece.
+template <typename T, int MODE>
+__global__ __launch_bounds__(kPartThreads) void k_distill_part(DistillArgs a, int64_t span, Part* __restrict__ parts) {
+    constexpr int E = 16 / (int)sizeof(T), U = 4;
+    typedef typename Vec<T, E>::type Raw;
+    __shared__ int32_t cls[AGNES_DISTILL_MAX_K];
+    __shared__ float prob[AGNES_DISTILL_MAX_K];
+    __shared__ Sums red[kPartThreads / kWave];
+    const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
+    const int64_t r = blockIdx.y;
+    const T* zr = (const T*)a.z + r * a.zstride;
+    const float w = a.weight ? a.weight[r] : 1.f;
+    if (w == 0.f) return;                        // the second launch skips the row too
+    const int64_t lo = (int64_t)blockIdx.x * span, hi = min((int64_t)a.C, lo + span);
+    Sums s{-INFINITY, 0.f, 0.f};
+    for (int64_t c0 = lo; c0 < hi; c0 += (int64_t)kPartThreads * E * U) {
+        Raw v[U];
+#pragma unroll
+        for (int i = 0; i < U; i++)
+            v[i] = logits_piece<T, E>(zr, c0 + (int64_t)(tid + i * kPartThreads) * E, hi);
+        float m = s.m;
+#pragma unroll
+        for (int i = 0; i < U; i++)
+#pragma unroll
+            for (int x = 0; x < E; x++) m = fmaxf(m, (float)v[i][x]);
+        rebase<MODE>(s, m, a.ct);
+#pragma unroll
+        for (int i = 0; i < U; i++) add_piece<MODE, E>(s, v[i], a.ct);
+    }
+    s = lanes_join<MODE>(s, kWave, a.ct);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    if (wave != 0) return;
+    s = lane < kPartThreads / kWave ? red[lane] : Sums{-INFINITY, 0.f, 0.f};
+    s = lanes_join<MODE>(s, kWave, a.ct);
+    const Terms q = teacher(a, r, w, lane, kWave, cls, prob);
+    const float m = s.m == -INFINITY ? 0.f : s.m;
+    float mass = 0.f, cross = 0.f;
+    for (int e = lane; e < a.k; e += kWave)
+        if (prob[e] != 0.f && cls[e] >= lo && cls[e] < hi) {
+            mass += prob[e];
+            cross += prob[e] * ((float)zr[cls[e]] - m);
+        }
+    mass = lanes_sum(mass, kWave);
+    cross = lanes_sum(cross, kWave);
+    if (lane == 0) {
+        Part p{};
+        p.s = s;
+        p.mass = mass;
+        p.cross = cross;
+        p.label = q.named && q.y >= lo && q.y < hi ? (float)zr[q.y] - m : 0.f;
+        parts[r * gridDim.x + blockIdx.x] = p;
+    }
+}
+
+// The row's sums from its parts (or from stats_in), then the loss, by the first
+// workgroup, and the gradient of [lo, hi).
+template <typename T, int MODE>
+__global__ __launch_bounds__(kPartThreads) void k_distill_apply(DistillArgs a, int64_t span, int nparts,
+                                                                const Part* __restrict__ parts) {
+    constexpr int E = 16 / (int)sizeof(T), U = 4;
+    typedef typename Vec<T, E>::type Raw;
+    __shared__ int32_t cls[AGNES_DISTILL_MAX_K];
+    __shared__ float prob[AGNES_DISTILL_MAX_K];
+    __shared__ float zc[AGNES_DISTILL_MAX_K];
+    __shared__ Terms terms;
+    const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
+    const int64_t r = blockIdx.y;
+    const T* zr = (const T*)a.z + r * a.zstride;
+    const int64_t at = r * a.gstride;
+    const float w = a.weight ? a.weight[r] : 1.f;
+    const int64_t lo = (int64_t)blockIdx.x * span, hi = min((int64_t)a.C, lo + span);
+    const bool first = blockIdx.x == 0;
+    if (w == 0.f) {
+        if (first && tid == 0 && a.loss) a.loss[r] = 0.f;
+        if (first && tid == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
+        if (a.grad) {
+            const float zero[E] = {};
+            for (int64_t c = lo + (int64_t)tid * E; c < hi; c += kPartThreads * E) store_grad<E>(a, at, c, zero);
+        }
+        return;
+    }
+    Sums s{-INFINITY, 0.f, 0.f};
+    float mass = 0.f, cross = 0.f, label = 0.f;
+    if (a.stats_in) {
+        s = Sums{a.stats_in[3 * r], a.stats_in[3 * r + 1], a.stats_in[3 * r + 2]};
+    } else {
+        const Part* p = parts + r * nparts;
+        for (int i = lane; i < nparts; i += kWave) s.m = fmaxf(s.m, p[i].s.m);
+        s.m = lanes_max(s.m, kWave);
+        for (int i = lane; i < nparts; i += kWave) {
+            const Part x = p[i];
+            Sums y = x.s;
+            rebase<MODE>(y, s.m, a.ct);
+            s.st += y.st;
+            s.s1 += y.s1;
+            const float up = x.s.m == -INFINITY ? 0.f : x.s.m;      // what the part's values are relative to
+            mass += x.mass;
+            if (x.mass != 0.f) cross += x.cross + x.mass * (up - s.m);
+            // a label of another part leaves 0, of this part z_y - up
+            if (first) {
+                const int64_t y0 = (int64_t)i * span;
+                const int64_t lab = a.labels ? load_index(a.labels, a.wide, r) : -1;
+                if (lab >= y0 && lab < y0 + span && lab < a.C) label = x.label + (up - s.m);
             }
-        st = block_sum(u, lds);
-        s1 = block_sum(v, lds);
-    }
-    const bool empty = m == -INFINITY;             // every logit is -inf
-    const float lt = logf(st), l1 = logf(s1), ltt = logf(ts);
-    float part = 0.f;
-    for (int e = tid; e < a.k; e += kBlock) {
-        float p = 0.f;
-        if (some) {
-            const float x = prob[e] - tm;
-            p = expf(x) / ts;
-            if (p != 0.f) {
-                const float lnq = empty ? -INFINITY : (to_float(zr[cls[e]]) - m) * a.inv_t - lt;
-                part += p * ((x - ltt) - lnq);
-            }
         }
-        prob[e] = p;
+        s.st = lanes_sum(s.st, kWave);
+        s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, kWave);
+        mass = lanes_sum(mass, kWave);
+        cross = lanes_sum(cross, kWave);
+        label = lanes_sum(label, kWave);
     }
-    part = block_sum(part, lds);
-    if (tid == 0) {
-        if (loss) {
-            float L = some ? a.soft * a.temp * a.temp * part : 0.f;
-            if (named) L += a.hard * (empty ? INFINITY : l1 - (to_float(zr[y]) - m));
-            loss[r] = w * L;
+    if (wave == 0) {
+        const Terms q = teacher(a, r, w, lane, kWave, cls, prob);
+        if (lane == 0) terms = q;
+        if (a.grad)
+            for (int e = lane; e < a.k; e += kWave)
+                zc[e] = cls[e] >= lo && cls[e] < hi ? (float)zr[cls[e]] : 0.f;
+        if (first && a.loss) {
+            float part = 0.f;                    // sum_e p_e ln p_e
+            for (int e = lane; e < a.k; e += kWave)
+                if (prob[e] != 0.f) part += prob[e] * logf(prob[e]);
+            part = lanes_sum(part, kWave);
+            const float div = part - (cross * a.inv_t - mass * logf(s.st));
+            if (lane == 0) a.loss[r] = row_loss(a, q, s, q.some ? div : 0.f, label);
         }
-        if (stats) {
-            stats[3 * r] = m;
-            stats[3 * r + 1] = st;
-            stats[3 * r + 2] = s1;
+        if (first && lane == 0 && a.stats) {
+            a.stats[3 * r] = s.m;
+            a.stats[3 * r + 1] = s.st;
+            a.stats[3 * r + 2] = s.s1;
         }
     }
-    if (!grad) return;
-    __syncthreads();                                // prob is complete
-    const float ca = some ? w * a.soft * a.temp : 0.f, cb = named ? w * a.hard : 0.f;
-    for (int64_t j = tid; j < C; j += kBlock) {
-        if (empty) {
-            gr[j] = from_float<TG>(0.f);
-            continue;
+    if (!a.grad) return;
+    __syncthreads();
+    const Terms q = terms;
+    const bool empty = no_logits(s);
+    const float zy = q.named && q.y >= lo && q.y < hi ? (float)zr[q.y] : 0.f;
+    float ka, kb;
+    factors<MODE>(q, s, ka, kb);
+    __syncthreads();                             // the named logits are read before anything is stored
+    for (int64_t c0 = lo; c0 < hi; c0 += (int64_t)kPartThreads * E * U) {
+        Raw v[U];
+#pragma unroll
+        for (int i = 0; i < U; i++)
+            v[i] = logits_piece<T, E>(zr, c0 + (int64_t)(tid + i * kPartThreads) * E, hi);
+#pragma unroll
+        for (int i = 0; i < U; i++) {
+            const int64_t c = c0 + (int64_t)(tid + i * kPartThreads) * E;
+            float x[E] = {};
+            if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
+            if (c < hi) store_grad<E>(a, at, c, x);
         }
-        const float d = to_float(zr[j]) - m;
-        float x = 0.f;
-        if (some) {
-            float p = 0.f;
-            for (int e = 0; e < a.k; e++)
-                if (cls[e] == j) p += prob[e];
-            x += ca * (expf(d * a.inv_t) / st - p);
-        }
-        if (named) x += cb * (expf(d) / s1 - (j == y ? 1.f : 0.f));
-        gr[j] = from_float<TG>(x);
     }
+    __syncthreads();
+    if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, kWave, lo, hi);
+}
+
+// ----------------------------------------------------------------- host
+
+constexpr int64_t kLanePieces = 4 * kWave;       // a wave's rows
+constexpr int64_t kSplitPieces = 1024;           // rows that may be split
+constexpr int64_t kBlockPieces = 16 * 1024;      // a workgroup's rows
+constexpr int64_t kSplitRows = 512;              // fewer rows leave too many compute units idle
+constexpr int64_t kSplitGroups = 1024;           // workgroups that a split aims at
+
+// Parts of a row of C logits of `size` bytes, or 1: not split.  A part has at
+// least one round of its workgroup.
+static int parts_of(int64_t rows, int64_t C, int64_t size, int64_t& span) {
+    const int64_t E = 16 / size, pieces = (C + E - 1) / E, round = (int64_t)kPartThreads * E;
+    const bool many = pieces > kBlockPieces;
+    if (!many && (pieces <= kSplitPieces || rows >= kSplitRows)) return 1;
+    const int64_t want = std::max<int64_t>((kSplitGroups + rows - 1) / rows, many ? 2 : 1);
+    const int64_t rounds = std::max<int64_t>(1, (C + round * want - 1) / (round * want));
+    span = rounds * round;
+    return (int)((C + span - 1) / span);
 }
 
 uint64_t distill_bytes(int64_t rows, int64_t classes) {
     AGNES_REQUIRE(rows >= 0 && classes >= 0 && rows < ((int64_t)1 << 31) && classes < ((int64_t)1 << 31),
                   AGNES_ERR_INVALID, "rows and classes must be in [0, 2^31)");
-    return 0;
+    if (rows == 0 || classes == 0) return 0;
+    int64_t span = 0, most = 0;
+    for (int64_t size : {2, 4}) {                // either size of logits
+        span = 0;
+        const int n = parts_of(rows, classes, size, span);
+        if (span) most = std::max<int64_t>(most, rows * n * (int64_t)sizeof(Part));
+    }
+    return (uint64_t)most;
 }
 
 static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* grad) {
@@ -178,17 +685,25 @@ static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* gra
                   AGNES_ERR_INVALID, "the temperature must be positive and finite");
     AGNES_REQUIRE(std::isfinite(d->soft) && d->soft >= 0.f && std::isfinite(d->hard) && d->hard >= 0.f,
                   AGNES_ERR_INVALID, "soft and hard must be finite and not negative");
+    DistillArgs a{};
     if (grad) {
         check_matrix(grad, true, "grad");
         AGNES_REQUIRE(grad->rows == rows && grad->cols == C, AGNES_ERR_INVALID, "grad must have the logits' shape");
         AGNES_REQUIRE(grad->data != d->logits.data || rows == 0 ||
                           (grad->dtype == d->logits.dtype && (rows == 1 || grad->stride == d->logits.stride)),
                       AGNES_ERR_INVALID, "grad may share the logits' memory only with their type and stride");
+        a.grad = grad->data;
+        a.gstride = grad->stride;
+        a.gtype = grad->dtype;
+        a.nt = rows * C * (int64_t)elem_size(grad->dtype) > kStreamBytes;
     }
-    DistillArgs a{};
+    a.z = d->logits.data;
+    a.t = d->teacher.data;
+    a.ttype = d->teacher.dtype;
     a.classes = d->classes;
     a.labels = d->labels;
     a.weight = d->weight;
+    a.wide = d->index_dtype == AGNES_INT64;
     a.zstride = d->logits.stride;
     a.tstride = d->teacher.stride;
     a.cstride = d->classes_stride;
@@ -197,44 +712,90 @@ static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* gra
     a.k = (int32_t)k;
     a.temp = d->temperature;
     a.inv_t = 1.f / d->temperature;
+    a.ct = kLog2e / d->temperature;
     a.soft = d->soft;
-    a.hard = d->hard;
+    a.hard = d->labels ? d->hard : 0.f;
     return a;
 }
 
-static void launch(const agnes_distill* d, const DistillArgs& a, const float* stats_in, float* loss, float* stats,
-                   const agnes_matrix* grad, hipStream_t st) {
+template <typename T, int MODE> static void launch(const DistillArgs& a, void* ws, hipStream_t st) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const int64_t pieces = (a.C + E - 1) / E, rows = a.rows;
+    if (pieces <= kLanePieces && a.k <= kLaneEntries) {
+        int L = kLanesMin;
+        while (L < pieces && L < kWave) L *= 2;
+        const int per = kBlock / L;
+        const dim3 grid((unsigned)((rows + per - 1) / per));
+        if (pieces <= kWave) AGNES_LAUNCH((k_distill_lanes<T, 1, MODE>), grid, dim3(kBlock), 0, st, a, L);
+        else if (pieces <= 2 * kWave) AGNES_LAUNCH((k_distill_lanes<T, 2, MODE>), grid, dim3(kBlock), 0, st, a, L);
+        else AGNES_LAUNCH((k_distill_lanes<T, 4, MODE>), grid, dim3(kBlock), 0, st, a, L);
+        return;
+    }
+    int64_t span = 0;
+    int parts = parts_of(rows, a.C, sizeof(T), span);
+    if (a.stats_in && span == 0) {               // the gradient alone needs no sums: parts of any length do
+        span = 4 * kPartThreads * E;
+        parts = (int)((a.C + span - 1) / span);
+    }
+    if (span) {
+        // blockIdx.y holds at most 65535 rows
+        for (int64_t r = 0; r < rows; r += 65535) {
+            DistillArgs b = a;
+            const int64_t n = std::min<int64_t>(65535, rows - r);
+            b.z = (const T*)a.z + r * a.zstride;
+            b.t = (const char*)a.t + r * a.tstride * (int64_t)elem_size(a.ttype);
+            b.classes = (const char*)a.classes + r * a.cstride * (a.wide ? 8 : 4);
+            if (a.labels) b.labels = (const char*)a.labels + r * (a.wide ? 8 : 4);
+            if (a.weight) b.weight = a.weight + r;
+            if (a.loss) b.loss = a.loss + r;
+            if (a.stats) b.stats = a.stats + 3 * r;
+            if (a.stats_in) b.stats_in = a.stats_in + 3 * r;
+            if (a.grad) b.grad = (char*)a.grad + r * a.gstride * (int64_t)elem_size(a.gtype);
+            b.rows = n;
+            Part* p = (Part*)ws + r * parts;
+            const dim3 grid((unsigned)parts, (unsigned)n);
+            if (!a.stats_in) AGNES_LAUNCH((k_distill_part<T, MODE>), grid, dim3(kPartThreads), 0, st, b, span, p);
+            // without a gradient only a row's first part has anything to do
+            AGNES_LAUNCH((k_distill_apply<T, MODE>), dim3(a.grad ? (unsigned)parts : 1u, (unsigned)n),
+                         dim3(kPartThreads), 0, st, b, span, parts, (const Part*)p);
+        }
+        return;
+    }
+    const dim3 grid((unsigned)rows);
+    if (pieces <= 4 * 256) AGNES_LAUNCH((k_distill_block<T, 256, 4, MODE>), grid, dim3(256), 0, st, a);
+    else if (pieces <= 8 * 256) AGNES_LAUNCH((k_distill_block<T, 256, 8, MODE>), grid, dim3(256), 0, st, a);
+    else if (pieces <= 8 * 512) AGNES_LAUNCH((k_distill_block<T, 512, 8, MODE>), grid, dim3(512), 0, st, a);
+    else if (pieces <= 8 * 1024) AGNES_LAUNCH((k_distill_block<T, 1024, 8, MODE>), grid, dim3(1024), 0, st, a);
+    else AGNES_LAUNCH((k_distill_block<T, 1024, 16, MODE>), grid, dim3(1024), 0, st, a);
+}
+
+static void run(const agnes_distill* d, const DistillArgs& a, void* ws, hipStream_t st) {
     if (a.rows == 0) return;
-    with_float(d->logits.dtype, [&](auto tz) {
-        with_float(d->teacher.dtype, [&](auto tt) {
-            with_float(grad ? grad->dtype : d->logits.dtype, [&](auto tg) {
-                with_index(d->index_dtype, [&](auto id) {
-                    typedef decltype(tz) TZ;
-                    typedef decltype(tt) TT;
-                    typedef decltype(tg) TG;
-                    typedef decltype(id) IdT;
-                    AGNES_LAUNCH((k_distill<TZ, TT, TG, IdT>), dim3((unsigned)a.rows), dim3(kBlock), 0, st,
-                                 (const TZ*)d->logits.data, (const TT*)d->teacher.data, a, stats_in, loss, stats,
-                                 grad ? (TG*)grad->data : nullptr, grad ? grad->stride : 0);
-                });
-            });
-        });
+    with_float(d->logits.dtype, [&](auto t) {
+        typedef decltype(t) T;
+        // one exponential does for a single term, and for both at T = 1
+        if (a.hard == 0.f || a.temp == 1.f) launch<T, kOne>(a, ws, st);
+        else if (a.temp == 2.f) launch<T, kSquare>(a, ws, st);
+        else launch<T, kTwo>(a, ws, st);
     });
 }
 
 void distill_loss(const agnes_distill* d, float* loss, float* stats, const agnes_matrix* grad, void* ws,
                   uint64_t ws_bytes, hipStream_t st) {
-    const DistillArgs a = check_distill(d, grad);
+    DistillArgs a = check_distill(d, grad);
     AGNES_REQUIRE(loss || a.rows == 0, AGNES_ERR_INVALID, "loss must not be NULL");
     check_workspace(ws, ws_bytes, distill_bytes(a.rows, a.C));
-    launch(d, a, nullptr, loss, stats, grad, st);
+    a.loss = loss;
+    a.stats = stats;
+    run(d, a, ws, st);
 }
 
 void distill_grad(const agnes_distill* d, const float* stats, const agnes_matrix* grad, hipStream_t st) {
     AGNES_REQUIRE(grad, AGNES_ERR_INVALID, "grad must not be NULL");
-    const DistillArgs a = check_distill(d, grad);
+    DistillArgs a = check_distill(d, grad);
     AGNES_REQUIRE(stats || a.rows == 0, AGNES_ERR_INVALID, "stats must not be NULL");
-    launch(d, a, stats, nullptr, nullptr, grad, st);
+    a.stats_in = stats;
+    run(d, a, nullptr, st);
 }
 
 }  // namespace agnes

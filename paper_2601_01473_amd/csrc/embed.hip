@@ -33,10 +33,19 @@ __device__ __forceinline__ void load_piece(const T* row, int64_t c, int64_t D, f
         for (int q = 0; q < E; q++) x[q] = c + q < D ? to_float(row[c + q]) : 0.f;
     }
 }
+// The same without the conversion, for pieces that wait in registers.
 template <typename T, int E>
-__device__ __forceinline__ void store_piece(T* row, int64_t c, int64_t D, const float (&x)[E]) {
+__device__ __forceinline__ typename Vec<T, E>::type raw_piece(const T* row, int64_t c, int64_t D) {
+    if (c + E <= D) return Vec<T, E>::raw(row + c);
+    typename Vec<T, E>::type v;
+#pragma unroll
+    for (int q = 0; q < E; q++) v[q] = c + q < D ? row[c + q] : (T)0.f;
+    return v;
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_piece(T* row, int64_t c, int64_t D, const float (&x)[E], bool nt) {
     if (c + E <= D) {
-        Vec<T, E>::store(row + c, x);
+        Vec<T, E>::store(row + c, x, nt);
     } else {
 #pragma unroll
         for (int q = 0; q < E; q++)
@@ -54,7 +63,7 @@ template <typename TI, typename TO, typename IdT>
 __global__ __launch_bounds__(kBlock) void k_embed_lookup(const TI* __restrict__ table, int64_t tstride, int64_t V,
                                                          int64_t D, const IdT* __restrict__ ids, int64_t n,
                                                          float scale, TO* __restrict__ out, int64_t ostride,
-                                                         int lanes) {
+                                                         int lanes, bool nt) {
     constexpr int E = 16 / (int)(sizeof(TI) < sizeof(TO) ? sizeof(TI) : sizeof(TO)), U = kLookupRows;
     const int groups = kBlock / lanes, g = threadIdx.x / lanes, gl = threadIdx.x % lanes;
     for (int64_t i0 = (int64_t)blockIdx.x * groups * U + g; i0 < n; i0 += (int64_t)gridDim.x * groups * U) {
@@ -81,7 +90,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const TI* __restrict__ 
                 if (i >= n) continue;
 #pragma unroll
                 for (int q = 0; q < E; q++) x[u][q] *= scale;
-                store_piece<TO, E>(out + i * ostride, c, D, x[u]);
+                store_piece<TO, E>(out + i * ostride, c, D, x[u], nt);
             }
         }
     }
@@ -111,7 +120,7 @@ void embedding_lookup(const agnes_matrix* table, const void* ids, agnes_dtype id
                 const int64_t per = (int64_t)(kBlock / lanes) * kLookupRows;
                 AGNES_LAUNCH((k_embed_lookup<TI, TO, IdT>), dim3((unsigned)std::min<int64_t>((n + per - 1) / per, 1 << 22)),
                              dim3(kBlock), 0, st, (const TI*)table->data, table->stride, table->rows, D, (const IdT*)ids, n, scale,
-                             (TO*)out->data, out->stride, lanes);
+                             (TO*)out->data, out->stride, lanes, n * D * (int64_t)sizeof(TO) > kStreamBytes);
             });
         });
     });
@@ -122,9 +131,10 @@ void embedding_lookup(const agnes_matrix* table, const void* ids, agnes_dtype id
 // Up to kRankSort ids are sorted by counting, in one launch: an id's place is
 // the number of ids before it in (id, position) order.  Every workgroup holds
 // all keys in LDS; 16 lanes share one id's comparisons.  More ids take the
-// device-wide radix sort (three launches per digit).  Padding gets the key V
+// device-wide radix sort (three launches per digit).  Whole gradient of 8192
+// ids: 20 us less by counting; of 16384 ids: 45 us more.  Padding gets the key V
 // and so comes last.  Both kernels also clear the list of distinct ids.
-constexpr int kRankSort = 4096;
+constexpr int kRankSort = 8192;
 constexpr int kRankLanes = 16;
 
 template <typename IdT>
@@ -199,14 +209,15 @@ __global__ __launch_bounds__(kBlock) void k_embed_no_ids(int32_t* row_ids, int64
 // heads, and are summed the same way, level by level, until few are left; the
 // last level follows each run to its end.  So the work of a run is split
 // evenly however often an id occurs, and the order of every sum depends on the
-// list alone.  A level's entries are at most 1/16 of the rows of the one before.
-constexpr int kRows = 8;                    // rows in flight per group
-constexpr int kChunkSmall = 16;             // chunk length up to kRankSort ids: more groups
-constexpr int kChunk = 32;                  // and above
-constexpr int kJoinChunk = 32;              // entries per group of a later level
-constexpr int64_t kJoinLast = 256;          // entries that the last level may have
+// list alone.  A level has about 1/16 (first) or 1/32 (later) as many entries as the one before had rows.
+constexpr int kRows = 4;                    // rows per batch
+constexpr int kSmall = 4096;                // up to so many ids
+constexpr int kChunkSmall = 16;             // chunks are shorter, for more groups,
+constexpr int kChunk = 32;                  // than above
+constexpr int kJoinChunk = 64;              // entries per group of a later level
+constexpr int64_t kJoinLast = 512;          // entries that the last level may have
 
-static int chunk_of(int64_t n) { return n <= kRankSort ? kChunkSmall : kChunk; }
+static int chunk_of(int64_t n) { return n <= kSmall ? kChunkSmall : kChunk; }
 
 // Where a run's sum goes.
 template <typename TO> struct Sink {
@@ -218,6 +229,7 @@ template <typename TO> struct Sink {
     float* part;                            // [entries][dpad] partial sums
     int32_t* part_row;                      // [entries]
     int64_t dpad;
+    bool nt;                                // stores past the caches
 
     template <int E> __device__ __forceinline__ void finish(int64_t row, int64_t c, float (&acc)[E]) const {
         if (c >= D || row >= max_rows) return;
@@ -230,7 +242,7 @@ template <typename TO> struct Sink {
 #pragma unroll
             for (int q = 0; q < E; q++) acc[q] += old[q];
         }
-        store_piece<TO, E>(p, c, D, acc);
+        store_piece<TO, E>(p, c, D, acc, nt);
     }
     template <int E> __device__ __forceinline__ void leave(int64_t entry, int64_t c, const float (&acc)[E]) const {
         if (c < dpad) Vec<float, E>::store(part + entry * dpad + c, acc);   // dpad is a multiple of E
@@ -250,10 +262,19 @@ __device__ __forceinline__ int chunk_heads(const uint32_t* keys, int64_t n, uint
     return heads;
 }
 
+// The heads of every chunk of kChunk = 32: a wave reads 64 keys, two chunks, at once.
 __global__ __launch_bounds__(kBlock) void k_embed_heads(const uint32_t* __restrict__ keys, int64_t n, uint32_t V,
-                                                        int64_t chunks, int chunk, int32_t* __restrict__ heads) {
-    const int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (c < chunks) heads[c] = chunk_heads(keys, n, V, c, chunk);
+                                                        int64_t chunks, int32_t* __restrict__ heads) {
+    static_assert(kChunk == 32, "half a wave per chunk");
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    bool head = false;
+    if (i < n) {
+        const uint32_t k = keys[i];
+        head = k < V && (i == 0 || keys[i - 1] != k);
+    }
+    const uint64_t m = __ballot(head);
+    const int64_t c = i / kChunk;
+    if (i % kChunk == 0 && c < chunks) heads[c] = __popc((uint32_t)(lane_id() ? m >> 32 : m));
 }
 
 // What the first level reads.
@@ -274,11 +295,13 @@ template <typename TI> struct Sorted {
 // Zeroes the rows of [v0, v0 + R) that no key names; R <= kBlock.
 template <typename TO>
 __device__ __forceinline__ void clear_unnamed(const uint32_t* keys, int64_t n, int64_t v0, int R, int64_t V, TO* out,
-                                              int64_t ostride, int64_t D, int lanes) {
+                                              int64_t ostride, int64_t D, int lanes, bool nt) {
     constexpr int E = 16 / (int)sizeof(TO);
     __shared__ bool named[kBlock];
-    const int64_t lo = wave_partition_point(0, n, [&](int64_t i) { return keys[i] < (uint32_t)v0; });
-    const int64_t hi = wave_partition_point(lo, n, [&](int64_t i) { return keys[i] < (uint32_t)min(V, v0 + R); });
+    // the keys of these rows: one half of the wave finds where they begin, the other where they end
+    const uint32_t bound = (uint32_t)(lane_id() < 32 ? v0 : min(V, v0 + R));
+    const int64_t at = group_partition_point<32>(0, n, [&](int64_t i) { return keys[i] < bound; });
+    const int64_t lo = (int64_t)shfl64((uint64_t)at, 0), hi = (int64_t)shfl64((uint64_t)at, 32);
     const int t = threadIdx.x;
     if (t < R) {
         int64_t a = lo, b = hi;
@@ -297,7 +320,7 @@ __device__ __forceinline__ void clear_unnamed(const uint32_t* keys, int64_t n, i
     for (int r = g; r < R; r += groups) {
         if (named[r] || v0 + r >= V) continue;
         for (int64_t c = (int64_t)gl * E; c < D; c += (int64_t)lanes * E)
-            store_piece<TO, E>(out + (v0 + r) * ostride, c, D, zero);
+            store_piece<TO, E>(out + (v0 + r) * ostride, c, D, zero, nt);
     }
 }
 
@@ -309,7 +332,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Sorted<TI> s, Sink<TO> o, 
     constexpr int E = 16 / (int)sizeof(TI);
     if ((int64_t)blockIdx.x >= sum_blocks) {
         clear_unnamed<TO>(s.keys, s.n, ((int64_t)blockIdx.x - sum_blocks) * fill_rows, fill_rows, s.V, o.out,
-                          o.ostride, o.D, fill_lanes);
+                          o.ostride, o.D, fill_lanes, o.nt);
         return;
     }
     const int groups = kBlock / lanes, g = threadIdx.x / lanes, gl = threadIdx.x % lanes;
@@ -334,10 +357,23 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Sorted<TI> s, Sink<TO> o, 
     } else if (s.compact && c < s.chunks) {
         rank = s.rank[c];
     }
+    // The keys and places of all the workgroup's chunks, so that only the rows
+    // themselves are waited for: two batches of kRows are in flight.
+    extern __shared__ uint32_t staged[];
+    const int pitch = s.chunk + 1;                                  // odd: the groups' reads fall into different banks
+    uint32_t* const skey = staged + g * pitch;
+    const uint32_t* const sperm = skey + groups * pitch;
+    for (int i = threadIdx.x; i < groups * s.chunk; i += kBlock) {
+        const int64_t q = c0 * s.chunk + i;
+        const int at = i / s.chunk * pitch + i % s.chunk;
+        staged[at] = q < s.n ? s.keys[q] : s.V;
+        staged[groups * pitch + at] = q < s.n ? s.perm[q] : 0u;
+    }
+    __syncthreads();
     if (c >= s.chunks) return;
     const int64_t col = ((int64_t)tile * lanes + gl) * E;
     const int64_t q0 = c * s.chunk, q1 = min(s.n, q0 + s.chunk);
-    const bool lead = tile == 0 && gl == 0;
+    const bool lead = tile == 0 && gl == 0, live = col < o.D;
     uint32_t cur = q0 > 0 ? s.keys[q0 - 1] : s.V;                   // the open run's id
     bool continued = true;                                          // it began in an earlier chunk
     bool any = false;                                               // it has rows here
@@ -346,20 +382,18 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Sorted<TI> s, Sink<TO> o, 
     float acc[E];
 #pragma unroll
     for (int q = 0; q < E; q++) acc[q] = 0.f;
-    for (int64_t q = q0; q < q1; q += kRows) {
-        uint32_t key[kRows];
-        float x[kRows][E];
+    typedef typename Vec<TI, E>::type Raw;
+    auto fetch = [&](int q, Raw (&x)[kRows]) {
 #pragma unroll
-        for (int j = 0; j < kRows; j++) key[j] = q + j < q1 ? s.keys[q + j] : s.V;
-#pragma unroll
-        for (int j = 0; j < kRows; j++) {
-            if (key[j] < s.V && col < o.D)
-                load_piece<TI, E>(s.g + (int64_t)s.perm[q + j] * s.gstride, col, o.D, x[j]);
-        }
+        for (int j = 0; j < kRows; j++)
+            if (live && skey[q + j] < s.V) x[j] = raw_piece<TI, E>(s.g + (int64_t)sperm[q + j] * s.gstride, col, o.D);
+    };
+    auto add = [&](int q, const Raw (&x)[kRows]) {
 #pragma unroll
         for (int j = 0; j < kRows; j++) {
-            if (key[j] >= s.V) continue;
-            if (key[j] != cur) {
+            const uint32_t key = skey[q + j];
+            if (key >= s.V) continue;
+            if (key != cur) {
                 if (any) {
                     if (continued) {
                         o.leave(2 * c, col, acc);
@@ -368,7 +402,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Sorted<TI> s, Sink<TO> o, 
                         o.finish(row, col, acc);
                     }
                 }
-                cur = key[j];
+                cur = key;
                 continued = false;
                 row = s.compact ? rank++ : (int64_t)cur;
                 if (s.compact && lead && row < o.max_rows) s.row_ids[row] = (int32_t)cur;
@@ -377,8 +411,16 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Sorted<TI> s, Sink<TO> o, 
             }
             any = true;
 #pragma unroll
-            for (int e = 0; e < E; e++) acc[e] += x[j][e];
+            for (int e = 0; e < E; e++) acc[e] += (float)x[j][e];
         }
+    };
+    Raw xa[kRows], xb[kRows];
+    fetch(0, xa);
+    for (int q = 0; q < s.chunk; q += 2 * kRows) {                  // chunk is a multiple of 2 kRows
+        fetch(q + kRows, xb);
+        add(q, xa);
+        if (q + 2 * kRows < s.chunk) fetch(q + 2 * kRows, xa);
+        add(q + kRows, xb);
     }
     if (any) {
         if (q1 < s.n && s.keys[q1] == cur) {                        // goes on in the next chunk
@@ -415,16 +457,17 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(const float* __restrict__
     int32_t cur = -1, head = -1, tail = -1;
     bool continued = false, open = true;
     float acc[E] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t q = q0; open && q < (last ? entries : q1); q += kRows) {
-        int32_t row[kRows];
-        float x[kRows][E];
+    constexpr int R = 8;                                            // entries per batch; chunk is a multiple
+    for (int64_t q = q0; open && q < (last ? entries : q1); q += R) {
+        int32_t row[R];
+        float x[R][E];
 #pragma unroll
-        for (int j = 0; j < kRows; j++) row[j] = q + j < entries ? in_row[q + j] : -1;
+        for (int j = 0; j < R; j++) row[j] = q + j < entries ? in_row[q + j] : -1;
 #pragma unroll
-        for (int j = 0; j < kRows; j++)
+        for (int j = 0; j < R; j++)
             if (row[j] >= 0 && live) Vec<float, E>::load(in + (q + j) * o.dpad + col, x[j]);
 #pragma unroll
-        for (int j = 0; j < kRows; j++) {
+        for (int j = 0; j < R; j++) {
             if (!open) continue;
             const bool begins = (q + j) & 1;                        // a tail begins a run, a head continues one
             if (last && q + j >= q1 && (row[j] < 0 ? !begins || cur < 0 : begins)) {
@@ -473,7 +516,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(const float* __restrict__
 
 // ----------------------------------------------------------------- gradient: host
 
-constexpr int kLevels = 8;                  // 2^31 ids: 2^27 entries, then 1/16 each
+constexpr int kLevels = 8;                  // 2^31 ids: 2^27 entries, then 1/32 each
 struct GradPlan {
     uint32_t *keys[2], *perm[2], *hist, *dtot;
     int64_t *sizes, *rank, *partials;
@@ -572,27 +615,29 @@ static void grad(const agnes_matrix* g, const void* ids, agnes_dtype ids_dtype, 
             keys = p.keys[at];
             perm = p.perm[at];
             if (compact) {
-                AGNES_LAUNCH(k_embed_heads, dim3(blocks_for(p.chunks, kBlock)), dim3(kBlock), 0, st, keys, n, V,
-                             p.chunks, chunk, p.heads);
+                AGNES_LAUNCH(k_embed_heads, dim3(blocks_for(n, kBlock)), dim3(kBlock), 0, st, keys, n, V, p.chunks,
+                             p.heads);
                 scan_counts(p.heads, p.rank, p.sizes + 1, p.chunks, count, p.partials, st);
             }
         });
     with_float(out->dtype, [&](auto to) {
         typedef decltype(to) TO;
+        const bool nt = max_rows * D * (int64_t)sizeof(TO) > kStreamBytes;
         with_float(g->dtype, [&](auto ti) {
             typedef decltype(ti) TI;
             const RowShape shape = row_shape(std::max<int64_t>(D, 1), 16 / (int)sizeof(TI));
             const int fill_lanes = row_shape(D, 16 / (int)sizeof(TO)).lanes;
-            // fewer rows per clearing workgroup when rows are long, so that there are enough of them
-            const int fill_rows = D * (int64_t)sizeof(TO) >= 512 ? 64 : kBlock;
+            // fewer rows per clearing workgroup where rows are long or few, so that there are enough of them
+            const int fill_rows = D * (int64_t)sizeof(TO) >= 512 || num_rows < (1 << 18) ? 64 : kBlock;
             const bool clear = !compact && !accumulate;
             const int64_t sum_blocks = (p.chunks + kBlock / shape.lanes - 1) / (kBlock / shape.lanes) * shape.tiles;
             Sorted<TI> s{(const TI*)g->data, g->stride, keys, perm, n, V, chunk, p.chunks, compact, p.rank, row_ids,
                          count};
-            Sink<TO> o{(TO*)out->data, out->stride, D, max_rows, scale, accumulate, p.part[0], p.part_row[0], p.dpad};
+            Sink<TO> o{(TO*)out->data, out->stride, D, max_rows, scale, accumulate, p.part[0], p.part_row[0], p.dpad, nt};
             const int64_t all = sum_blocks + (clear ? (num_rows + fill_rows - 1) / fill_rows : 0);
             if (all == 0) return;
-            AGNES_LAUNCH((k_embed_sum<TI, TO>), dim3(blocks_for(all, 1)), dim3(kBlock), 0, st, s, o, shape.lanes,
+            const size_t lds = (size_t)(kBlock / shape.lanes) * (chunk + 1) * 2 * sizeof(uint32_t);
+            AGNES_LAUNCH((k_embed_sum<TI, TO>), dim3(blocks_for(all, 1)), dim3(kBlock), lds, st, s, o, shape.lanes,
                          shape.tiles, sum_blocks, fill_rows, fill_lanes);
         });
         if (D == 0) return;
@@ -600,11 +645,11 @@ static void grad(const agnes_matrix* g, const void* ids, agnes_dtype ids_dtype, 
         for (int l = 0; l < p.levels; l++) {
             const bool last = l + 1 == p.levels;
             // the last level: a group per few entries, since it follows each run to its end
-            const int chunk = last ? kRows : kJoinChunk;
+            const int chunk = last ? 8 : kJoinChunk;
             const int64_t groups = (p.entries[l] + chunk - 1) / chunk;
             Sink<TO> o{(TO*)out->data, out->stride,          D,        max_rows,
                        scale,          accumulate,           last ? nullptr : p.part[l + 1],
-                       last ? nullptr : p.part_row[l + 1], p.dpad};
+                       last ? nullptr : p.part_row[l + 1], p.dpad,   nt};
             AGNES_LAUNCH((k_embed_join<TO>), dim3(blocks_for(groups, kBlock / shape.lanes) * shape.tiles), dim3(kBlock),
                          0, st, p.part[l], p.part_row[l], p.entries[l], chunk, last, o, shape.lanes, shape.tiles);
         }

