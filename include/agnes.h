@@ -543,7 +543,8 @@ agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_mat
  * -inf has no q: its loss is +inf (0 if it has no term) and its gradient 0.  NaN or +inf
  * logits make the row's loss and gradient NaN.  All arithmetic is float32; the
  * gradient is rounded once to its type.
- *   logits, teacher: matrices of equal rows; teacher.cols in [0, AGNES_DISTILL_MAX_K].
+ *   logits, teacher: matrices of equal rows; logits.cols in [1, 2^31 - 2^16),
+ *     teacher.cols in [0, AGNES_DISTILL_MAX_K].
  *   classes: index_dtype (AGNES_INT32 or AGNES_INT64) [rows], stride
  *     classes_stride >= 0 elements.
  *   labels: index_dtype [rows], or NULL (no second term).

@@ -61,7 +61,7 @@ __device__ __forceinline__ int64_t load_index(const void* p, bool wide, int64_t 
 
 // E elements at column c of the row whose first element is p[at].
 template <int E, typename T>
-__device__ __forceinline__ void store_typed(T* p, int64_t c, int64_t C, const float (&x)[E], bool nt) {
+__device__ __forceinline__ void store_typed(T* p, int c, int C, const float (&x)[E], bool nt) {
     if (c + E <= C) {
         Vec<T, E>::store(p + c, x, nt);
     } else {
@@ -71,20 +71,10 @@ __device__ __forceinline__ void store_typed(T* p, int64_t c, int64_t C, const fl
     }
 }
 template <int E>
-__device__ __forceinline__ void store_grad(const DistillArgs& a, int64_t at, int64_t c, const float (&x)[E]) {
+__device__ __forceinline__ void store_grad(const DistillArgs& a, int64_t at, int c, const float (&x)[E]) {
     if (a.gtype == AGNES_FLOAT32) store_typed<E>((float*)a.grad + at, c, a.C, x, a.nt);
     else if (a.gtype == AGNES_FLOAT16) store_typed<E>((_Float16*)a.grad + at, c, a.C, x, a.nt);
     else store_typed<E>((__bf16*)a.grad + at, c, a.C, x, a.nt);
-}
-
-// Lanes [g L, (g + 1) L) of a wave reduce among themselves.
-__device__ __forceinline__ float lanes_max(float x, int L) {
-    for (int d = 1; d < L; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, kWave));
-    return x;
-}
-__device__ __forceinline__ float lanes_sum(float x, int L) {
-    for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d, kWave);
-    return x;
 }
 
 // 2^x with results below 2^-126 as 0.
@@ -141,7 +131,7 @@ __device__ __forceinline__ bool no_logits(const Sums& s) { return s.m == -INFINI
 
 // A row's piece, -inf behind the last logit.
 template <typename T, int E>
-__device__ __forceinline__ typename Vec<T, E>::type logits_piece(const T* row, int64_t c, int64_t C) {
+__device__ __forceinline__ typename Vec<T, E>::type logits_piece(const T* row, int c, int C) {
     if (c + E <= C) return Vec<T, E>::raw(row + c);
     typename Vec<T, E>::type v;
 #pragma unroll
@@ -172,11 +162,13 @@ struct Terms {
 // classes (-1: padding) to cls, probabilities to prob.  Every lane gets the terms.
 __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float w, int gl, int L, int32_t* cls,
                                          float* prob) {
+    const int64_t y = a.labels ? load_index(a.labels, a.wide, r) : -1;
     float tm = -INFINITY;
     for (int e = gl; e < a.k; e += L) {
         const int64_t c = load_index(a.classes, a.wide, r * a.cstride + e);
+        const float t = load_any(a.t, a.ttype, r * a.tstride + e);
         const bool ok = c >= 0 && c < a.C;
-        const float x = ok ? load_any(a.t, a.ttype, r * a.tstride + e) * a.inv_t : -INFINITY;
+        const float x = ok ? t * a.inv_t : -INFINITY;
         cls[e] = ok ? (int32_t)c : -1;
         prob[e] = x;
         tm = x != x ? INFINITY : fmaxf(tm, x);   // NaN: as +inf, which makes the sum NaN
@@ -196,7 +188,7 @@ __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float 
         const float inv = 1.f / ts;
         for (int e = gl; e < a.k; e += L) prob[e] *= inv;
     }
-    q.y = a.labels ? load_index(a.labels, a.wide, r) : -1;
+    q.y = y;
     q.named = a.hard > 0.f && q.y >= 0 && q.y < a.C;
     q.ca = q.some ? w * a.soft * a.temp : 0.f;
     q.cb = q.named ? w * a.hard : 0.f;
@@ -320,33 +312,31 @@ template <typename T, int P, int MODE>
 __global__ __launch_bounds__(kBlock) void k_distill_lanes(DistillArgs a, int L) {
     constexpr int E = 16 / (int)sizeof(T);
     typedef typename Vec<T, E>::type Raw;
-    __shared__ int32_t cls_all[kBlock / kLanesMin * kLaneEntries];
-    __shared__ float prob_all[kBlock / kLanesMin * kLaneEntries];
-    __shared__ float zc_all[kBlock / kLanesMin * kLaneEntries];
+    extern __shared__ int32_t entries[];         // per row: classes, probabilities, logits
     const int g = threadIdx.x / L, gl = threadIdx.x % L;
     const int64_t r = (int64_t)blockIdx.x * (kBlock / L) + g;
     if (r >= a.rows) return;                     // whole groups; nothing below crosses a group
-    int32_t* cls = cls_all + g * kLaneEntries;
-    float* prob = prob_all + g * kLaneEntries;
-    float* zc = zc_all + g * kLaneEntries;
+    int32_t* cls = entries + g * 3 * a.k;
+    float* prob = (float*)(cls + a.k);
+    float* zc = prob + a.k;
     const T* zr = (const T*)a.z + r * a.zstride;
     const int64_t at = r * a.gstride;
     const float w = a.weight ? a.weight[r] : 1.f;
+    Raw v[P];
+#pragma unroll
+    for (int i = 0; i < P; i++) v[i] = logits_piece<T, E>(zr, (gl + i * L) * E, a.C);
     if (w == 0.f) {
         if (gl == 0 && a.loss) a.loss[r] = 0.f;
         if (gl == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
         if (a.grad) {
             const float zero[E] = {};
             for (int i = 0; i < P; i++) {
-                const int64_t c = (int64_t)(gl + i * L) * E;
+                const int c = (gl + i * L) * E;
                 if (c < a.C) store_grad<E>(a, at, c, zero);
             }
         }
         return;
     }
-    Raw v[P];
-#pragma unroll
-    for (int i = 0; i < P; i++) v[i] = logits_piece<T, E>(zr, (int64_t)(gl + i * L) * E, a.C);
     const Terms q = teacher(a, r, w, gl, L, cls, prob);
     for (int e = gl; e < a.k; e += L) zc[e] = cls[e] >= 0 ? (float)zr[cls[e]] : 0.f;
     const float zy = q.named ? (float)zr[q.y] : 0.f;
@@ -379,7 +369,7 @@ __global__ __launch_bounds__(kBlock) void k_distill_lanes(DistillArgs a, int L) 
     factors<MODE>(q, s, ka, kb);
 #pragma unroll
     for (int i = 0; i < P; i++) {
-        const int64_t c = (int64_t)(gl + i * L) * E;
+        const int c = (gl + i * L) * E;
         float x[E] = {};
         if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
         if (c < a.C) store_grad<E>(a, at, c, x);
@@ -390,7 +380,7 @@ __global__ __launch_bounds__(kBlock) void k_distill_lanes(DistillArgs a, int L) 
 // ----------------------------------------------------------------- a workgroup per row
 
 template <typename T, int THREADS, int P, int MODE>
-__global__ __launch_bounds__(THREADS) void k_distill_block(DistillArgs a) {
+__global__ __launch_bounds__(THREADS, THREADS == 1024 && P == 8 ? 8 : 4) void k_distill_block(DistillArgs a) {
     constexpr int E = 16 / (int)sizeof(T), WAVES = THREADS / kWave;
     typedef typename Vec<T, E>::type Raw;
     __shared__ int32_t cls[AGNES_DISTILL_MAX_K];
@@ -408,13 +398,14 @@ __global__ __launch_bounds__(THREADS) void k_distill_block(DistillArgs a) {
         if (tid == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
         if (a.grad) {
             const float zero[E] = {};
-            for (int64_t c = (int64_t)tid * E; c < a.C; c += THREADS * E) store_grad<E>(a, at, c, zero);
+            for (int c = tid * E; c < a.C; c += THREADS * E) store_grad<E>(a, at, c, zero);
         }
         return;
     }
     Raw v[P];
 #pragma unroll
-    for (int i = 0; i < P; i++) v[i] = logits_piece<T, E>(zr, (int64_t)(tid + i * THREADS) * E, a.C);
+    for (int i = 0; i < P; i++)
+        if (i * THREADS * E < a.C) v[i] = logits_piece<T, E>(zr, (tid + i * THREADS) * E, a.C);
     Terms q{};
     float zy = 0.f;
     if (wave == 0) {
@@ -426,14 +417,18 @@ __global__ __launch_bounds__(THREADS) void k_distill_block(DistillArgs a) {
     Sums s{-INFINITY, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < P; i++)
+        if (i * THREADS * E < a.C) {
 #pragma unroll
-        for (int x = 0; x < E; x++) s.m = fmaxf(s.m, (float)v[i][x]);
+            for (int x = 0; x < E; x++) s.m = fmaxf(s.m, (float)v[i][x]);
+        }
     s.m = lanes_max(s.m, kWave);
 #pragma unroll
-    for (int i = 0; i < P; i++) {
-        keep_packed(v[i]);
-        add_piece<MODE, E>(s, v[i], a.ct);
-    }
+    for (int i = 0; i < P; i++)
+        if (i * THREADS * E < a.C) {             // no work for rounds that lie behind the row
+            keep_packed(v[i]);
+            add_piece<MODE, E>(s, v[i], a.ct);
+            __builtin_amdgcn_sched_barrier(0);   // one piece's values at a time: registers decide the occupancy
+        }
     s.st = lanes_sum(s.st, kWave);
     s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, kWave);
     if (lane == 0) red[wave] = s;
@@ -458,11 +453,14 @@ __global__ __launch_bounds__(THREADS) void k_distill_block(DistillArgs a) {
     factors<MODE>(q, s, ka, kb);
 #pragma unroll
     for (int i = 0; i < P; i++) {
-        const int64_t c = (int64_t)(tid + i * THREADS) * E;
-        float x[E] = {};
-        keep_packed(v[i]);
-        if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
-        if (c < a.C) store_grad<E>(a, at, c, x);
+        if (i * THREADS * E < a.C) {
+            const int c = (tid + i * THREADS) * E;
+            float x[E] = {};
+            keep_packed(v[i]);
+            if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
+            if (c < a.C) store_grad<E>(a, at, c, x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     __syncthreads();                             // the row's values are stored before the named classes'
     if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, kWave, 0, a.C);
@@ -493,13 +491,13 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_part(DistillArgs a, in
     const T* zr = (const T*)a.z + r * a.zstride;
     const float w = a.weight ? a.weight[r] : 1.f;
     if (w == 0.f) return;                        // the second launch skips the row too
-    const int64_t lo = (int64_t)blockIdx.x * span, hi = min((int64_t)a.C, lo + span);
+    const int lo = (int)(blockIdx.x * span), hi = (int)min((int64_t)a.C, lo + span);
     Sums s{-INFINITY, 0.f, 0.f};
-    for (int64_t c0 = lo; c0 < hi; c0 += (int64_t)kPartThreads * E * U) {
+    for (int c0 = lo; c0 < hi; c0 += kPartThreads * E * U) {
         Raw v[U];
 #pragma unroll
         for (int i = 0; i < U; i++)
-            v[i] = logits_piece<T, E>(zr, c0 + (int64_t)(tid + i * kPartThreads) * E, hi);
+            v[i] = logits_piece<T, E>(zr, c0 + (tid + i * kPartThreads) * E, hi);
         float m = s.m;
 #pragma unroll
         for (int i = 0; i < U; i++)
@@ -551,14 +549,14 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_apply(DistillArgs a, i
     const T* zr = (const T*)a.z + r * a.zstride;
     const int64_t at = r * a.gstride;
     const float w = a.weight ? a.weight[r] : 1.f;
-    const int64_t lo = (int64_t)blockIdx.x * span, hi = min((int64_t)a.C, lo + span);
+    const int lo = (int)(blockIdx.x * span), hi = (int)min((int64_t)a.C, lo + span);
     const bool first = blockIdx.x == 0;
     if (w == 0.f) {
         if (first && tid == 0 && a.loss) a.loss[r] = 0.f;
         if (first && tid == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
         if (a.grad) {
             const float zero[E] = {};
-            for (int64_t c = lo + (int64_t)tid * E; c < hi; c += kPartThreads * E) store_grad<E>(a, at, c, zero);
+            for (int c = lo + tid * E; c < hi; c += kPartThreads * E) store_grad<E>(a, at, c, zero);
         }
         return;
     }
@@ -620,14 +618,14 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_apply(DistillArgs a, i
     float ka, kb;
     factors<MODE>(q, s, ka, kb);
     __syncthreads();                             // the named logits are read before anything is stored
-    for (int64_t c0 = lo; c0 < hi; c0 += (int64_t)kPartThreads * E * U) {
+    for (int c0 = lo; c0 < hi; c0 += kPartThreads * E * U) {
         Raw v[U];
 #pragma unroll
         for (int i = 0; i < U; i++)
-            v[i] = logits_piece<T, E>(zr, c0 + (int64_t)(tid + i * kPartThreads) * E, hi);
+            v[i] = logits_piece<T, E>(zr, c0 + (tid + i * kPartThreads) * E, hi);
 #pragma unroll
         for (int i = 0; i < U; i++) {
-            const int64_t c = c0 + (int64_t)(tid + i * kPartThreads) * E;
+            const int c = c0 + (tid + i * kPartThreads) * E;
             float x[E] = {};
             if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
             if (c < hi) store_grad<E>(a, at, c, x);
@@ -676,6 +674,7 @@ static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* gra
     check_matrix(&d->teacher, false, "teacher");
     const int64_t rows = d->logits.rows, C = d->logits.cols, k = d->teacher.cols;
     AGNES_REQUIRE(C >= 1, AGNES_ERR_INVALID, "there must be at least one class");
+    AGNES_REQUIRE(C < ((int64_t)1 << 31) - (1 << 16), AGNES_ERR_INVALID, "there must be fewer than 2^31 - 2^16 classes");
     AGNES_REQUIRE(d->teacher.rows == rows, AGNES_ERR_INVALID, "teacher and logits must have equal rows");
     AGNES_REQUIRE(k <= AGNES_DISTILL_MAX_K, AGNES_ERR_INVALID, "the teacher may have at most 1024 entries per row");
     AGNES_REQUIRE(is_index(d->index_dtype), AGNES_ERR_INVALID, "classes and labels must be int32 or int64");
@@ -726,9 +725,10 @@ template <typename T, int MODE> static void launch(const DistillArgs& a, void* w
         while (L < pieces && L < kWave) L *= 2;
         const int per = kBlock / L;
         const dim3 grid((unsigned)((rows + per - 1) / per));
-        if (pieces <= kWave) AGNES_LAUNCH((k_distill_lanes<T, 1, MODE>), grid, dim3(kBlock), 0, st, a, L);
-        else if (pieces <= 2 * kWave) AGNES_LAUNCH((k_distill_lanes<T, 2, MODE>), grid, dim3(kBlock), 0, st, a, L);
-        else AGNES_LAUNCH((k_distill_lanes<T, 4, MODE>), grid, dim3(kBlock), 0, st, a, L);
+        const size_t lds = (size_t)per * 3 * a.k * 4;
+        if (pieces <= kWave) AGNES_LAUNCH((k_distill_lanes<T, 1, MODE>), grid, dim3(kBlock), lds, st, a, L);
+        else if (pieces <= 2 * kWave) AGNES_LAUNCH((k_distill_lanes<T, 2, MODE>), grid, dim3(kBlock), lds, st, a, L);
+        else AGNES_LAUNCH((k_distill_lanes<T, 4, MODE>), grid, dim3(kBlock), lds, st, a, L);
         return;
     }
     int64_t span = 0;

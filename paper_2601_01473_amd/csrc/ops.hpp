@@ -37,6 +37,42 @@ template <typename T, int E> struct Vec {
     }
 };
 
+// ----------------------------------------------------------------- reductions over lanes
+
+// x of the lane that this one pairs with in step D = 1, 2, .. 32 of a butterfly,
+// without a trip through LDS.  Steps 4 and 8 mirror 8 and 16 lanes: once the
+// steps before have been taken, all lanes of a half hold the same value.
+template <int D> __device__ __forceinline__ float lane_pair(float x) {
+    const int v = __float_as_int(x);
+    if (D == 1) return __int_as_float(__builtin_amdgcn_update_dpp(v, v, 0xB1, 0xF, 0xF, false));    // quad_perm 1 0 3 2
+    if (D == 2) return __int_as_float(__builtin_amdgcn_update_dpp(v, v, 0x4E, 0xF, 0xF, false));    // quad_perm 2 3 0 1
+    if (D == 4) return __int_as_float(__builtin_amdgcn_update_dpp(v, v, 0x141, 0xF, 0xF, false));   // row_half_mirror
+    return __int_as_float(__builtin_amdgcn_update_dpp(v, v, 0x140, 0xF, 0xF, false));               // row_mirror
+}
+
+// Lanes [g L, (g + 1) L) of a wave (L a power of two) reduce among themselves.
+template <typename Op> __device__ __forceinline__ float lanes_reduce(float x, int L, Op op) {
+    if (L > 1) x = op(x, lane_pair<1>(x));
+    if (L > 2) x = op(x, lane_pair<2>(x));
+    if (L > 4) x = op(x, lane_pair<4>(x));
+    if (L > 8) x = op(x, lane_pair<8>(x));
+    if (L > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (L > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return x;
+}
+__device__ __forceinline__ float lanes_max(float x, int L) {
+    return lanes_reduce(x, L, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float lanes_sum(float x, int L) {
+    return lanes_reduce(x, L, [](float a, float b) { return a + b; });
+}
+
 // ----------------------------------------------------------------- host side
 
 inline size_t elem_size(agnes_dtype t) { return t == AGNES_FLOAT32 ? 4 : 2; }
