@@ -59,22 +59,37 @@ __device__ __forceinline__ int64_t load_index(const void* p, bool wide, int64_t 
     return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i];
 }
 
-// E elements at column c of the row whose first element is p[at].
+// Pieces count from the row's first logit wherever that lies, so that equal rows
+// have equal sums at any address.  (8192 rows of 50021 bfloat16, which start
+// anywhere: 358 us; with pieces at multiples of 16 bytes of memory 309 us, but
+// sums that depend on the address.)
 template <int E, typename T>
-__device__ __forceinline__ void store_typed(T* p, int c, int C, const float (&x)[E], bool nt) {
-    if (c + E <= C) {
+__device__ __forceinline__ void store_typed(T* p, int c, int hi, const float (&x)[E], bool nt) {
+    if (c + E <= hi) {
         Vec<T, E>::store(p + c, x, nt);
     } else {
 #pragma unroll
         for (int q = 0; q < E; q++)
-            if (c + q < C) p[c + q] = (T)x[q];
+            if (c + q < hi) p[c + q] = (T)x[q];
     }
 }
+
+// E gradients from column c on, those before column hi, of the row whose first element is number `at`.
 template <int E>
-__device__ __forceinline__ void store_grad(const DistillArgs& a, int64_t at, int c, const float (&x)[E]) {
-    if (a.gtype == AGNES_FLOAT32) store_typed<E>((float*)a.grad + at, c, a.C, x, a.nt);
-    else if (a.gtype == AGNES_FLOAT16) store_typed<E>((_Float16*)a.grad + at, c, a.C, x, a.nt);
-    else store_typed<E>((__bf16*)a.grad + at, c, a.C, x, a.nt);
+__device__ __forceinline__ void store_grad(const DistillArgs& a, int64_t at, int c, int hi, const float (&x)[E]) {
+    if (a.gtype == AGNES_FLOAT32) store_typed<E>((float*)a.grad + at, c, hi, x, a.nt);
+    else if (a.gtype == AGNES_FLOAT16) store_typed<E>((_Float16*)a.grad + at, c, hi, x, a.nt);
+    else store_typed<E>((__bf16*)a.grad + at, c, hi, x, a.nt);
+}
+
+// A row's piece from column c on, -inf from column hi on.
+template <typename T, int E>
+__device__ __forceinline__ typename Vec<T, E>::type logits_piece(const T* row, int c, int hi) {
+    if (c + E <= hi) return Vec<T, E>::raw(row + c);
+    typename Vec<T, E>::type v;
+#pragma unroll
+    for (int q = 0; q < E; q++) v[q] = c + q < hi ? row[c + q] : (T)-INFINITY;
+    return v;
 }
 
 // 2^x with results below 2^-126 as 0.
@@ -129,16 +144,6 @@ template <int MODE> __device__ __forceinline__ Sums lanes_join(Sums s, int L, fl
 // Every logit is -inf.
 __device__ __forceinline__ bool no_logits(const Sums& s) { return s.m == -INFINITY && s.st == 0.f; }
 
-// A row's piece, -inf behind the last logit.
-template <typename T, int E>
-__device__ __forceinline__ typename Vec<T, E>::type logits_piece(const T* row, int c, int C) {
-    if (c + E <= C) return Vec<T, E>::raw(row + c);
-    typename Vec<T, E>::type v;
-#pragma unroll
-    for (int q = 0; q < E; q++) v[q] = c + q < C ? row[c + q] : (T)-INFINITY;
-    return v;
-}
-
 // Makes the compiler take the piece from its packed registers again: it would
 // otherwise keep the logits' float32 values from the maximum to the gradient,
 // twice the registers, and spill.
@@ -158,18 +163,35 @@ struct Terms {
     float w, ca, cb;
 };
 
-// The teacher's distribution over lanes gl = 0 .. L - 1, entries e = gl, gl + L, ...:
-// classes (-1: padding) to cls, probabilities to prob.  Every lane gets the terms.
-__device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float w, int gl, int L, int32_t* cls,
-                                         float* prob) {
-    const int64_t y = a.labels ? load_index(a.labels, a.wide, r) : -1;
+// A lane's entry e of the teacher and the row's label, as loaded.
+struct Entry {
+    int64_t c;
+    float t;
+};
+__device__ __forceinline__ Entry load_entry(const DistillArgs& a, int64_t r, int e) {
+    Entry x{-1, 0.f};
+    if (e < a.k) {
+        x.c = load_index(a.classes, a.wide, r * a.cstride + e);
+        x.t = load_any(a.t, a.ttype, r * a.tstride + e);
+    }
+    return x;
+}
+__device__ __forceinline__ int64_t load_label(const DistillArgs& a, int64_t r) {
+    return a.labels ? load_index(a.labels, a.wide, r) : -1;
+}
+
+// The teacher's distribution over lanes gl = 0 .. L - 1, entries e = gl (loaded
+// before: first), gl + L, ...: classes (-1: padding) to cls, probabilities to
+// prob.  Every lane gets the terms.
+__device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float w, Entry first, int64_t y, int gl,
+                                         int L, int32_t* cls, float* prob) {
     float tm = -INFINITY;
+    Entry n = first;
     for (int e = gl; e < a.k; e += L) {
-        const int64_t c = load_index(a.classes, a.wide, r * a.cstride + e);
-        const float t = load_any(a.t, a.ttype, r * a.tstride + e);
-        const bool ok = c >= 0 && c < a.C;
-        const float x = ok ? t * a.inv_t : -INFINITY;
-        cls[e] = ok ? (int32_t)c : -1;
+        if (e != gl) n = load_entry(a, r, e);
+        const bool ok = n.c >= 0 && n.c < a.C;
+        const float x = ok ? n.t * a.inv_t : -INFINITY;
+        cls[e] = ok ? (int32_t)n.c : -1;
         prob[e] = x;
         tm = x != x ? INFINITY : fmaxf(tm, x);   // NaN: as +inf, which makes the sum NaN
     }
@@ -193,6 +215,10 @@ __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float 
     q.ca = q.some ? w * a.soft * a.temp : 0.f;
     q.cb = q.named ? w * a.hard : 0.f;
     return q;
+}
+__device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float w, int gl, int L, int32_t* cls,
+                                         float* prob) {
+    return teacher(a, r, w, load_entry(a, r, gl), load_label(a, r), gl, L, cls, prob);
 }
 
 // sum_e p_e (ln p_e - ln q_{c_e}) over the lanes, from z_{c_e} in zc.
@@ -268,34 +294,38 @@ __device__ __forceinline__ float listed(const int32_t* cls, const float* prob, i
     return p;
 }
 
+// Whether the lane's class c (-1: none) may be listed twice: certain if all
+// entries are in the L lanes of its group, else assumed.
+__device__ __forceinline__ bool listed_twice(const DistillArgs& a, int32_t c, int L) {
+    if (a.k > L) return true;
+    uint64_t same = __ballot(c >= 0);
+    if (L < kWave) same &= ((1ull << L) - 1) << (lane_id() & ~(L - 1));
+    for (int b = 0; b < 31 && (a.C >> b); b++) {
+        const uint64_t m = __ballot((c >> b) & 1);
+        same &= ((c >> b) & 1) ? m : ~m;
+    }
+    return (same & (same - 1)) != 0;
+}
+
 // Stores the gradient of the classes in [lo, hi) that the teacher lists or the
-// label names, by lanes gl = 0 .. L - 1 of one wave.  A class listed twice is stored
-// twice, with the same value.
+// label names, by one wave.  A class listed twice is stored twice, with the
+// same value.
 template <int MODE>
 __device__ __forceinline__ void store_named(const DistillArgs& a, const Terms& q, const Sums& s, float ka, float kb,
                                             const int32_t* cls, const float* prob, const float* zc, float zy,
-                                            int64_t at, int gl, int L, int64_t lo, int64_t hi) {
+                                            int64_t at, int lane, int lo, int hi) {
     wave_sync();                                 // cls and prob of the other lanes
     if (q.some) {
-        for (int e0 = 0; e0 < a.k; e0 += L) {
-            const int e = e0 + gl;
+        for (int e0 = 0; e0 < a.k; e0 += kWave) {
+            const int e = e0 + lane;
             const int32_t c = e < a.k ? cls[e] : -1;
-            bool again = true;
-            if (a.k <= kWave && L == kWave) {
-                // all entries are in this wave: is any class in two lanes?
-                uint64_t same = __ballot(c >= 0);
-                for (int b = 0; b < 31 && (a.C >> b); b++) {
-                    const uint64_t m = __ballot((c >> b) & 1);
-                    same &= ((c >> b) & 1) ? m : ~m;
-                }
-                again = __ballot(c >= 0 && (same & (same - 1))) != 0;
-            }
+            const bool again = listed_twice(a, c, kWave);
             if (c < 0 || c < lo || c >= hi) continue;
             const float p = again ? listed(cls, prob, a.k, c) : prob[e];
             store_any(a.grad, a.gtype, at + c, grad_named<MODE>(a, q, s, ka, kb, zc[e], c, p));
         }
     }
-    if (q.named && gl == 0 && q.y >= lo && q.y < hi) {
+    if (q.named && lane == 0 && q.y >= lo && q.y < hi) {
         const float p = q.some ? listed(cls, prob, a.k, (int32_t)q.y) : 0.f;
         store_any(a.grad, a.gtype, at + q.y, grad_named<MODE>(a, q, s, ka, kb, zy, q.y, p));
     }
@@ -303,78 +333,141 @@ __device__ __forceinline__ void store_named(const DistillArgs& a, const Terms& q
 
 // ----------------------------------------------------------------- lanes of a wave per row
 
-// L lanes per row, P pieces per lane (P > 1: L = 64).  Up to kLaneEntries
-// teacher entries.
+// L lanes per row, P pieces per lane, up to kLaneEntries teacher entries.  What a
+// row costs besides its logits is the same for every row of a wave, so a lane
+// takes up to four pieces before a row takes more lanes (65536 rows of 172
+// float32: 74 us with 64 lanes per row, 36 us with 16).  A row is short work behind a long wait, so a group takes several
+// rows, and the next row's logits, entries, label and weight are loaded before
+// the present row's arithmetic.  The row also goes to LDS, where the named
+// logits are found; then what the named classes lose goes there, so that every
+// gradient is stored once.
 constexpr int kLaneEntries = 64;
 constexpr int kLanesMin = 8;
+constexpr int kLaneGroups = 2048;                // workgroups, about what the chip holds at once
+
+template <typename T, int P> struct LaneRow {
+    static constexpr int E = 16 / (int)sizeof(T);
+    typename Vec<T, E>::type v[P];
+    float w;
+    Entry first;
+    int64_t y;
+};
 
 template <typename T, int P, int MODE>
 __global__ __launch_bounds__(kBlock) void k_distill_lanes(DistillArgs a, int L) {
     constexpr int E = 16 / (int)sizeof(T);
-    typedef typename Vec<T, E>::type Raw;
-    extern __shared__ int32_t entries[];         // per row: classes, probabilities, logits
-    const int g = threadIdx.x / L, gl = threadIdx.x % L;
-    const int64_t r = (int64_t)blockIdx.x * (kBlock / L) + g;
-    if (r >= a.rows) return;                     // whole groups; nothing below crosses a group
-    int32_t* cls = entries + g * 3 * a.k;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int groups = kBlock / L, g = threadIdx.x / L, gl = threadIdx.x % L;
+    float* corr = lds + g * (L * P * E);                    // what a column's gradient loses
+    T* zrow = (T*)corr;                                     // before that, the row's logits
+    int32_t* cls = (int32_t*)(lds + kBlock * P * E) + g * 2 * a.k;
     float* prob = (float*)(cls + a.k);
-    float* zc = prob + a.k;
-    const T* zr = (const T*)a.z + r * a.zstride;
-    const int64_t at = r * a.gstride;
-    const float w = a.weight ? a.weight[r] : 1.f;
-    Raw v[P];
+    const int64_t step = (int64_t)gridDim.x * groups;
+    int64_t r = (int64_t)blockIdx.x * groups + g;
+    auto load = [&](int64_t i) {
+        LaneRow<T, P> x;
+        const T* zr = (const T*)a.z + i * a.zstride;
 #pragma unroll
-    for (int i = 0; i < P; i++) v[i] = logits_piece<T, E>(zr, (gl + i * L) * E, a.C);
-    if (w == 0.f) {
-        if (gl == 0 && a.loss) a.loss[r] = 0.f;
-        if (gl == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
-        if (a.grad) {
-            const float zero[E] = {};
-            for (int i = 0; i < P; i++) {
-                const int c = (gl + i * L) * E;
-                if (c < a.C) store_grad<E>(a, at, c, zero);
+        for (int p = 0; p < P; p++) x.v[p] = logits_piece<T, E>(zr, (gl + p * L) * E, a.C);
+        x.w = a.weight ? a.weight[i] : 1.f;
+        x.first = load_entry(a, i, gl);
+        x.y = load_label(a, i);
+        return x;
+    };
+    LaneRow<T, P> next;
+    if (r < a.rows) next = load(r);
+    for (; r < a.rows; r += step) {                         // per group; nothing below crosses a group
+        LaneRow<T, P> x = next;
+        if (r + step < a.rows) next = load(r + step);
+        const int64_t at = r * a.gstride;
+        if (x.w == 0.f) {
+            if (gl == 0 && a.loss) a.loss[r] = 0.f;
+            if (gl == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
+            if (a.grad) {
+                const float zero[E] = {};
+#pragma unroll
+                for (int p = 0; p < P; p++) store_grad<E>(a, at, (gl + p * L) * E, a.C, zero);
             }
+            continue;
         }
-        return;
-    }
-    const Terms q = teacher(a, r, w, gl, L, cls, prob);
-    for (int e = gl; e < a.k; e += L) zc[e] = cls[e] >= 0 ? (float)zr[cls[e]] : 0.f;
-    const float zy = q.named ? (float)zr[q.y] : 0.f;
-    Sums s{-INFINITY, 0.f, 0.f};
-    if (a.stats_in) {
-        s = Sums{a.stats_in[3 * r], a.stats_in[3 * r + 1], a.stats_in[3 * r + 2]};
-    } else {
+        wave_sync();                                        // the row before is done with the LDS
 #pragma unroll
-        for (int i = 0; i < P; i++)
+        for (int p = 0; p < P; p++) __builtin_memcpy(__builtin_assume_aligned(zrow + (gl + p * L) * E, 16), &x.v[p], 16);
+        const Terms q = teacher(a, r, x.w, x.first, x.y, gl, L, cls, prob);
+        Sums s{-INFINITY, 0.f, 0.f};
+        if (a.stats_in) {
+            s = Sums{a.stats_in[3 * r], a.stats_in[3 * r + 1], a.stats_in[3 * r + 2]};
+        } else {
 #pragma unroll
-            for (int x = 0; x < E; x++) s.m = fmaxf(s.m, (float)v[i][x]);
-        s.m = lanes_max(s.m, L);
+            for (int p = 0; p < P; p++)
 #pragma unroll
-        for (int i = 0; i < P; i++) add_piece<MODE, E>(s, v[i], a.ct);
-        s.st = lanes_sum(s.st, L);
-        s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, L);
-    }
-    if (a.loss) {
-        const float div = q.some ? divergence(a, s, prob, zc, gl, L) : 0.f;
-        if (gl == 0) a.loss[r] = row_loss(a, q, s, div, zy - s.m);
-    }
-    if (gl == 0 && a.stats) {
-        a.stats[3 * r] = s.m;
-        a.stats[3 * r + 1] = s.st;
-        a.stats[3 * r + 2] = s.s1;
-    }
-    if (!a.grad) return;
-    const bool empty = no_logits(s);
-    float ka, kb;
-    factors<MODE>(q, s, ka, kb);
+                for (int e = 0; e < E; e++) s.m = fmaxf(s.m, (float)x.v[p][e]);
+            s.m = lanes_max(s.m, L);
 #pragma unroll
-    for (int i = 0; i < P; i++) {
-        const int c = (gl + i * L) * E;
-        float x[E] = {};
-        if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
-        if (c < a.C) store_grad<E>(a, at, c, x);
+            for (int p = 0; p < P; p++) {
+                keep_packed(x.v[p]);
+                add_piece<MODE, E>(s, x.v[p], a.ct);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            s.st = lanes_sum(s.st, L);
+            s.s1 = MODE == kOne ? s.st : lanes_sum(s.s1, L);
+        }
+        if (a.loss) {
+            wave_sync();                                    // the row is in LDS
+            float div = 0.f;
+            if (q.some) {
+                const float lt = logf(s.st);
+                for (int e = gl; e < a.k; e += L) {
+                    const float p = prob[e];
+                    if (p != 0.f) {
+                        const float z = (float)zrow[cls[e]];
+                        div += p * (logf(p) - ((z - s.m) * a.inv_t - lt));
+                    }
+                }
+                div = lanes_sum(div, L);
+            }
+            const float zy = q.named ? (float)zrow[q.y] : 0.f;
+            if (gl == 0) a.loss[r] = row_loss(a, q, s, div, zy - s.m);
+        }
+        if (gl == 0 && a.stats) {
+            a.stats[3 * r] = s.m;
+            a.stats[3 * r + 1] = s.st;
+            a.stats[3 * r + 2] = s.s1;
+        }
+        if (!a.grad) continue;
+        wave_sync();                                        // the row's logits have been read
+        const bool empty = no_logits(s), live = !empty && (q.some || q.named);
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        f32x4* const mine = (f32x4*)(corr + gl * E);        // piece p: mine[p L E / 4 ..]
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int e = 0; e < E / 4; e++) mine[p * (L * E / 4) + e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        wave_sync();
+        if (q.some)
+            for (int e = gl; e < a.k; e += L) {
+                const int32_t c = cls[e];
+                const bool again = listed_twice(a, c, L);
+                if (c >= 0) corr[c] = q.ca * (again ? listed(cls, prob, a.k, c) : prob[e]);
+            }
+        wave_sync();
+        if (q.named && gl == 0) corr[q.y] += q.cb;
+        wave_sync();
+        float ka, kb;
+        factors<MODE>(q, s, ka, kb);
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            float y[E] = {};
+            keep_packed(x.v[p]);
+            if (live) {
+                grad_piece<MODE, E>(a, x.v[p], s, ka, kb, y);
+#pragma unroll
+                for (int e = 0; e < E; e++) y[e] -= mine[p * (L * E / 4) + e / 4][e % 4];
+            }
+            store_grad<E>(a, at, (gl + p * L) * E, a.C, y);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    if (!empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, gl, L, 0, a.C);
 }
 
 // ----------------------------------------------------------------- a workgroup per row
@@ -398,7 +491,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 && P == 8 ? 8 : 4) void k_
         if (tid == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
         if (a.grad) {
             const float zero[E] = {};
-            for (int c = tid * E; c < a.C; c += THREADS * E) store_grad<E>(a, at, c, zero);
+            for (int c = tid * E; c < a.C; c += THREADS * E) store_grad<E>(a, at, c, a.C, zero);
         }
         return;
     }
@@ -458,12 +551,12 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 && P == 8 ? 8 : 4) void k_
             float x[E] = {};
             keep_packed(v[i]);
             if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
-            if (c < a.C) store_grad<E>(a, at, c, x);
+            store_grad<E>(a, at, c, a.C, x);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
     __syncthreads();                             // the row's values are stored before the named classes'
-    if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, kWave, 0, a.C);
+    if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, 0, a.C);
 }
 
 // ----------------------------------------------------------------- a row over several workgroups
@@ -556,7 +649,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_apply(DistillArgs a, i
         if (first && tid == 0 && a.stats) a.stats[3 * r] = a.stats[3 * r + 1] = a.stats[3 * r + 2] = 0.f;
         if (a.grad) {
             const float zero[E] = {};
-            for (int c = lo + tid * E; c < hi; c += kPartThreads * E) store_grad<E>(a, at, c, zero);
+            for (int c = lo + tid * E; c < hi; c += kPartThreads * E) store_grad<E>(a, at, c, hi, zero);
         }
         return;
     }
@@ -628,11 +721,11 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_apply(DistillArgs a, i
             const int c = c0 + (tid + i * kPartThreads) * E;
             float x[E] = {};
             if (!empty && (q.some || q.named)) grad_piece<MODE, E>(a, v[i], s, ka, kb, x);
-            if (c < hi) store_grad<E>(a, at, c, x);
+            store_grad<E>(a, at, c, hi, x);
         }
     }
     __syncthreads();
-    if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, kWave, lo, hi);
+    if (wave == 0 && !empty) store_named<MODE>(a, q, s, ka, kb, cls, prob, zc, zy, at, lane, lo, hi);
 }
 
 // ----------------------------------------------------------------- host
@@ -643,10 +736,11 @@ constexpr int64_t kBlockPieces = 16 * 1024;      // a workgroup's rows
 constexpr int64_t kSplitRows = 512;              // fewer rows leave too many compute units idle
 constexpr int64_t kSplitGroups = 1024;           // workgroups that a split aims at
 
-// Parts of a row of C logits of `size` bytes, or 1: not split.  A part has at
-// least one round of its workgroup.
+// Parts of a row of C logits of `size` bytes, or 1 and span 0: not split.  A
+// part has at least one round of its workgroup.
 static int parts_of(int64_t rows, int64_t C, int64_t size, int64_t& span) {
     const int64_t E = 16 / size, pieces = (C + E - 1) / E, round = (int64_t)kPartThreads * E;
+    span = 0;
     const bool many = pieces > kBlockPieces;
     if (!many && (pieces <= kSplitPieces || rows >= kSplitRows)) return 1;
     const int64_t want = std::max<int64_t>((kSplitGroups + rows - 1) / rows, many ? 2 : 1);
@@ -661,7 +755,6 @@ uint64_t distill_bytes(int64_t rows, int64_t classes) {
     if (rows == 0 || classes == 0) return 0;
     int64_t span = 0, most = 0;
     for (int64_t size : {2, 4}) {                // either size of logits
-        span = 0;
         const int n = parts_of(rows, classes, size, span);
         if (span) most = std::max<int64_t>(most, rows * n * (int64_t)sizeof(Part));
     }
@@ -721,13 +814,15 @@ template <typename T, int MODE> static void launch(const DistillArgs& a, void* w
     constexpr int E = 16 / (int)sizeof(T);
     const int64_t pieces = (a.C + E - 1) / E, rows = a.rows;
     if (pieces <= kLanePieces && a.k <= kLaneEntries) {
+        // at least a lane per teacher entry: their comparisons grow with the entries of a lane
         int L = kLanesMin;
-        while (L < pieces && L < kWave) L *= 2;
+        while (L * 4 < pieces || L < a.k) L *= 2;
+        const int P = pieces <= L ? 1 : pieces <= 2 * L ? 2 : 4;
         const int per = kBlock / L;
-        const dim3 grid((unsigned)((rows + per - 1) / per));
-        const size_t lds = (size_t)per * 3 * a.k * 4;
-        if (pieces <= kWave) AGNES_LAUNCH((k_distill_lanes<T, 1, MODE>), grid, dim3(kBlock), lds, st, a, L);
-        else if (pieces <= 2 * kWave) AGNES_LAUNCH((k_distill_lanes<T, 2, MODE>), grid, dim3(kBlock), lds, st, a, L);
+        const dim3 grid((unsigned)std::min<int64_t>((rows + per - 1) / per, kLaneGroups));
+        const size_t lds = (size_t)kBlock * P * E * 4 + (size_t)per * 2 * a.k * 4;
+        if (P == 1) AGNES_LAUNCH((k_distill_lanes<T, 1, MODE>), grid, dim3(kBlock), lds, st, a, L);
+        else if (P == 2) AGNES_LAUNCH((k_distill_lanes<T, 2, MODE>), grid, dim3(kBlock), lds, st, a, L);
         else AGNES_LAUNCH((k_distill_lanes<T, 4, MODE>), grid, dim3(kBlock), lds, st, a, L);
         return;
     }
