@@ -312,10 +312,12 @@ class Batch:
         rows = int(v.node_off[v.H])
         with ops._on(stream, table, out):
             if out is None:
-                out = torch.empty(rows, m.cols, dtype=dtype or table.dtype, device="cuda")
+                out, o = ops._new(table, rows, m.cols, dtype or table.dtype)
             elif dtype is not None and out.dtype != dtype:
                 raise ValueError("out must be of the type asked for")
-            B.agnes_batch_embedding_lookup(self.handle, m, scale, ops._matrix(out, "out"), ops._handle(stream))
+            else:
+                o = ops._matrix(out, "out")
+            B.agnes_batch_embedding_lookup(self.handle, m, scale, o, ops._handle(stream))
         return out
 
     def embedding_grad_rows(self, grad_out: torch.Tensor, max_rows: int | None = None, scale: float = 1.0,
@@ -329,13 +331,13 @@ class Batch:
         with ops._on(stream, grad_out):
             g = ops._rows_of(grad_out)
             m = ops._matrix(g, "grad_out")
-            row_ids = torch.empty(max_rows, dtype=torch.int32, device="cuda")
-            rows = torch.empty(max_rows, m.cols, dtype=dtype or grad_out.dtype, device="cuda")
-            count = torch.empty(1, dtype=torch.int64, device="cuda")
-            ws = ops._workspace(B.agnes_embedding_grad_bytes(m.rows, self.store.num_nodes, m.cols))
-            B.agnes_batch_embedding_grad_rows(self.handle, m, scale, row_ids.data_ptr(), ops._matrix(rows, "rows"),
-                                              count.data_ptr(), ops._ptr(ws), 0 if ws is None else ws.numel(),
-                                              ops._handle(stream))
+            row_ids = g.new_empty(max_rows, dtype=torch.int32)
+            rows, o = ops._new(g, max_rows, m.cols, dtype or grad_out.dtype)
+            count = g.new_empty(1, dtype=torch.int64)
+            need = ops._grad_bytes(m.rows, self.store.num_nodes, m.cols)
+            ws = ops._workspace(g, need)
+            B.agnes_batch_embedding_grad_rows(self.handle, m, scale, row_ids.data_ptr(), o, count.data_ptr(),
+                                              ops._ptr(ws), need, ops._handle(stream))
         return row_ids, rows, count
 
     def tier_stats(self) -> dict:

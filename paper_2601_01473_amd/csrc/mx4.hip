@@ -17,109 +17,391 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kMxBlock = 32;                       // elements per scale
 static int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
-// The 4-bit code of y: nearest magnitude of {0, 0.5, 1, 1.5, 2, 3, 4, 6}, ties to the even code.
-__device__ __forceinline__ uint32_t e2m1(float y) {
-    const float a = fabsf(y);
-    const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
-    return c | (y < 0.f ? 8u : 0u);
-}
+// ----------------------------------------------------------------- elements
 
 // 2^e for e in [-127, 127] (2^-127 is a subnormal).
 __device__ __forceinline__ float exp2_int(int e) {
     return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : 1u << 22);
 }
 
-// One thread per block of 32.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_mx4_quantize(const T* __restrict__ x, int64_t stride, int64_t rows,
-                                                         int64_t cols, int64_t blocks, uint8_t* __restrict__ codes,
-                                                         uint8_t* __restrict__ scales) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= rows * blocks) return;
-    const int64_t r = i / blocks, b = i % blocks;
-    float v[kMxBlock];
-    uint32_t top = 0;
-#pragma unroll
-    for (int q = 0; q < kMxBlock; q++) {
-        const int64_t c = b * kMxBlock + q;
-        v[q] = c < cols ? to_float(x[r * stride + c]) : 0.f;
-        top = max(top, __float_as_uint(v[q]) & 0x7FFFFFFFu);
-    }
+// The scale code of a block whose largest magnitude has the float32 bits `top`.
+__device__ __forceinline__ int scale_code(uint32_t top) {
     const int e = (int)(top >> 23);
-    const int code = e == 255 ? 255 : max(e - 2, 0);
-    const float inv = code == 255 ? 0.f : exp2_int(127 - code);
-    uint32_t out[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int q = 0; q < kMxBlock; q++) out[q / 8] |= (code == 255 ? 0u : e2m1(v[q] * inv)) << (4 * (q % 8));
-    scales[i] = (uint8_t)code;
-    *(uint4*)(codes + 16 * i) = uint4{out[0], out[1], out[2], out[3]};
+    return e == 255 ? 255 : max(e - 2, 0);
 }
 
-__device__ __forceinline__ float e2m1_value(uint32_t c) {
-    const float mag = (c & 6u) ? __uint_as_float((((c >> 1) & 3u) + 126u) << 23 | (c & 1u) << 22) : 0.5f * (float)(c & 1u);
-    return (c & 8u) ? -mag : mag;
+// Eight elements times 2^(127 - code), to eight 4-bit codes, the first in the
+// low bits: nearest, ties to the even code, magnitudes above 6 to 6.  The
+// product is exact, so the conversion instruction rounds once; its own scale
+// is 1.
+__device__ __forceinline__ uint32_t to_codes(const float (&x)[8], int code) {
+    const float inv = code == 255 ? 0.f : exp2_int(127 - code);
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[0] * inv, x[1] * inv, 1.f, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[2] * inv, x[3] * inv, 1.f, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[4] * inv, x[5] * inv, 1.f, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6] * inv, x[7] * inv, 1.f, 3);
+    if (code == 255) return 0;                     // 0 * inf above
+    const uint32_t zero = ((x[0] == 0.f) << 3) | ((x[1] == 0.f) << 7) | ((x[2] == 0.f) << 11) | ((x[3] == 0.f) << 15) |
+                          ((x[4] == 0.f) << 19) | ((x[5] == 0.f) << 23) | ((x[6] == 0.f) << 27) |
+                          ((uint32_t)(x[7] == 0.f) << 31);
+    return r & ~zero;                              // -0 as 0
+}
+
+__device__ __forceinline__ uint32_t top_bits(const float (&x)[8]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 8; q++) top = max(top, __float_as_uint(x[q]) & 0x7FFFFFFFu);
+    return top;
+}
+
+// Eight elements from column c of a row on, zeros behind its end.
+template <typename T> __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, float (&x)[8]) {
+    if (c + 8 <= cols) {
+        Vec<T, 8>::load(row + c, x);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; q++) x[q] = c + q < cols ? to_float(row[c + q]) : 0.f;
+    }
+}
+
+// ----------------------------------------------------------------- quantisation
+
+// A piece is 8 elements, a block four pieces in adjacent lanes.  Pieces are
+// numbered row after row; a workgroup takes kPieces rounds of 256.
+constexpr int kPieces = 4;
+
+struct PieceAt {
+    int64_t row;
+    int32_t piece;
+};
+// Piece i of rows of `per_row` pieces; base: the workgroup's first piece.
+__device__ __forceinline__ PieceAt piece_at(int64_t base_row, uint32_t base_piece, uint32_t off, uint32_t per_row) {
+    const uint32_t x = base_piece + off;           // both below 2^30
+    return {base_row + x / per_row, (int32_t)(x % per_row)};
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_mx4_quantize(const T* __restrict__ x, int64_t stride, int64_t pieces,
+                                                         int64_t cols, uint32_t per_row, uint8_t* __restrict__ codes,
+                                                         uint8_t* __restrict__ scales) {
+    const int64_t base = (int64_t)blockIdx.x * (kBlock * kPieces);
+    const int64_t base_row = base / per_row;
+    const uint32_t base_piece = (uint32_t)(base % per_row);
+    float v[kPieces][8];
+#pragma unroll
+    for (int u = 0; u < kPieces; u++) {
+        const uint32_t off = u * kBlock + threadIdx.x;
+        if (base + off < pieces) {
+            const PieceAt p = piece_at(base_row, base_piece, off, per_row);
+            load8<T>(x + p.row * stride, (int64_t)p.piece * 8, cols, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kPieces; u++) {
+        const int64_t i = base + u * kBlock + threadIdx.x;
+        if (i >= pieces) continue;                 // whole blocks: pieces is a multiple of 4
+        float top = __uint_as_float(top_bits(v[u]));
+        // as unsigned numbers, NaN above infinity above all finite values
+        uint32_t t = __float_as_uint(top);
+        t = max(t, __float_as_uint(lane_pair<1>(__uint_as_float(t))));
+        t = max(t, __float_as_uint(lane_pair<2>(__uint_as_float(t))));
+        const int code = scale_code(t);
+        *(uint32_t*)(codes + 4 * i) = to_codes(v[u], code);
+        if (threadIdx.x % 4 == 0) scales[i / 4] = (uint8_t)code;
+    }
+}
+
+// Two 4-bit codes to float32, exactly; the scale is applied by a product, since
+// 2^-127 is no normal number.
+template <int BYTE> __device__ __forceinline__ void from_codes(uint32_t c, float s, float (&x)[8]) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, BYTE);
+    x[2 * BYTE] = v[0] * s;
+    x[2 * BYTE + 1] = v[1] * s;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_mx4_dequantize(const uint8_t* __restrict__ codes,
-                                                           const uint8_t* __restrict__ scales, int64_t rows,
-                                                           int64_t cols, int64_t blocks, T* __restrict__ x,
-                                                           int64_t stride) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= rows * blocks) return;
-    const int64_t r = i / blocks, b = i % blocks;
-    const int code = scales[i];
-    const float s = code == 255 ? __uint_as_float(0x7FC00000u) : exp2_int(code - 127);
-    const uint4 w = *(const uint4*)(codes + 16 * i);
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+                                                           const uint8_t* __restrict__ scales, int64_t pieces,
+                                                           int64_t cols, uint32_t per_row, T* __restrict__ x,
+                                                           int64_t stride, bool nt) {
+    const int64_t base = (int64_t)blockIdx.x * (kBlock * kPieces);
+    const int64_t base_row = base / per_row;
+    const uint32_t base_piece = (uint32_t)(base % per_row);
+    uint32_t w[kPieces], s[kPieces];
 #pragma unroll
-    for (int q = 0; q < kMxBlock; q++) {
-        const int64_t c = b * kMxBlock + q;
-        if (c < cols) x[r * stride + c] = from_float<T>(s * e2m1_value((ws[q / 8] >> (4 * (q % 8))) & 15u));
+    for (int u = 0; u < kPieces; u++) {
+        const int64_t i = base + u * kBlock + threadIdx.x;
+        if (i < pieces) {
+            w[u] = *(const uint32_t*)(codes + 4 * i);
+            s[u] = scales[i / 4];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kPieces; u++) {
+        const uint32_t off = u * kBlock + threadIdx.x;
+        if (base + off >= pieces) continue;
+        const PieceAt p = piece_at(base_row, base_piece, off, per_row);
+        const float f = s[u] == 255 ? __uint_as_float(0x7FC00000u) : exp2_int((int)s[u] - 127);
+        float v[8];
+        from_codes<0>(w[u], f, v);
+        from_codes<1>(w[u], f, v);
+        from_codes<2>(w[u], f, v);
+        from_codes<3>(w[u], f, v);
+        T* row = x + p.row * stride;
+        const int64_t c = (int64_t)p.piece * 8;
+        if (c + 8 <= cols) {
+            Vec<T, 8>::store(row + c, v, nt);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; q++)
+                if (c + q < cols) row[c + q] = from_float<T>(v[q]);
+        }
     }
 }
 
 // ----------------------------------------------------------------- product
 
-// One wave per 16 x 16 tile of out, K in steps of 128.  v_mfma_scale_f32_16x16x128
-// with 4-bit operands: lane l holds 32 consecutive k (one block) of row l % 16
-// of either operand, k = 32 (l / 16), and that block's scale; D[4 (l / 16) + r][l % 16].
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_mx4_product(const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xs,
-                                                        const uint8_t* __restrict__ wc, const uint8_t* __restrict__ ws,
-                                                        int64_t M, int64_t N, int64_t blocks,
-                                                        const float* __restrict__ bias, bool relu,
-                                                        T* __restrict__ out, int64_t stride) {
-    const int lane = lane_id();
-    const int64_t tiles_n = (N + 15) / 16, tile = (int64_t)blockIdx.x * kWavesPerBlock + wave_id();
-    const int64_t m0 = tile / tiles_n * 16, n0 = tile % tiles_n * 16;
-    if (m0 >= M) return;
-    const int64_t m = m0 + (lane & 15), n = n0 + (lane & 15);
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t b0 = 0; b0 < blocks; b0 += 4) {
-        const int64_t b = b0 + (lane >> 4);
-        i32x4 a = {0, 0, 0, 0}, w = {0, 0, 0, 0};
-        int sa = 127, sw = 127;
-        if (b < blocks && m < M) {
-            a = *(const i32x4*)(xc + 16 * (m * blocks + b));
-            sa = xs[m * blocks + b];
-        }
-        if (b < blocks && n < N) {
-            w = *(const i32x4*)(wc + 16 * (n * blocks + b));
-            sw = ws[n * blocks + b];
-        }
-        const i32x8 a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, w8 = {w[0], w[1], w[2], w[3], 0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, w8, acc, 4, 4, 0, sa, 0, sw);
+// v_mfma_scale_f32_16x16x128 with 4-bit operands: lane l holds 32 consecutive k
+// (one block, 16 bytes) of row l % 16 of either operand, k = 32 (l / 16), and
+// that block's scale code in one byte of a register; D[4 (l / 16) + r][l % 16].  The
+// weight goes in first, so a lane holds four adjacent columns of a row of out.
+struct MxArgs {
+    const uint8_t *xc, *xs, *wc, *ws;
+    int64_t M, N;
+    int32_t blocks;                                // per row
+    const float* bias;
+    bool relu, nt;
+    void* out;
+    int64_t stride;
+};
+
+__device__ __forceinline__ i32x8 operand(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
+
+__device__ __forceinline__ float finish(float y, float bias, bool relu) {
+    y += bias;
+    return relu && y < 0.f ? 0.f : y;
+}
+
+template <int N> struct Const { static constexpr int value = N; };
+template <int N, int I = 0, typename F> __device__ __forceinline__ void static_for(F&& f) {
+    if constexpr (I < N) {
+        f(Const<I>{});
+        static_for<N, I + 1>(f);
     }
-    if (n >= N) return;
-    const float bn = bias ? bias[n] : 0.f;
+}
+
+// Sixteen zero bytes: blocks behind the last one of a row.
+static __device__ const uint4 k_mx4_zero = {0u, 0u, 0u, 0u};
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
+// A workgroup of WM x WN waves computes a tile of out, a wave 16 F x 16 G of it,
+// in steps of 256 k: 128 bytes per row, a whole cache line.  The next step's
+// codes go from memory straight to the other half of LDS while this step's are
+// multiplied.  A step's LDS image: row after row, 8 pieces of 16 bytes each,
+// piece p of row r at place p ^ (r % 8): the 16 rows that a wave reads at once
+// then lie in different banks.  Scales pass through registers into the order in
+// which lanes read them: per 128 k and four 16-row tiles one register per lane
+// holds all four tiles' codes, and the MFMA picks its byte.
+constexpr int kStep = 8;                           // blocks per step
+
+// One operand of a workgroup: WAVES waves of F 16-row tiles.
+template <int WAVES, int F> struct MxSide {
+    static constexpr int ROWS = WAVES * 16 * F;
+    static constexpr int GROUPS = (F + 3) / 4;     // registers of scale codes per lane and 128 k
+    static constexpr int CODES = ROWS * 16 * kStep;
+    static constexpr int SCALES = 2 * WAVES * GROUPS * 256;
+};
+
+// One operand's rows of a step, codes straight to LDS.  The rows are `last` + 1
+// from `codes` on; rows behind them repeat the last: they are not stored.
+template <int THREADS, int ROWS>
+__device__ __forceinline__ void fetch_codes(const uint8_t* __restrict__ codes, int last, int blocks, int b0, char* lds) {
+    const int t = threadIdx.x, r = t / 8, piece = (t % 8) ^ (r % 8);
+    const uint32_t row_bytes = (uint32_t)blocks * 16;
+    const uint8_t* const from = codes + (int64_t)b0 * 16;
+    char* const to = lds + t / kWave * kWave * 16;
+    if (b0 + kStep <= blocks) {
 #pragma unroll
-    for (int r = 0; r < 4; r++) {
-        const int64_t row = m0 + 4 * (lane >> 4) + r;
-        if (row >= M) continue;
-        float y = acc[r] + bn;
-        if (relu) y = y < 0.f ? 0.f : y;
-        out[row * stride + n] = from_float<T>(y);
+        for (int i = 0; i < ROWS * 8 / THREADS; i++)
+            __builtin_amdgcn_global_load_lds(
+                (global_void*)(from + ((uint32_t)min(r + i * (THREADS / 8), last) * row_bytes + (uint32_t)piece * 16)),
+                (lds_void*)(to + i * THREADS * 16), 16, 0, 0);
+    } else {                                       // zeros behind a row's last block
+        for (int i = 0; i < ROWS * 8 / THREADS; i++) {
+            const uint8_t* p = from + ((uint32_t)min(r + i * (THREADS / 8), last) * row_bytes + (uint32_t)piece * 16);
+            if (b0 + piece >= blocks) p = (const uint8_t*)&k_mx4_zero;
+            __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(to + i * THREADS * 16), 16, 0, 0);
+        }
+    }
+}
+
+// One row's scale codes of a step: 8 bytes.
+__device__ __forceinline__ uint64_t fetch_scales(const uint8_t* __restrict__ scales, int64_t row, int blocks, int b0) {
+    typedef uint64_t __attribute__((aligned(1))) u64_bytes;
+    const uint8_t* p = scales + row * blocks + b0;
+    if (b0 + kStep <= blocks) return *(const u64_bytes*)p;
+    uint64_t v = 0;
+#pragma unroll
+    for (int b = 0; b < kStep; b++) v |= (uint64_t)(b0 + b < blocks ? p[b] : 127) << (8 * b);
+    return v;
+}
+
+template <int WAVES, int F> __device__ __forceinline__ void put_scales(uint64_t v, int r, char* lds) {
+    const int part = r / (16 * F), tile = r % (16 * F) / 16;
+    char* const at = lds + (part * MxSide<WAVES, F>::GROUPS + tile / 4) * 256 + r % 16 * 4 + tile % 4;
+#pragma unroll
+    for (int b = 0; b < kStep; b++)
+        at[b / 4 * (WAVES * MxSide<WAVES, F>::GROUPS * 256) + b % 4 * 64] = (char)(uint8_t)(v >> (8 * b));
+}
+
+template <typename T, int WM, int WN, int F, int G>
+__global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
+    typedef MxSide<WM, F> X;
+    typedef MxSide<WN, G> W;
+    constexpr int THREADS = kWave * WM * WN;
+    __shared__ __attribute__((aligned(1024))) char even[X::CODES + W::CODES];
+    __shared__ __attribute__((aligned(1024))) char odd[X::CODES + W::CODES];
+    __shared__ __attribute__((aligned(16))) char scales[2][X::SCALES + W::SCALES];
+    const int t = threadIdx.x, lane = lane_id(), wave = wave_id(), wm = wave / WN, wn = wave % WN;
+    // XCD x takes a contiguous run of tiles, in strips of 8 tile rows: the tiles
+    // that run at once on it share rows of both operands in its L2.
+    const int64_t tm = (a.M + X::ROWS - 1) / X::ROWS, tn = (a.N + W::ROWS - 1) / W::ROWS, tiles = tm * tn;
+    const int64_t per = (tiles + kXcds - 1) / kXcds, id = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+    if ((int64_t)blockIdx.x / kXcds >= per || id >= tiles) return;
+    const int64_t strip = id / (8 * tn), high = min((int64_t)8, tm - strip * 8), in = id - strip * 8 * tn;
+    const int64_t m0 = (strip * 8 + in % high) * X::ROWS, n0 = in / high * W::ROWS;
+    const int steps = (a.blocks + kStep - 1) / kStep;
+    const int xlast = (int)min((int64_t)X::ROWS, a.M - m0) - 1, wlast = (int)min((int64_t)W::ROWS, a.N - n0) - 1;
+
+    f32x4 acc[F][G];
+#pragma unroll
+    for (int i = 0; i < F; i++)
+#pragma unroll
+        for (int j = 0; j < G; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int SROWS = X::ROWS + W::ROWS, SPER = (SROWS + THREADS - 1) / THREADS;
+    uint64_t sc[SPER];
+    auto get_scales = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < SPER; i++) {
+            const int r = t + i * THREADS;
+            if (r < X::ROWS) sc[i] = fetch_scales(a.xs, m0 + min(r, xlast), a.blocks, s * kStep);
+            else if (r < SROWS) sc[i] = fetch_scales(a.ws, n0 + min(r - X::ROWS, wlast), a.blocks, s * kStep);
+        }
+    };
+    auto set_scales = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < SPER; i++) {
+            const int r = t + i * THREADS;
+            if (r < X::ROWS) put_scales<WM, F>(sc[i], r, scales[half]);
+            else if (r < SROWS) put_scales<WN, G>(sc[i], r - X::ROWS, scales[half] + X::SCALES);
+        }
+    };
+    const uint8_t* const xc = a.xc + m0 * a.blocks * 16;
+    const uint8_t* const wc = a.wc + n0 * a.blocks * 16;
+    auto fetch = [&](int s, char* lds) {
+        fetch_codes<THREADS, X::ROWS>(xc, xlast, a.blocks, s * kStep, lds);
+        fetch_codes<THREADS, W::ROWS>(wc, wlast, a.blocks, s * kStep, lds + X::CODES);
+    };
+    auto multiply = [&](const char* lds, int half) {
+        const char* const xr = lds + (wm * 16 * F + lane % 16) * (16 * kStep);
+        const char* const wr = lds + X::CODES + (wn * 16 * G + lane % 16) * (16 * kStep);
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int piece = ((k * 4 + lane / 16) ^ (lane % 8)) * 16;
+            i32x4 x[F], w[G];
+            int sx[X::GROUPS], sw[W::GROUPS];
+#pragma unroll
+            for (int i = 0; i < X::GROUPS; i++)
+                sx[i] = *(const int*)(scales[half] + ((k * WM + wm) * X::GROUPS + i) * 256 + lane * 4);
+#pragma unroll
+            for (int j = 0; j < W::GROUPS; j++)
+                sw[j] = *(const int*)(scales[half] + X::SCALES + ((k * WN + wn) * W::GROUPS + j) * 256 + lane * 4);
+#pragma unroll
+            for (int i = 0; i < F; i++) x[i] = *(const i32x4*)(xr + i * (16 * 16 * kStep) + piece);
+#pragma unroll
+            for (int j = 0; j < G; j++) w[j] = *(const i32x4*)(wr + j * (16 * 16 * kStep) + piece);
+            static_for<F>([&](auto ci) {
+                static_for<G>([&](auto cj) {
+                    constexpr int i = decltype(ci)::value, j = decltype(cj)::value;
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w[j]), operand(x[i]), acc[i][j],
+                                                                                4, 4, j % 4, sw[j / 4], i % 4, sx[i / 4]);
+                });
+            });
+        }
+    };
+    if (steps > 0) {
+        fetch(0, even);
+        get_scales(0);
+        set_scales(0);
+    }
+    for (int s = 0; s < steps; s += 2) {
+        __syncthreads();                           // step s has arrived; nobody reads the other half any more
+        if (s + 1 < steps) {
+            fetch(s + 1, odd);
+            get_scales(s + 1);
+        }
+        multiply(even, 0);
+        if (s + 1 >= steps) break;
+        set_scales(1);
+        __syncthreads();
+        if (s + 2 < steps) {
+            fetch(s + 2, even);
+            get_scales(s + 2);
+        }
+        multiply(odd, 1);
+        if (s + 2 < steps) set_scales(0);
+    }
+    // Rows leave through LDS, each wave its own part in strips of 16 rows, as
+    // pieces of 16 bytes along a row: whole lines per store.
+    constexpr int E = 16 / (int)sizeof(T), PITCH = 16 * G + E;
+    constexpr int HALF = WM * WN / 2;
+    static_assert(HALF * 16 * PITCH * sizeof(T) <= sizeof(even), "a strip per wave");
+    __syncthreads();
+    T* const strip_at = (T*)(wave < HALF ? even : odd) + wave % HALF * 16 * PITCH;
+    const int64_t wm0 = m0 + wm * 16 * F, wn0 = n0 + wn * 16 * G;
+    float bias[G][4];
+#pragma unroll
+    for (int j = 0; j < G; j++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int64_t n = wn0 + j * 16 + lane / 16 * 4 + r;
+            bias[j][r] = a.bias && n < a.N ? a.bias[n] : 0.f;
+        }
+#pragma unroll
+    for (int i = 0; i < F; i++) {
+#pragma unroll
+        for (int j = 0; j < G; j++) {
+            float y[4];
+#pragma unroll
+            for (int r = 0; r < 4; r++) y[r] = finish(acc[i][j][r], bias[j][r], a.relu);
+            Vec<T, 4>::store(strip_at + lane % 16 * PITCH + j * 16 + lane / 16 * 4, y);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        constexpr int PER_ROW = 16 * G / E, ROUNDS = (16 * PER_ROW + kWave - 1) / kWave;
+#pragma unroll
+        for (int q = 0; q < ROUNDS; q++) {
+            const int at = q * kWave + lane, row = at / PER_ROW, c = at % PER_ROW * E;
+            const int64_t m = wm0 + i * 16 + row, n = wn0 + c;
+            if (row >= 16 || m >= a.M || n >= a.N) continue;
+            T* to = (T*)a.out + m * a.stride + n;
+            const T* from = strip_at + row * PITCH + c;
+            if (n + E <= a.N) {
+                typedef typename Vec<T, E>::type Piece;
+                const Piece v = *(const Piece*)from;
+                if (a.nt) __builtin_nontemporal_store(v, (Piece*)to);
+                else *(Piece*)to = v;
+            } else {
+                for (int e = 0; n + e < a.N; e++) to[e] = from[e];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -145,12 +427,12 @@ void mx4_quantize(const agnes_matrix* x, const agnes_mx4* q, hipStream_t st) {
     check_matrix(x, false, "x");
     check_mx4(q, "q");
     AGNES_REQUIRE(q->rows == x->rows && q->cols == x->cols, AGNES_ERR_INVALID, "x and q must have equal shapes");
-    const int64_t blocks = mx_blocks(x->cols), n = x->rows * blocks;
-    if (n == 0) return;
+    const int64_t per_row = mx_blocks(x->cols) * 4, pieces = x->rows * per_row;
+    if (pieces == 0) return;
     with_float(x->dtype, [&](auto t) {
         typedef decltype(t) T;
-        AGNES_LAUNCH((k_mx4_quantize<T>), dim3(grid_of(n, kBlock)), dim3(kBlock), 0, st, (const T*)x->data, x->stride,
-                     x->rows, x->cols, blocks, q->codes, q->scales);
+        AGNES_LAUNCH((k_mx4_quantize<T>), dim3(grid_of(pieces, kBlock * kPieces)), dim3(kBlock), 0, st,
+                     (const T*)x->data, x->stride, pieces, x->cols, (uint32_t)per_row, q->codes, q->scales);
     });
 }
 
@@ -158,18 +440,23 @@ void mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, hipStream_t st) {
     check_matrix(x, true, "x");
     check_mx4(q, "q");
     AGNES_REQUIRE(q->rows == x->rows && q->cols == x->cols, AGNES_ERR_INVALID, "x and q must have equal shapes");
-    const int64_t blocks = mx_blocks(x->cols), n = x->rows * blocks;
-    if (n == 0) return;
+    const int64_t per_row = mx_blocks(x->cols) * 4, pieces = x->rows * per_row;
+    if (pieces == 0) return;
     with_float(x->dtype, [&](auto t) {
         typedef decltype(t) T;
-        AGNES_LAUNCH((k_mx4_dequantize<T>), dim3(grid_of(n, kBlock)), dim3(kBlock), 0, st, q->codes, q->scales,
-                     x->rows, x->cols, blocks, (T*)x->data, x->stride);
+        AGNES_LAUNCH((k_mx4_dequantize<T>), dim3(grid_of(pieces, kBlock * kPieces)), dim3(kBlock), 0, st, q->codes,
+                     q->scales, pieces, x->cols, (uint32_t)per_row, (T*)x->data, x->stride,
+                     x->rows * x->cols * (int64_t)sizeof(T) > kStreamBytes);
     });
 }
+
+constexpr int64_t kFullGrid = 256;
 
 static void check_sizes(int64_t M, int64_t N, int64_t K) {
     for (int64_t v : {M, N, K})
         AGNES_REQUIRE(v >= 0 && v < ((int64_t)1 << 31), AGNES_ERR_INVALID, "M, N and K must be in [0, 2^31)");
+    // a tile's rows are addressed with 32 bits
+    AGNES_REQUIRE(K <= ((int64_t)1 << 24), AGNES_ERR_INVALID, "K must be at most 2^24");
 }
 
 uint64_t mx4_product_bytes(int64_t M, int64_t N, int64_t K) {
@@ -185,6 +472,22 @@ uint64_t mx4_linear_bytes(int64_t M, int64_t N, int64_t K) {
     return c.used + mx4_product_bytes(M, N, K);
 }
 
+template <typename T, int WM, int WN, int F, int G> static void launch_tile(const MxArgs& a, hipStream_t st) {
+    constexpr int R = MxSide<WM, F>::ROWS, C = MxSide<WN, G>::ROWS;
+    const int64_t tiles = ((a.M + R - 1) / R) * ((a.N + C - 1) / C);
+    AGNES_REQUIRE(tiles < (1 << 23), AGNES_ERR_RANGE, "the product has too many tiles");
+    const unsigned grid = (unsigned)((tiles + kXcds - 1) / kXcds * kXcds);
+    AGNES_LAUNCH((k_mx4_gemm<T, WM, WN, F, G>), dim3(grid), dim3(kWave * WM * WN), 0, st, a);
+}
+
+// The largest tile that still gives every compute unit one.
+template <typename T> static void launch_gemm(const MxArgs& a, hipStream_t st) {
+    auto tiles = [&](int64_t r) { return ((a.M + r - 1) / r) * ((a.N + r - 1) / r); };
+    if (tiles(256) >= kFullGrid) launch_tile<T, 4, 2, 4, 8>(a, st);
+    else if (tiles(128) >= kFullGrid) launch_tile<T, 2, 2, 4, 4>(a, st);
+    else launch_tile<T, 2, 2, 2, 2>(a, st);
+}
+
 void mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, bool relu, const agnes_matrix* out,
                  void* ws, uint64_t ws_bytes, hipStream_t st) {
     check_mx4(x, "x");
@@ -194,13 +497,13 @@ void mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, bool
     AGNES_REQUIRE(out->rows == x->rows && out->cols == w->rows, AGNES_ERR_INVALID,
                   "out must have x's rows and one column per row of w");
     const int64_t M = x->rows, N = w->rows, blocks = mx_blocks(x->cols);
-    check_workspace(ws, ws_bytes, mx4_product_bytes(M, N, x->cols));
+    check_workspace(ws, ws_bytes, mx4_product_bytes(M, N, x->cols));   // checks the sizes too
     if (M == 0 || N == 0) return;
-    const int64_t tiles = ((M + 15) / 16) * ((N + 15) / 16);
     with_float(out->dtype, [&](auto t) {
         typedef decltype(t) T;
-        AGNES_LAUNCH((k_mx4_product<T>), dim3(grid_of(tiles, kWavesPerBlock)), dim3(kBlock), 0, st, x->codes,
-                     x->scales, w->codes, w->scales, M, N, blocks, bias, relu, (T*)out->data, out->stride);
+        const MxArgs a{x->codes, x->scales, w->codes, w->scales, M, N, (int32_t)blocks, bias, relu,
+                       M * N * (int64_t)sizeof(T) > kStreamBytes, out->data, out->stride};
+        launch_gemm<T>(a, st);
     });
 }
 

@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import collections
 import contextlib
-import ctypes
+import functools
 
 import torch
 
@@ -28,16 +28,26 @@ Mx4.__doc__ = """Rows in microscaled 4-bit floating point: codes uint8 [rows, 16
 even one in the low four bits), scales uint8 [rows, ceil(cols / 32)] (2^(code - 127), 255 = NaN), and the row length."""
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)   # once a CUDA tensor exists
+
+
 def _handle(stream) -> int:
+    """The HIP stream that a call enqueues on (None: the current one)."""
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     return int(getattr(stream, "cuda_stream", stream))
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream, *inputs):
     """A context in which torch allocates for `stream`; records the inputs on it if it is not the current one."""
-    if stream is None or _handle(stream) == torch.cuda.current_stream().cuda_stream:
-        return contextlib.nullcontext()
+    if stream is None or _handle(stream) == _handle(None):
+        return _HERE
     s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
     for t in inputs:
         if t is not None:
@@ -48,9 +58,9 @@ def _on(stream, *inputs):
 def _device(t: torch.Tensor, name: str) -> None:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % name)
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != _current_device():
         raise ValueError("%s is on device %d, the current device is %d"
-                         % (name, t.device.index, torch.cuda.current_device()))
+                         % (name, t.get_device(), _current_device()))
 
 
 def _matrix(t: torch.Tensor, name: str) -> B.agnes_matrix:
@@ -62,9 +72,18 @@ def _matrix(t: torch.Tensor, name: str) -> B.agnes_matrix:
         raise ValueError("%s must be 2-D" % name)
     rows, cols = t.shape
     row_stride, col_stride = t.stride()
-    if cols > 1 and col_stride != 1:
+    if col_stride != 1 and cols > 1:
         raise ValueError("%s must have adjacent columns" % name)
     return B.agnes_matrix(t.data_ptr(), rows, cols, row_stride, code)
+
+
+def _new(like: torch.Tensor, rows: int, cols: int, dtype: torch.dtype):
+    """A new matrix beside `like` and its structure."""
+    t = like.new_empty((rows, cols), dtype=dtype)
+    code = _FLOATS.get(dtype)
+    if code is None:
+        raise TypeError("the result must be float32, float16 or bfloat16")
+    return t, B.agnes_matrix(t.data_ptr(), rows, cols, cols, code)
 
 
 def _rows_of(t: torch.Tensor) -> torch.Tensor:
@@ -80,8 +99,15 @@ def _index(t: torch.Tensor, name: str) -> int:
     return code
 
 
-def _workspace(nbytes: int):
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+# Workspace sizes follow from the sizes alone.
+_grad_bytes = functools.lru_cache(1024)(B.agnes_embedding_grad_bytes)
+_distill_bytes = functools.lru_cache(1024)(B.agnes_distill_bytes)
+_product_bytes = functools.lru_cache(1024)(B.agnes_mx4_product_bytes)
+_linear_bytes = functools.lru_cache(1024)(B.agnes_mx4_linear_bytes)
+
+
+def _workspace(like: torch.Tensor, nbytes: int):
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
 def _ptr(t) -> int | None:
@@ -98,12 +124,15 @@ def embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     m = _matrix(table, "table")
     code = _index(ids, "ids")
     with _on(stream, table, ids, out):
-        flat = ids.contiguous()
+        flat = ids if ids.is_contiguous() else ids.contiguous()
+        n = ids.numel()
         if out is None:
-            out = torch.empty(*ids.shape, m.cols, dtype=dtype or table.dtype, device="cuda")
+            rows, o = _new(table, n, m.cols, dtype or table.dtype)
+            out = rows if ids.dim() == 1 else rows.view(*ids.shape, m.cols)
         elif tuple(out.shape) != (*ids.shape, m.cols) or (dtype is not None and out.dtype != dtype):
             raise ValueError("out must be [*ids.shape, dim] of the type asked for")
-        o = _matrix(out if out.dim() == 2 else out.view(-1, m.cols) if m.cols else out.reshape(flat.numel(), 0), "out")
+        else:
+            o = _matrix(out if out.dim() == 2 else out.view(n, m.cols), "out")
         B.agnes_embedding_lookup(m, flat.data_ptr(), code, scale, o, _handle(stream))
     return out
 
@@ -115,7 +144,7 @@ def _grad_args(grad_out, ids, dim_name="grad_out"):
     if grad_out.dim() != 2:
         grad_out = grad_out.reshape(ids.numel(), grad_out.shape[-1])
     g = _rows_of(grad_out)
-    return g, _matrix(g, dim_name), code, ids.contiguous()
+    return g, _matrix(g, dim_name), code, ids if ids.is_contiguous() else ids.contiguous()
 
 
 def embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, num_rows: int, scale: float = 1.0,
@@ -128,12 +157,15 @@ def embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, num_rows: int, sca
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs out")
-            out = torch.empty(num_rows, g.cols, dtype=dtype or grad_out.dtype, device="cuda")
+            out, o = _new(keep, num_rows, g.cols, dtype or grad_out.dtype)
         elif tuple(out.shape) != (num_rows, g.cols) or (dtype is not None and out.dtype != dtype):
             raise ValueError("out must be [num_rows, dim] of the type asked for")
-        ws = _workspace(B.agnes_embedding_grad_bytes(g.rows, num_rows, g.cols))
-        B.agnes_embedding_grad(g, flat.data_ptr(), code, scale, 1 if accumulate else 0, _matrix(out, "out"),
-                               _ptr(ws), 0 if ws is None else ws.numel(), _handle(stream))
+        else:
+            o = _matrix(out, "out")
+        need = _grad_bytes(g.rows, num_rows, g.cols)
+        ws = _workspace(keep, need)
+        B.agnes_embedding_grad(g, flat.data_ptr(), code, scale, 1 if accumulate else 0, o, _ptr(ws), need,
+                               _handle(stream))
     return out
 
 
@@ -149,13 +181,13 @@ def embedding_grad_rows(grad_out: torch.Tensor, ids: torch.Tensor, num_rows: int
         max_rows = min(ids.numel(), num_rows)
     with _on(stream, grad_out, ids):
         keep, g, code, flat = _grad_args(grad_out, ids)
-        row_ids = torch.empty(max_rows, dtype=torch.int32, device="cuda")
-        rows = torch.empty(max_rows, g.cols, dtype=dtype or grad_out.dtype, device="cuda")
-        count = torch.empty(1, dtype=torch.int64, device="cuda")
-        ws = _workspace(B.agnes_embedding_grad_bytes(g.rows, num_rows, g.cols))
-        B.agnes_embedding_grad_rows(g, flat.data_ptr(), code, scale, num_rows, row_ids.data_ptr(),
-                                    _matrix(rows, "rows"), count.data_ptr(), _ptr(ws),
-                                    0 if ws is None else ws.numel(), _handle(stream))
+        row_ids = keep.new_empty(max_rows, dtype=torch.int32)
+        rows, o = _new(keep, max_rows, g.cols, dtype or grad_out.dtype)
+        count = keep.new_empty(1, dtype=torch.int64)
+        need = _grad_bytes(g.rows, num_rows, g.cols)
+        ws = _workspace(keep, need)
+        B.agnes_embedding_grad_rows(g, flat.data_ptr(), code, scale, num_rows, row_ids.data_ptr(), o,
+                                    count.data_ptr(), _ptr(ws), need, _handle(stream))
     return row_ids, rows, count
 
 
@@ -186,20 +218,21 @@ def distill_loss(logits, teacher, classes, labels=None, weight=None, temperature
     [rows], stats float32 [rows, 3]); distill_grad takes the statistics."""
     d = _distill(logits, teacher, classes, labels, weight, temperature, soft, hard)
     with _on(stream, logits, teacher, classes, labels, weight):
-        loss = torch.empty(d.logits.rows, dtype=torch.float32, device="cuda")
-        stats = torch.empty(d.logits.rows, 3, dtype=torch.float32, device="cuda")
-        ws = _workspace(B.agnes_distill_bytes(d.logits.rows, d.logits.cols))
-        B.agnes_distill_loss(d, loss.data_ptr(), stats.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
-                             _handle(stream))
+        rows = d.logits.rows
+        loss = logits.new_empty(rows, dtype=torch.float32)
+        stats = logits.new_empty((rows, 3), dtype=torch.float32)
+        need = _distill_bytes(rows, d.logits.cols)
+        ws = _workspace(logits, need)
+        B.agnes_distill_loss(d, loss.data_ptr(), stats.data_ptr(), _ptr(ws), need, _handle(stream))
     return loss, stats
 
 
 def _grad_like(logits, out):
     if out is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device="cuda")
+        return _new(logits, logits.shape[0], logits.shape[1], logits.dtype)
     if out.shape != logits.shape:
         raise ValueError("out must have the logits' shape")
-    return out
+    return out, _matrix(out, "out")
 
 
 def distill_grad(logits, teacher, classes, stats, labels=None, weight=None, temperature: float = 1.0,
@@ -212,8 +245,8 @@ def distill_grad(logits, teacher, classes, stats, labels=None, weight=None, temp
     if stats.dtype != torch.float32 or tuple(stats.shape) != (d.logits.rows, 3) or not stats.is_contiguous():
         raise ValueError("stats must be distill_loss's statistics, contiguous float32 [rows, 3]")
     with _on(stream, logits, teacher, classes, stats, labels, weight, out):
-        out = _grad_like(logits, out)
-        B.agnes_distill_grad(d, stats.data_ptr(), _matrix(out, "out"), _handle(stream))
+        out, o = _grad_like(logits, out)
+        B.agnes_distill_grad(d, stats.data_ptr(), o, _handle(stream))
     return out
 
 
@@ -223,27 +256,28 @@ def distill_loss_grad(logits, teacher, classes, labels=None, weight=None, temper
     the logits (agnes_distill_loss_grad).  out may be the logits themselves."""
     d = _distill(logits, teacher, classes, labels, weight, temperature, soft, hard)
     with _on(stream, logits, teacher, classes, labels, weight, out):
-        out = _grad_like(logits, out)
-        loss = torch.empty(d.logits.rows, dtype=torch.float32, device="cuda")
-        ws = _workspace(B.agnes_distill_bytes(d.logits.rows, d.logits.cols))
-        B.agnes_distill_loss_grad(d, loss.data_ptr(), _matrix(out, "out"), _ptr(ws),
-                                  0 if ws is None else ws.numel(), _handle(stream))
+        out, o = _grad_like(logits, out)
+        loss = logits.new_empty(d.logits.rows, dtype=torch.float32)
+        need = _distill_bytes(d.logits.rows, d.logits.cols)
+        ws = _workspace(logits, need)
+        B.agnes_distill_loss_grad(d, loss.data_ptr(), o, _ptr(ws), need, _handle(stream))
     return loss, out
 
 
 # ----------------------------------------------------------------- 4-bit rows
 
 def _mx4(q: Mx4, name: str) -> B.agnes_mx4:
-    blocks = -(-q.cols // 32)
-    _device(q.codes, name + ".codes")
-    _device(q.scales, name + ".scales")
-    rows = q.codes.shape[0]
-    if q.codes.dtype != torch.uint8 or q.scales.dtype != torch.uint8 or \
-            tuple(q.codes.shape) != (rows, 16 * blocks) or tuple(q.scales.shape) != (rows, blocks) or \
-            not (q.codes.is_contiguous() and q.scales.is_contiguous()):
+    codes, scales, cols = q
+    blocks = -(-cols // 32)
+    _device(codes, name + ".codes")
+    _device(scales, name + ".scales")
+    rows = codes.shape[0]
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or \
+            tuple(codes.shape) != (rows, 16 * blocks) or tuple(scales.shape) != (rows, blocks) or \
+            not (codes.is_contiguous() and scales.is_contiguous()):
         raise ValueError("%s must be contiguous uint8 codes [rows, 16 ceil(cols / 32)] and scales "
                          "[rows, ceil(cols / 32)]" % name)
-    return B.agnes_mx4(q.codes.data_ptr(), q.scales.data_ptr(), rows, q.cols)
+    return B.agnes_mx4(codes.data_ptr(), scales.data_ptr(), rows, cols)
 
 
 def mx4_quantize(x: torch.Tensor, stream=None) -> Mx4:
@@ -251,9 +285,10 @@ def mx4_quantize(x: torch.Tensor, stream=None) -> Mx4:
     m = _matrix(x, "x")
     blocks = -(-m.cols // 32)
     with _on(stream, x):
-        q = Mx4(torch.empty(m.rows, 16 * blocks, dtype=torch.uint8, device="cuda"),
-                torch.empty(m.rows, blocks, dtype=torch.uint8, device="cuda"), m.cols)
-        B.agnes_mx4_quantize(m, _mx4(q, "q"), _handle(stream))
+        q = Mx4(x.new_empty((m.rows, 16 * blocks), dtype=torch.uint8),
+                x.new_empty((m.rows, blocks), dtype=torch.uint8), m.cols)
+        d = B.agnes_mx4(q.codes.data_ptr(), q.scales.data_ptr(), m.rows, m.cols)
+        B.agnes_mx4_quantize(m, d, _handle(stream))
     return q
 
 
@@ -261,8 +296,8 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.float32, stream=None) -> t
     """The values [R, K] that 4-bit rows stand for (agnes_mx4_dequantize)."""
     d = _mx4(q, "q")
     with _on(stream, q.codes, q.scales):
-        x = torch.empty(d.rows, d.cols, dtype=dtype, device="cuda")
-        B.agnes_mx4_dequantize(d, _matrix(x, "x"), _handle(stream))
+        x, m = _new(q.codes, d.rows, d.cols, dtype)
+        B.agnes_mx4_dequantize(d, m, _handle(stream))
     return x
 
 
@@ -280,12 +315,13 @@ def mx4_linear(x, weight: Mx4, bias: torch.Tensor | None = None, relu: bool = Fa
             raise ValueError("bias must be contiguous float32 [N]")
     with _on(stream, *((x.codes, x.scales) if given else (x,)), weight.codes, weight.scales, bias, out):
         if out is None:
-            out = torch.empty(a.rows, w.rows, dtype=dtype or (torch.float32 if given else x.dtype), device="cuda")
+            out, o = _new(weight.codes, a.rows, w.rows, dtype or (torch.float32 if given else x.dtype))
         elif tuple(out.shape) != (a.rows, w.rows) or (dtype is not None and out.dtype != dtype):
             raise ValueError("out must be [M, N] of the type asked for")
-        o = _matrix(out, "out")
-        size, call = (B.agnes_mx4_product_bytes, B.agnes_mx4_product) if given else \
-            (B.agnes_mx4_linear_bytes, B.agnes_mx4_linear)
-        ws = _workspace(size(a.rows, w.rows, a.cols))
-        call(a, w, _ptr(bias), 1 if relu else 0, o, _ptr(ws), 0 if ws is None else ws.numel(), _handle(stream))
+        else:
+            o = _matrix(out, "out")
+        size, call = (_product_bytes, B.agnes_mx4_product) if given else (_linear_bytes, B.agnes_mx4_linear)
+        need = size(a.rows, w.rows, a.cols)
+        ws = _workspace(weight.codes, need)
+        call(a, w, _ptr(bias), 1 if relu else 0, o, _ptr(ws), need, _handle(stream))
     return out
