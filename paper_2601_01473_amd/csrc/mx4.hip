@@ -184,7 +184,7 @@ __device__ __forceinline__ float finish(float y, float bias, bool relu) {
     return relu && y < 0.f ? 0.f : y;
 }
 
-template <int N> struct Const { static constexpr int value = N; };
+template <auto N> struct Const { static constexpr auto value = N; };
 template <int N, int I = 0, typename F> __device__ __forceinline__ void static_for(F&& f) {
     if constexpr (I < N) {
         f(Const<I>{});
@@ -218,44 +218,34 @@ template <int WAVES, int F> struct MxSide {
 
 // One operand's rows of a step, codes straight to LDS.  The rows are `last` + 1
 // from `codes` on; rows behind them repeat the last: they are not stored.
-template <int THREADS, int ROWS>
+// TAIL: the step is a row's last and partial; zeros behind its end.
+template <bool TAIL, int THREADS, int ROWS>
 __device__ __forceinline__ void fetch_codes(const uint8_t* __restrict__ codes, int last, int blocks, int b0, char* lds) {
     const int t = threadIdx.x, r = t / 8, piece = (t % 8) ^ (r % 8);
     const uint32_t row_bytes = (uint32_t)blocks * 16;
     const uint8_t* const from = codes + (int64_t)b0 * 16;
     char* const to = lds + t / kWave * kWave * 16;
-    if (b0 + kStep <= blocks) {
 #pragma unroll
-        for (int i = 0; i < ROWS * 8 / THREADS; i++)
-            __builtin_amdgcn_global_load_lds(
-                (global_void*)(from + ((uint32_t)min(r + i * (THREADS / 8), last) * row_bytes + (uint32_t)piece * 16)),
-                (lds_void*)(to + i * THREADS * 16), 16, 0, 0);
-    } else {                                       // zeros behind a row's last block
-        for (int i = 0; i < ROWS * 8 / THREADS; i++) {
-            const uint8_t* p = from + ((uint32_t)min(r + i * (THREADS / 8), last) * row_bytes + (uint32_t)piece * 16);
-            if (b0 + piece >= blocks) p = (const uint8_t*)&k_mx4_zero;
-            __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(to + i * THREADS * 16), 16, 0, 0);
-        }
+    for (int i = 0; i < ROWS * 8 / THREADS; i++) {
+        const uint8_t* p = from + ((uint32_t)min(r + i * (THREADS / 8), last) * row_bytes + (uint32_t)piece * 16);
+        if (TAIL && b0 + piece >= blocks) p = (const uint8_t*)&k_mx4_zero;
+        __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(to + i * THREADS * 16), 16, 0, 0);
     }
 }
 
-// One row's scale codes of a step: 8 bytes.
-__device__ __forceinline__ uint64_t fetch_scales(const uint8_t* __restrict__ scales, int64_t row, int blocks, int b0) {
+// A row's scale codes of a step: 8 bytes; 1 behind its end, where codes are 0.
+template <bool TAIL> __device__ __forceinline__ uint64_t fetch_scales(const uint8_t* __restrict__ row, int blocks, int b0) {
     typedef uint64_t __attribute__((aligned(1))) u64_bytes;
-    const uint8_t* p = scales + row * blocks + b0;
-    if (b0 + kStep <= blocks) return *(const u64_bytes*)p;
+    if (!TAIL) return *(const u64_bytes*)(row + b0);
     uint64_t v = 0;
-#pragma unroll
-    for (int b = 0; b < kStep; b++) v |= (uint64_t)(b0 + b < blocks ? p[b] : 127) << (8 * b);
+    for (int b = 0; b < kStep; b++) v |= (uint64_t)(b0 + b < blocks ? row[b0 + b] : 127) << (8 * b);
     return v;
 }
 
-template <int WAVES, int F> __device__ __forceinline__ void put_scales(uint64_t v, int r, char* lds) {
+// Where row r's codes go: block b of a step at + b / 4 * half + b % 4 * 64.
+template <int WAVES, int F> __device__ __forceinline__ int scale_place(int r) {
     const int part = r / (16 * F), tile = r % (16 * F) / 16;
-    char* const at = lds + (part * MxSide<WAVES, F>::GROUPS + tile / 4) * 256 + r % 16 * 4 + tile % 4;
-#pragma unroll
-    for (int b = 0; b < kStep; b++)
-        at[b / 4 * (WAVES * MxSide<WAVES, F>::GROUPS * 256) + b % 4 * 64] = (char)(uint8_t)(v >> (8 * b));
+    return (part * MxSide<WAVES, F>::GROUPS + tile / 4) * 256 + r % 16 * 4 + tile % 4;
 }
 
 template <typename T, int WM, int WN, int F, int G>
@@ -274,7 +264,6 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
     if ((int64_t)blockIdx.x / kXcds >= per || id >= tiles) return;
     const int64_t strip = id / (8 * tn), high = min((int64_t)8, tm - strip * 8), in = id - strip * 8 * tn;
     const int64_t m0 = (strip * 8 + in % high) * X::ROWS, n0 = in / high * W::ROWS;
-    const int steps = (a.blocks + kStep - 1) / kStep;
     const int xlast = (int)min((int64_t)X::ROWS, a.M - m0) - 1, wlast = (int)min((int64_t)W::ROWS, a.N - n0) - 1;
 
     f32x4 acc[F][G];
@@ -283,29 +272,29 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
 #pragma unroll
         for (int j = 0; j < G; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int SROWS = X::ROWS + W::ROWS, SPER = (SROWS + THREADS - 1) / THREADS;
-    uint64_t sc[SPER];
-    auto get_scales = [&](int s) {
+    // Thread t carries the scale codes of row t of both operands, the first's rows
+    // first (threads behind them repeat them: a branch here would keep the
+    // compiler from ordering the multiplications among the loads).
+    constexpr int SROWS = X::ROWS + W::ROWS;
+    static_assert(SROWS <= THREADS, "a thread per row");
+    const int sr = t % SROWS;
+    const bool of_x = sr < X::ROWS;
+    const uint8_t* const srow = of_x ? a.xs + (m0 + min(sr, xlast)) * a.blocks
+                                     : a.ws + (n0 + min(sr - X::ROWS, wlast)) * a.blocks;
+    char* const splace = &scales[0][0] + (of_x ? scale_place<WM, F>(sr) : X::SCALES + scale_place<WN, G>(sr - X::ROWS));
+    const int shalf = of_x ? WM * X::GROUPS * 256 : WN * W::GROUPS * 256;
+    auto put_scales = [&](uint64_t v, int half) {
 #pragma unroll
-        for (int i = 0; i < SPER; i++) {
-            const int r = t + i * THREADS;
-            if (r < X::ROWS) sc[i] = fetch_scales(a.xs, m0 + min(r, xlast), a.blocks, s * kStep);
-            else if (r < SROWS) sc[i] = fetch_scales(a.ws, n0 + min(r - X::ROWS, wlast), a.blocks, s * kStep);
-        }
-    };
-    auto set_scales = [&](int half) {
-#pragma unroll
-        for (int i = 0; i < SPER; i++) {
-            const int r = t + i * THREADS;
-            if (r < X::ROWS) put_scales<WM, F>(sc[i], r, scales[half]);
-            else if (r < SROWS) put_scales<WN, G>(sc[i], r - X::ROWS, scales[half] + X::SCALES);
-        }
+        for (int b = 0; b < kStep; b++)
+            splace[half * (X::SCALES + W::SCALES) + b / 4 * shalf + b % 4 * 64] = (char)(uint8_t)(v >> (8 * b));
     };
     const uint8_t* const xc = a.xc + m0 * a.blocks * 16;
     const uint8_t* const wc = a.wc + n0 * a.blocks * 16;
-    auto fetch = [&](int s, char* lds) {
-        fetch_codes<THREADS, X::ROWS>(xc, xlast, a.blocks, s * kStep, lds);
-        fetch_codes<THREADS, W::ROWS>(wc, wlast, a.blocks, s * kStep, lds + X::CODES);
+    auto fetch = [&](auto tail, int s, char* lds) {
+        constexpr bool TAIL = decltype(tail)::value;
+        fetch_codes<TAIL, THREADS, X::ROWS>(xc, xlast, a.blocks, s * kStep, lds);
+        fetch_codes<TAIL, THREADS, W::ROWS>(wc, wlast, a.blocks, s * kStep, lds + X::CODES);
+        return fetch_scales<TAIL>(srow, a.blocks, s * kStep);
     };
     auto multiply = [&](const char* lds, int half) {
         const char* const xr = lds + (wm * 16 * F + lane % 16) * (16 * kStep);
@@ -332,29 +321,30 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
                                                                                 4, 4, j % 4, sw[j / 4], i % 4, sx[i / 4]);
                 });
             });
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    if (steps > 0) {
-        fetch(0, even);
-        get_scales(0);
-        set_scales(0);
-    }
-    for (int s = 0; s < steps; s += 2) {
-        __syncthreads();                           // step s has arrived; nobody reads the other half any more
-        if (s + 1 < steps) {
-            fetch(s + 1, odd);
-            get_scales(s + 1);
-        }
+    // Whole steps, two at a time, one for each half of LDS; behind the last one it
+    // is fetched again, into memory that nobody reads any more.
+    const int whole = a.blocks / kStep;
+    if (whole > 0) put_scales(fetch(Const<false>{}, 0, even), 0);
+    int s = 0;
+    for (; s + 1 < whole; s += 2) {
+        __syncthreads();                           // step s has arrived; nobody reads the other half
+        uint64_t sc = fetch(Const<false>{}, s + 1, odd);
         multiply(even, 0);
-        if (s + 1 >= steps) break;
-        set_scales(1);
+        put_scales(sc, 1);
         __syncthreads();
-        if (s + 2 < steps) {
-            fetch(s + 2, even);
-            get_scales(s + 2);
-        }
+        sc = fetch(Const<false>{}, min(s + 2, whole - 1), even);
         multiply(odd, 1);
-        if (s + 2 < steps) set_scales(0);
+        put_scales(sc, 0);
+    }
+    __syncthreads();
+    if (s < whole) multiply(even, 0);
+    if (whole * kStep < a.blocks) {
+        put_scales(fetch(Const<true>{}, whole, odd), 1);
+        __syncthreads();
+        multiply(odd, 1);
     }
     // Rows leave through LDS, each wave its own part in strips of 16 rows, as
     // pieces of 16 bytes along a row: whole lines per store.
