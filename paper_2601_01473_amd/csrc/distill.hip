@@ -279,13 +279,6 @@ __device__ __forceinline__ float grad_named(const DistillArgs& a, const Terms& q
     return x;
 }
 
-// Orders the lanes' LDS accesses within their wave.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // The total probability of class c: of all entries that list it, in their order.
 __device__ __forceinline__ float listed(const int32_t* cls, const float* prob, int k, int32_t c) {
     float p = 0.f;

@@ -253,8 +253,10 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
     typedef MxSide<WM, F> X;
     typedef MxSide<WN, G> W;
     constexpr int THREADS = kWave * WM * WN;
-    __shared__ __attribute__((aligned(1024))) char even[X::CODES + W::CODES];
-    __shared__ __attribute__((aligned(1024))) char odd[X::CODES + W::CODES];
+    // An object per operand and half, addressed with one offset: that way the
+    // compiler sees that a fetch under way does not write what is being read, and
+    // adds no wait of its own for it.
+    __shared__ __attribute__((aligned(1024))) char x0[X::CODES], x1[X::CODES], w0[W::CODES], w1[W::CODES];
     __shared__ __attribute__((aligned(16))) char scales[2][X::SCALES + W::SCALES];
     const int t = threadIdx.x, lane = lane_id(), wave = wave_id(), wm = wave / WN, wn = wave % WN;
     // XCD x takes a contiguous run of tiles, in strips of 8 tile rows: the tiles
@@ -272,87 +274,122 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
 #pragma unroll
         for (int j = 0; j < G; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // Thread t carries the scale codes of row t of both operands, the first's rows
+    // A thread carries the scale codes of row t of both operands, the first's rows
     // first (threads behind them repeat them: a branch here would keep the
-    // compiler from ordering the multiplications among the loads).
-    constexpr int SROWS = X::ROWS + W::ROWS;
-    static_assert(SROWS <= THREADS, "a thread per row");
-    const int sr = t % SROWS;
-    const bool of_x = sr < X::ROWS;
-    const uint8_t* const srow = of_x ? a.xs + (m0 + min(sr, xlast)) * a.blocks
-                                     : a.ws + (n0 + min(sr - X::ROWS, wlast)) * a.blocks;
-    char* const splace = &scales[0][0] + (of_x ? scale_place<WM, F>(sr) : X::SCALES + scale_place<WN, G>(sr - X::ROWS));
-    const int shalf = of_x ? WM * X::GROUPS * 256 : WN * W::GROUPS * 256;
-    auto put_scales = [&](uint64_t v, int half) {
+    // compiler from ordering the multiplications among the loads), or of two rows.
+    constexpr int SROWS = X::ROWS + W::ROWS, PER = (SROWS + THREADS - 1) / THREADS;
+    static_assert(SROWS % THREADS == 0 || SROWS < THREADS, "the same rows per thread");
+    struct Codes {
+        uint64_t row[PER];
+    };
+    const uint8_t* srow[PER];
+    char* splace[PER];
+    int shalf[PER];
 #pragma unroll
-        for (int b = 0; b < kStep; b++)
-            splace[half * (X::SCALES + W::SCALES) + b / 4 * shalf + b % 4 * 64] = (char)(uint8_t)(v >> (8 * b));
+    for (int i = 0; i < PER; i++) {
+        const int r = (t + i * THREADS) % SROWS;
+        const bool of_x = r < X::ROWS;
+        srow[i] = of_x ? a.xs + (m0 + min(r, xlast)) * a.blocks : a.ws + (n0 + min(r - X::ROWS, wlast)) * a.blocks;
+        splace[i] = &scales[0][0] + (of_x ? scale_place<WM, F>(r) : X::SCALES + scale_place<WN, G>(r - X::ROWS));
+        shalf[i] = of_x ? WM * X::GROUPS * 256 : WN * W::GROUPS * 256;
+    }
+    auto put_scales = [&](const Codes& v, int half) {
+#pragma unroll
+        for (int i = 0; i < PER; i++)
+#pragma unroll
+            for (int b = 0; b < kStep; b++)
+                splace[i][half * (X::SCALES + W::SCALES) + b / 4 * shalf[i] + b % 4 * 64] =
+                    (char)(uint8_t)(v.row[i] >> (8 * b));
     };
     const uint8_t* const xc = a.xc + m0 * a.blocks * 16;
     const uint8_t* const wc = a.wc + n0 * a.blocks * 16;
-    auto fetch = [&](auto tail, int s, char* lds) {
-        constexpr bool TAIL = decltype(tail)::value;
-        fetch_codes<TAIL, THREADS, X::ROWS>(xc, xlast, a.blocks, s * kStep, lds);
-        fetch_codes<TAIL, THREADS, W::ROWS>(wc, wlast, a.blocks, s * kStep, lds + X::CODES);
-        return fetch_scales<TAIL>(srow, a.blocks, s * kStep);
+    auto fetch = [&](auto tail, int s, auto half) {
+        constexpr bool TAIL = decltype(tail)::value, ODD = decltype(half)::value != 0;
+        fetch_codes<TAIL, THREADS, X::ROWS>(xc, xlast, a.blocks, s * kStep, ODD ? x1 : x0);
+        fetch_codes<TAIL, THREADS, W::ROWS>(wc, wlast, a.blocks, s * kStep, ODD ? w1 : w0);
+        Codes v;
+#pragma unroll
+        for (int i = 0; i < PER; i++) v.row[i] = fetch_scales<TAIL>(srow[i], a.blocks, s * kStep);
+        __builtin_amdgcn_sched_barrier(0);         // on their way before the multiplications begin
+        return v;
     };
-    auto multiply = [&](const char* lds, int half) {
-        const char* const xr = lds + (wm * 16 * F + lane % 16) * (16 * kStep);
-        const char* const wr = lds + X::CODES + (wn * 16 * G + lane % 16) * (16 * kStep);
+    // A step is 2 G columns of F multiplications: the weight's 16 rows j, 128 k.
+    // Operands are read kEarly columns ahead, so that LDS answers while the
+    // matrix cores are busy; the barriers keep the compiler from gathering the reads.
+    constexpr int EARLY = 3;
+    auto multiply = [&](auto half) {
+        constexpr bool ODD = decltype(half)::value != 0;
+        const char* const sbase = scales[ODD];
+        const int xr = (wm * 16 * F + lane % 16) * (16 * kStep), wr = (wn * 16 * G + lane % 16) * (16 * kStep);
+        const int piece[2] = {(lane / 16 ^ lane % 8) * 16, ((4 + lane / 16) ^ lane % 8) * 16};
+        i32x4 x[2][F], w[2 * G];
+        int sx[2][X::GROUPS], sw[2][W::GROUPS];
+        auto read_x = [&](auto k, auto i) {
+            constexpr int K = decltype(k)::value, I = decltype(i)::value;
+            x[K][I] = *(const i32x4*)((ODD ? x1 : x0) + (xr + I * (16 * 16 * kStep) + piece[K]));
+        };
+        auto read_w = [&](auto c) {
+            constexpr int C = decltype(c)::value;
+            w[C] = *(const i32x4*)((ODD ? w1 : w0) + (wr + C % G * (16 * 16 * kStep) + piece[C / G]));
+        };
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-            const int piece = ((k * 4 + lane / 16) ^ (lane % 8)) * 16;
-            i32x4 x[F], w[G];
-            int sx[X::GROUPS], sw[W::GROUPS];
 #pragma unroll
             for (int i = 0; i < X::GROUPS; i++)
-                sx[i] = *(const int*)(scales[half] + ((k * WM + wm) * X::GROUPS + i) * 256 + lane * 4);
+                sx[k][i] = *(const int*)(sbase + ((k * WM + wm) * X::GROUPS + i) * 256 + lane * 4);
 #pragma unroll
             for (int j = 0; j < W::GROUPS; j++)
-                sw[j] = *(const int*)(scales[half] + X::SCALES + ((k * WN + wn) * W::GROUPS + j) * 256 + lane * 4);
-#pragma unroll
-            for (int i = 0; i < F; i++) x[i] = *(const i32x4*)(xr + i * (16 * 16 * kStep) + piece);
-#pragma unroll
-            for (int j = 0; j < G; j++) w[j] = *(const i32x4*)(wr + j * (16 * 16 * kStep) + piece);
-            static_for<F>([&](auto ci) {
-                static_for<G>([&](auto cj) {
-                    constexpr int i = decltype(ci)::value, j = decltype(cj)::value;
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w[j]), operand(x[i]), acc[i][j],
-                                                                                4, 4, j % 4, sw[j / 4], i % 4, sx[i / 4]);
+                sw[k][j] = *(const int*)(sbase + X::SCALES + ((k * WN + wn) * W::GROUPS + j) * 256 + lane * 4);
+        }
+        static_for<F>([&](auto i) { read_x(Const<0>{}, i); });
+        static_for<EARLY>([&](auto c) { read_w(c); });
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<2 * G>([&](auto c) {
+            constexpr int C = decltype(c)::value, K = C / G, J = C % G;
+            if constexpr (C + EARLY < 2 * G) read_w(Const<C + EARLY>{});
+            // the second half's rows of x, spread over the first half's last columns
+            if constexpr (C < G)
+                static_for<F>([&](auto i) {
+                    if constexpr (decltype(i)::value * G / F / 2 + G / 2 == C) read_x(Const<1>{}, i);
                 });
+            static_for<F>([&](auto ci) {
+                constexpr int I = decltype(ci)::value;
+                acc[I][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w[C]), operand(x[K][I]), acc[I][J], 4, 4,
+                                                                            J % 4, sw[K][J / 4], I % 4, sx[K][I / 4]);
             });
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     };
     // Whole steps, two at a time, one for each half of LDS; behind the last one it
     // is fetched again, into memory that nobody reads any more.
     const int whole = a.blocks / kStep;
-    if (whole > 0) put_scales(fetch(Const<false>{}, 0, even), 0);
+    if (whole > 0) put_scales(fetch(Const<false>{}, 0, Const<0>{}), 0);
     int s = 0;
     for (; s + 1 < whole; s += 2) {
         __syncthreads();                           // step s has arrived; nobody reads the other half
-        uint64_t sc = fetch(Const<false>{}, s + 1, odd);
-        multiply(even, 0);
+        Codes sc = fetch(Const<false>{}, s + 1, Const<1>{});
+        multiply(Const<0>{});
         put_scales(sc, 1);
         __syncthreads();
-        sc = fetch(Const<false>{}, min(s + 2, whole - 1), even);
-        multiply(odd, 1);
+        sc = fetch(Const<false>{}, min(s + 2, whole - 1), Const<0>{});
+        multiply(Const<1>{});
         put_scales(sc, 0);
     }
     __syncthreads();
-    if (s < whole) multiply(even, 0);
+    if (s < whole) multiply(Const<0>{});
     if (whole * kStep < a.blocks) {
-        put_scales(fetch(Const<true>{}, whole, odd), 1);
+        put_scales(fetch(Const<true>{}, whole, Const<1>{}), 1);
         __syncthreads();
-        multiply(odd, 1);
+        multiply(Const<1>{});
     }
     // Rows leave through LDS, each wave its own part in strips of 16 rows, as
     // pieces of 16 bytes along a row: whole lines per store.
     constexpr int E = 16 / (int)sizeof(T), PITCH = 16 * G + E;
-    constexpr int HALF = WM * WN / 2;
-    static_assert(HALF * 16 * PITCH * sizeof(T) <= sizeof(even), "a strip per wave");
+    constexpr int SHARE = (WM * WN + 3) / 4;       // waves per LDS object
+    static_assert(SHARE * 16 * PITCH * sizeof(T) <= X::CODES && X::CODES == W::CODES, "a strip per wave");
     __syncthreads();
-    T* const strip_at = (T*)(wave < HALF ? even : odd) + wave % HALF * 16 * PITCH;
+    char* const part = wave / SHARE < 2 ? (wave / SHARE == 0 ? x0 : x1) : (wave / SHARE == 2 ? w0 : w1);
+    T* const strip_at = (T*)part + wave % SHARE * 16 * PITCH;
     const int64_t wm0 = m0 + wm * 16 * F, wn0 = n0 + wn * 16 * G;
     float bias[G][4];
 #pragma unroll
@@ -473,7 +510,7 @@ template <typename T, int WM, int WN, int F, int G> static void launch_tile(cons
 // The largest tile that still gives every compute unit one.
 template <typename T> static void launch_gemm(const MxArgs& a, hipStream_t st) {
     auto tiles = [&](int64_t r) { return ((a.M + r - 1) / r) * ((a.N + r - 1) / r); };
-    if (tiles(256) >= kFullGrid) launch_tile<T, 4, 2, 4, 8>(a, st);
+    if (tiles(256) >= kFullGrid) launch_tile<T, 2, 4, 8, 4>(a, st);
     else if (tiles(128) >= kFullGrid) launch_tile<T, 2, 2, 4, 4>(a, st);
     else launch_tile<T, 2, 2, 2, 2>(a, st);
 }

@@ -73,6 +73,13 @@ __device__ __forceinline__ float lanes_sum(float x, int L) {
     return lanes_reduce(x, L, [](float a, float b) { return a + b; });
 }
 
+// Orders the lanes' LDS accesses within their wave.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ----------------------------------------------------------------- host side
 
 inline size_t elem_size(agnes_dtype t) { return t == AGNES_FLOAT32 ? 4 : 2; }
