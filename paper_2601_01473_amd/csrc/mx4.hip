@@ -5,6 +5,7 @@
 // A block's scale is 2^(floor(log2 max|x|) - 2): the largest element lands in
 // [4, 8), and 2^2 is the largest power of two that the 4-bit format holds.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.hpp"
 
@@ -175,6 +176,7 @@ struct MxArgs {
     bool relu, nt;
     void* out;
     int64_t stride;
+    float* parts;                                  // [gridDim.y][M][N]: sums over parts of K instead of out, or NULL
 };
 
 __device__ __forceinline__ i32x8 operand(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
         return v;
     };
     // A step is 2 G columns of F multiplications: the weight's 16 rows j, 128 k.
-    // Operands are read kEarly columns ahead, so that LDS answers while the
+    // Operands are read EARLY columns ahead, so that LDS answers while the
     // matrix cores are busy; the barriers keep the compiler from gathering the reads.
     constexpr int EARLY = 3;
     auto multiply = [&](auto half) {
@@ -360,25 +362,26 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    // Whole steps, two at a time, one for each half of LDS; behind the last one it
-    // is fetched again, into memory that nobody reads any more.
-    const int whole = a.blocks / kStep;
-    if (whole > 0) put_scales(fetch(Const<false>{}, 0, Const<0>{}), 0);
-    int s = 0;
-    for (; s + 1 < whole; s += 2) {
+    // Whole steps of this part of K, two at a time, one for each half of LDS;
+    // behind the last one it is fetched again, into memory that nobody reads any more.
+    const int all = a.blocks / kStep, share = (all + gridDim.y - 1) / gridDim.y;
+    const int end = min(all, share * ((int)blockIdx.y + 1));
+    int s = min(all, share * (int)blockIdx.y);
+    if (s < end) put_scales(fetch(Const<false>{}, s, Const<0>{}), 0);
+    for (; s + 1 < end; s += 2) {
         __syncthreads();                           // step s has arrived; nobody reads the other half
         Codes sc = fetch(Const<false>{}, s + 1, Const<1>{});
         multiply(Const<0>{});
         put_scales(sc, 1);
         __syncthreads();
-        sc = fetch(Const<false>{}, min(s + 2, whole - 1), Const<0>{});
+        sc = fetch(Const<false>{}, min(s + 2, end - 1), Const<0>{});
         multiply(Const<1>{});
         put_scales(sc, 0);
     }
     __syncthreads();
-    if (s < whole) multiply(Const<0>{});
-    if (whole * kStep < a.blocks) {
-        put_scales(fetch(Const<true>{}, whole, Const<1>{}), 1);
+    if (s < end) multiply(Const<0>{});
+    if (all * kStep < a.blocks && blockIdx.y + 1 == gridDim.y) {
+        put_scales(fetch(Const<true>{}, all, Const<1>{}), 1);
         __syncthreads();
         multiply(Const<1>{});
     }
@@ -390,6 +393,9 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
     __syncthreads();
     char* const part = wave / SHARE < 2 ? (wave / SHARE == 0 ? x0 : x1) : (wave / SHARE == 2 ? w0 : w1);
     T* const strip_at = (T*)part + wave % SHARE * 16 * PITCH;
+    // a part of K: float32 sums, no bias (launched with T = float)
+    T* const out = a.parts ? (T*)a.parts + (int64_t)blockIdx.y * a.M * a.N : (T*)a.out;
+    const int64_t ostride = a.parts ? a.N : a.stride;
     const int64_t wm0 = m0 + wm * 16 * F, wn0 = n0 + wn * 16 * G;
     float bias[G][4];
 #pragma unroll
@@ -417,7 +423,7 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
             const int at = q * kWave + lane, row = at / PER_ROW, c = at % PER_ROW * E;
             const int64_t m = wm0 + i * 16 + row, n = wn0 + c;
             if (row >= 16 || m >= a.M || n >= a.N) continue;
-            T* to = (T*)a.out + m * a.stride + n;
+            T* to = out + m * ostride + n;
             const T* from = strip_at + row * PITCH + c;
             if (n + E <= a.N) {
                 typedef typename Vec<T, E>::type Piece;
@@ -429,6 +435,155 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
             }
         }
         __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// out = act(sum of the parts, in order, + bias).
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_mx4_join(MxArgs a, int parts) {
+    const int64_t total = a.M * a.N, step = (int64_t)gridDim.x * kBlock * 4;
+    for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4; i < total; i += step) {
+        const int64_t m = i / a.N, n = i % a.N;
+        const int count = (int)min((int64_t)4, total - i);
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < parts; p++) {
+            const float* from = a.parts + p * total + i;
+            if (count == 4) {
+                float v[4];
+                Vec<float, 4>::load(from, v);
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] += v[e];
+            } else {
+                for (int e = 0; e < count; e++) y[e] += from[e];
+            }
+        }
+        if (n + 4 <= a.N) {                        // all in one row
+#pragma unroll
+            for (int e = 0; e < 4; e++) y[e] = finish(y[e], a.bias ? a.bias[n + e] : 0.f, a.relu);
+            Vec<T, 4>::store((T*)a.out + m * a.stride + n, y);
+        } else {
+            for (int e = 0; e < count; e++) {
+                const int64_t mm = (i + e) / a.N, nn = (i + e) % a.N;
+                ((T*)a.out)[mm * a.stride + nn] = from_float<T>(finish(y[e], a.bias ? a.bias[nn] : 0.f, a.relu));
+            }
+        }
+    }
+}
+
+// ----------------------------------------------------------------- few rows
+
+// Up to 16 Q rows of x: the weight is read once and bounds the product.  A
+// workgroup computes 16 columns of out; its waves take the steps of 256 k (a
+// cache line of every row of the weight) in turn and join their sums in LDS.
+// Every lane's operand is one 16-byte load, a step ahead of its use.  S is the
+// type of x's elements, which the workgroup quantises into LDS first (for one
+// row of 4096 to 4096 columns 10 us in all, 14 with a launch for it), or
+// uint8_t: x is quantised already.
+template <typename S> struct FewRows {
+    const S* x;
+    int64_t stride;                                // of float rows
+    const uint8_t* xs;                             // scale codes of quantised rows
+    int64_t cols;
+};
+
+template <typename S, typename T, int Q>
+__global__ __launch_bounds__(1024) void k_mx4_few(MxArgs a, FewRows<S> f) {
+    constexpr bool QUANTISED = std::is_same<S, uint8_t>::value;
+    __shared__ f32x4 sums[16][Q][kWave];
+    extern __shared__ uint4 own_rows[];            // codes, then scale codes, of x
+    const int lane = lane_id(), wave = wave_id(), waves = blockDim.x / kWave;
+    const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + lane % 16;
+    f32x4 acc[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q++) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t wrow = min(n, a.N - 1) * a.blocks;           // columns behind the last are not stored
+    struct Weight {
+        i32x4 w[2];
+        int s[2];
+    };
+    auto load_w = [&](int b0) {
+        Weight v = {{{0, 0, 0, 0}, {0, 0, 0, 0}}, {127, 127}};
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int b = b0 + k * 4 + lane / 16;
+            if (b < a.blocks) {
+                v.w[k] = *(const i32x4*)(a.wc + 16 * (wrow + b));
+                v.s[k] = a.ws[wrow + b];
+            }
+        }
+        return v;
+    };
+    Weight next = load_w(wave * 8);
+    const uint8_t *xc, *xs;
+    if constexpr (QUANTISED) {
+        xc = f.x;
+        xs = f.xs;
+    } else {
+        uint8_t* const codes = (uint8_t*)own_rows;
+        uint8_t* const scales = codes + a.M * a.blocks * 16;
+        const int per_row = a.blocks * 4, pieces = (int)a.M * per_row;
+        for (int i = threadIdx.x; i < pieces; i += blockDim.x) {        // a block's four pieces in adjacent lanes
+            float v[8];
+            load8<S>(f.x + (int64_t)(i / per_row) * f.stride, (int64_t)(i % per_row) * 8, f.cols, v);
+            uint32_t top = top_bits(v);
+            top = max(top, __float_as_uint(lane_pair<1>(__uint_as_float(top))));
+            top = max(top, __float_as_uint(lane_pair<2>(__uint_as_float(top))));
+            const int code = scale_code(top);
+            *(uint32_t*)(codes + 4 * i) = to_codes(v, code);
+            if (i % 4 == 0) scales[i / 4] = (uint8_t)code;
+        }
+        __syncthreads();
+        xc = codes;
+        xs = scales;
+    }
+    for (int b0 = wave * 8; b0 < a.blocks; b0 += waves * 8) {
+        const Weight w = next;
+        next = load_w(b0 + waves * 8);
+        i32x4 x[2][Q] = {};
+        int sx[2][Q];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int b = b0 + k * 4 + lane / 16;
+#pragma unroll
+            for (int q = 0; q < Q; q++) {
+                const int64_t m = q * 16 + lane % 16;
+                sx[k][q] = 127;
+                if (b < a.blocks && m < a.M) {
+                    x[k][q] = *(const i32x4*)(xc + 16 * (m * a.blocks + b));
+                    sx[k][q] = xs[m * a.blocks + b];
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+            for (int q = 0; q < Q; q++)
+                acc[q] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(w.w[k]), operand(x[k][q]), acc[q], 4, 4, 0,
+                                                                         w.s[k], 0, sx[k][q]);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; q++) sums[wave][q][lane] = acc[q];
+    __syncthreads();
+    for (int q = wave; q < Q; q += waves) {
+        f32x4 y = sums[0][q][lane];
+        for (int v = 1; v < waves; v++) {
+            const f32x4 z = sums[v][q][lane];
+#pragma unroll
+            for (int r = 0; r < 4; r++) y[r] += z[r];
+        }
+        const int64_t m = q * 16 + lane % 16, c = n0 + lane / 16 * 4;
+        if (m >= a.M) continue;
+        T* const to = (T*)a.out + m * a.stride + c;
+        float o[4];
+#pragma unroll
+        for (int r = 0; r < 4; r++) o[r] = finish(y[r], a.bias && c + r < a.N ? a.bias[c + r] : 0.f, a.relu);
+        if (c + 4 <= a.N) {
+            Vec<T, 4>::store(to, o);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; r++)
+                if (c + r < a.N) to[r] = from_float<T>(o[r]);
+        }
     }
 }
 
@@ -477,7 +632,9 @@ void mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, hipStream_t st) {
     });
 }
 
-constexpr int64_t kFullGrid = 256;
+constexpr int64_t kFullGrid = 256;                 // workgroups that fill the chip
+constexpr int64_t kPartGrid = 512;                 // and that parts of K aim at
+constexpr int64_t kPartSteps = 4;                  // fewest steps of a part
 
 static void check_sizes(int64_t M, int64_t N, int64_t K) {
     for (int64_t v : {M, N, K})
@@ -486,9 +643,33 @@ static void check_sizes(int64_t M, int64_t N, int64_t K) {
     AGNES_REQUIRE(K <= ((int64_t)1 << 24), AGNES_ERR_INVALID, "K must be at most 2^24");
 }
 
+// Which kernel computes M x N x K, by sizes alone.
+constexpr int64_t kFewRows = 64;                   // rows of k_mx4_few
+constexpr int64_t kFewQuantize = 16;               // and rows that it quantises itself,
+constexpr int64_t kFewBytes = 40 << 10;            // if they take no more LDS than this
+static int64_t few_lds(int64_t M, int64_t blocks) { return M * blocks * 17; }
+struct MxPlan {
+    int rows, cols;                                // of a tile; 0: k_mx4_few
+    int parts;                                     // of K
+};
+
+static MxPlan plan_product(int64_t M, int64_t N, int64_t K) {
+    if (M <= kFewRows) return {0, 0, 1};
+    // the largest tile that still gives every compute unit one
+    auto tiles = [&](int64_t r) { return ((M + r - 1) / r) * ((N + r - 1) / r); };
+    for (int r : {256, 128})
+        if (tiles(r) >= kFullGrid) return {r, r, 1};
+    // else small tiles, and K in parts of at least kPartSteps steps
+    const int64_t steps = mx_blocks(K) / kStep;
+    const int64_t parts = std::min<int64_t>(kPartGrid / tiles(64), steps / kPartSteps);
+    return {64, 64, (int)std::max<int64_t>(1, parts)};
+}
+
 uint64_t mx4_product_bytes(int64_t M, int64_t N, int64_t K) {
     check_sizes(M, N, K);
-    return 0;
+    if (M == 0 || N == 0) return 0;
+    const MxPlan p = plan_product(M, N, K);
+    return p.parts > 1 ? (uint64_t)(p.parts * M * N) * 4 : 0;
 }
 
 uint64_t mx4_linear_bytes(int64_t M, int64_t N, int64_t K) {
@@ -499,20 +680,34 @@ uint64_t mx4_linear_bytes(int64_t M, int64_t N, int64_t K) {
     return c.used + mx4_product_bytes(M, N, K);
 }
 
-template <typename T, int WM, int WN, int F, int G> static void launch_tile(const MxArgs& a, hipStream_t st) {
+template <typename T, int WM, int WN, int F, int G> static void launch_tile(const MxArgs& a, int parts, hipStream_t st) {
     constexpr int R = MxSide<WM, F>::ROWS, C = MxSide<WN, G>::ROWS;
     const int64_t tiles = ((a.M + R - 1) / R) * ((a.N + C - 1) / C);
     AGNES_REQUIRE(tiles < (1 << 23), AGNES_ERR_RANGE, "the product has too many tiles");
     const unsigned grid = (unsigned)((tiles + kXcds - 1) / kXcds * kXcds);
-    AGNES_LAUNCH((k_mx4_gemm<T, WM, WN, F, G>), dim3(grid), dim3(kWave * WM * WN), 0, st, a);
+    AGNES_LAUNCH((k_mx4_gemm<T, WM, WN, F, G>), dim3(grid, (unsigned)parts), dim3(kWave * WM * WN), 0, st, a);
 }
 
-// The largest tile that still gives every compute unit one.
-template <typename T> static void launch_gemm(const MxArgs& a, hipStream_t st) {
-    auto tiles = [&](int64_t r) { return ((a.M + r - 1) / r) * ((a.N + r - 1) / r); };
-    if (tiles(256) >= kFullGrid) launch_tile<T, 2, 4, 8, 4>(a, st);
-    else if (tiles(128) >= kFullGrid) launch_tile<T, 2, 2, 4, 4>(a, st);
-    else launch_tile<T, 2, 2, 2, 2>(a, st);
+template <typename T> static void launch_gemm(const MxPlan& p, const MxArgs& a, hipStream_t st) {
+    if (p.rows == 256) launch_tile<T, 2, 4, 8, 4>(a, p.parts, st);
+    else if (p.rows == 128) launch_tile<T, 2, 2, 4, 4>(a, p.parts, st);
+    else launch_tile<T, 2, 2, 2, 2>(a, p.parts, st);
+}
+
+template <typename S, typename T> static void launch_few(const MxArgs& a, const FewRows<S>& f, hipStream_t st) {
+    const int64_t groups = (a.N + 15) / 16;
+    AGNES_REQUIRE(groups < (1 << 22), AGNES_ERR_RANGE, "the product has too many columns");
+    // more waves where there are few workgroups, but a step for each
+    const int steps = (a.blocks + 7) / 8;
+    int waves = groups <= 512 ? 16 : 8;
+    while (waves > 1 && waves / 2 >= steps) waves /= 2;
+    const dim3 grid((unsigned)groups), block((unsigned)(waves * kWave));
+    const size_t lds = std::is_same<S, uint8_t>::value ? 0 : (size_t)few_lds(a.M, a.blocks);
+    if (a.M <= 16) AGNES_LAUNCH((k_mx4_few<S, T, 1>), grid, block, lds, st, a, f);
+    else if constexpr (std::is_same<S, uint8_t>::value) {
+        if (a.M <= 32) AGNES_LAUNCH((k_mx4_few<S, T, 2>), grid, block, 0, st, a, f);
+        else AGNES_LAUNCH((k_mx4_few<S, T, 4>), grid, block, 0, st, a, f);
+    }
 }
 
 void mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, bool relu, const agnes_matrix* out,
@@ -526,11 +721,23 @@ void mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, bool
     const int64_t M = x->rows, N = w->rows, blocks = mx_blocks(x->cols);
     check_workspace(ws, ws_bytes, mx4_product_bytes(M, N, x->cols));   // checks the sizes too
     if (M == 0 || N == 0) return;
+    const MxPlan p = plan_product(M, N, x->cols);
+    MxArgs a{x->codes, x->scales, w->codes, w->scales, M, N, (int32_t)blocks, bias, relu,
+             M * N * (int64_t)elem_size(out->dtype) > kStreamBytes, out->data, out->stride, nullptr};
     with_float(out->dtype, [&](auto t) {
         typedef decltype(t) T;
-        const MxArgs a{x->codes, x->scales, w->codes, w->scales, M, N, (int32_t)blocks, bias, relu,
-                       M * N * (int64_t)sizeof(T) > kStreamBytes, out->data, out->stride};
-        launch_gemm<T>(a, st);
+        if (p.rows == 0) {
+            launch_few<uint8_t, T>(a, FewRows<uint8_t>{x->codes, 0, x->scales, x->cols}, st);
+        } else if (p.parts == 1) {
+            launch_gemm<T>(p, a, st);
+        } else {
+            a.parts = (float*)ws;
+            MxArgs sums = a;
+            sums.bias = nullptr;
+            sums.relu = sums.nt = false;
+            launch_gemm<float>(p, sums, st);
+            AGNES_LAUNCH((k_mx4_join<T>), dim3(grid_for((M * N + 3) / 4, 4096)), dim3(kBlock), 0, st, a, p.parts);
+        }
     });
 }
 
@@ -544,6 +751,18 @@ void mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const float* bias, bo
                   "out must have x's rows and one column per row of w");
     check_workspace(ws, ws_bytes, mx4_linear_bytes(x->rows, w->rows, x->cols));
     if (x->rows == 0 || w->rows == 0) return;
+    if (x->rows <= kFewQuantize && few_lds(x->rows, mx_blocks(x->cols)) <= kFewBytes) {
+        const MxArgs a{nullptr, nullptr, w->codes, w->scales, x->rows, w->rows, (int32_t)mx_blocks(x->cols), bias, relu,
+                       false, out->data, out->stride, nullptr};
+        with_float(x->dtype, [&](auto ts) {
+            with_float(out->dtype, [&](auto t) {
+                typedef decltype(ts) S;
+                typedef decltype(t) T;
+                launch_few<S, T>(a, FewRows<S>{(const S*)x->data, x->stride, nullptr, x->cols}, st);
+            });
+        });
+        return;
+    }
     Carve c(ws);
     agnes_mx4 q{};
     q.rows = x->rows;
