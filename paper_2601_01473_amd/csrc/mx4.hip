@@ -197,6 +197,8 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void static_f
 // Sixteen zero bytes: blocks behind the last one of a row.
 static __device__ const uint4 k_mx4_zero = {0u, 0u, 0u, 0u};
 
+constexpr int kVmcnt0 = 0x0F70;                    // s_waitcnt vmcnt(0) and nothing else
+
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
@@ -362,6 +364,13 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
             __builtin_amdgcn_sched_barrier(0);
         });
     };
+    // What a wave has fetched to LDS is there: a barrier alone does not wait for
+    // loads that are under way.  The scales, fetched behind the codes, have been
+    // waited for before, so this costs nothing.
+    auto arrived = [] {
+        __builtin_amdgcn_s_waitcnt(kVmcnt0);
+        __syncthreads();
+    };
     // Whole steps of this part of K, two at a time, one for each half of LDS;
     // behind the last one it is fetched again, into memory that nobody reads any more.
     const int all = a.blocks / kStep, share = (all + gridDim.y - 1) / gridDim.y;
@@ -369,20 +378,20 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx4_gemm(MxArgs a) {
     int s = min(all, share * (int)blockIdx.y);
     if (s < end) put_scales(fetch(Const<false>{}, s, Const<0>{}), 0);
     for (; s + 1 < end; s += 2) {
-        __syncthreads();                           // step s has arrived; nobody reads the other half
+        arrived();                                 // step s has arrived; nobody reads the other half
         Codes sc = fetch(Const<false>{}, s + 1, Const<1>{});
         multiply(Const<0>{});
         put_scales(sc, 1);
-        __syncthreads();
+        arrived();
         sc = fetch(Const<false>{}, min(s + 2, end - 1), Const<0>{});
         multiply(Const<1>{});
         put_scales(sc, 0);
     }
-    __syncthreads();
+    arrived();
     if (s < end) multiply(Const<0>{});
     if (all * kStep < a.blocks && blockIdx.y + 1 == gridDim.y) {
         put_scales(fetch(Const<true>{}, all, Const<1>{}), 1);
-        __syncthreads();
+        arrived();
         multiply(Const<1>{});
     }
     // Rows leave through LDS, each wave its own part in strips of 16 rows, as
