@@ -330,3 +330,20 @@ def test_batch_embedding(ag):
         batch.embedding_grad_rows(torch.empty(3, 40, device="cuda"))
     batch.close()
     store.close()
+
+
+@pytest.mark.parametrize("D", [5, 200])
+@pytest.mark.parametrize("length", [1, 2, 7, 8, 9, 15, 16, 17, 24, 25, 31, 32, 33, 40, 41, 70])
+@pytest.mark.parametrize("n", [600, 9500])
+def test_grad_runs_across_chunks(ag, n, length, D):
+    """Runs of one length, and behind them runs of every length from 1 to 45, lie in every position to the pieces
+    that the sorted list is cut into."""
+    first = torch.arange(n // 2) // length
+    lengths = torch.arange(1, 46).repeat(n // 1000 + 1)
+    rest = torch.repeat_interleave(torch.arange(len(lengths)), lengths)[: n - len(first)] + int(first[-1]) + 1
+    ids = torch.cat([first, rest])
+    V = int(ids[-1]) + 2
+    ids = ids[torch.randperm(len(ids), generator=torch.Generator().manual_seed(length))].int().cuda()
+    g = normal((len(ids), D), F32, 60 + length)
+    check_dense(ag, g, ids, V)
+    check_rows(ag, g, ids, V)
