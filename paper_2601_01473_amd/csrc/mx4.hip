@@ -486,7 +486,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_join(MxArgs a, int parts) {
 
 // ----------------------------------------------------------------- few rows
 
-// Up to 16 Q rows of x: the weight is read once and bounds the product.  A
+// Up to 16 Q rows of x, Q = 1 or 2: the weight is read once and bounds the product.  A
 // workgroup computes 16 columns of out; its waves take the steps of 256 k (a
 // cache line of every row of the weight) in turn and join their sums in LDS.
 // Every lane's operand is one 16-byte load, a step ahead of its use.  S is the
@@ -658,7 +658,15 @@ static void check_sizes(int64_t M, int64_t N, int64_t K) {
 }
 
 // Which kernel computes M x N x K, by sizes alone.
-constexpr int64_t kFewRows = 64;                   // rows of k_mx4_few
+// k_mx4_few reads x again for every 16 columns of out, and a workgroup's steps
+// follow each other, so more than one 16-row tile pays only while rows x K x
+// rounds of workgroups is small.  us, k_mx4_few against tiles with K in parts, of
+// N x K: 32 rows of 4096 x 4096 7.8 / 9.5, of 8192 x 1000 4.9 / 4.8, of 256 x 2048 4.9 / 7.3;
+// 17 rows of 8192 x 8192 18.8 / 14.0, of 1024 x 8192 9.8 / 9.2; 64 rows of 4096 x
+// 4096 11.5 / 10.6, of 8192 x 8192 40 / 16, of 8192 x 1000 7.0 / 4.9.
+constexpr int64_t kFewTile = 16;                   // rows of k_mx4_few, whatever the sizes,
+constexpr int64_t kFewRows = 32;                   // and at most, as long as
+constexpr int64_t kFewWork = 1 << 17;              // rows x K x rounds is no more than this
 constexpr int64_t kFewQuantize = 16;               // and rows that it quantises itself,
 constexpr int64_t kFewBytes = 40 << 10;            // if they take no more LDS than this
 static int64_t few_lds(int64_t M, int64_t blocks) { return M * blocks * 17; }
@@ -668,8 +676,10 @@ struct MxPlan {
 };
 
 static MxPlan plan_product(int64_t M, int64_t N, int64_t K) {
-    if (M <= kFewRows) return {0, 0, 1};
-    // the largest tile that still gives every compute unit one
+    const int64_t rounds = (N + 16 * kFullGrid - 1) / (16 * kFullGrid);
+    if (M <= kFewTile || (M <= kFewRows && K <= kFewWork && M * K * rounds <= kFewWork)) return {0, 0, 1};
+    // the largest tile that still gives every compute unit one (8192^3: 305 us in
+    // tiles of 256, 407 in tiles of 128)
     auto tiles = [&](int64_t r) { return ((M + r - 1) / r) * ((N + r - 1) / r); };
     for (int r : {256, 128})
         if (tiles(r) >= kFullGrid) return {r, r, 1};
@@ -719,8 +729,7 @@ template <typename S, typename T> static void launch_few(const MxArgs& a, const 
     const size_t lds = std::is_same<S, uint8_t>::value ? 0 : (size_t)few_lds(a.M, a.blocks);
     if (a.M <= 16) AGNES_LAUNCH((k_mx4_few<S, T, 1>), grid, block, lds, st, a, f);
     else if constexpr (std::is_same<S, uint8_t>::value) {
-        if (a.M <= 32) AGNES_LAUNCH((k_mx4_few<S, T, 2>), grid, block, 0, st, a, f);
-        else AGNES_LAUNCH((k_mx4_few<S, T, 4>), grid, block, 0, st, a, f);
+        AGNES_LAUNCH((k_mx4_few<S, T, 2>), grid, block, 0, st, a, f);
     }
 }
 

@@ -221,3 +221,10 @@ def test_linear_same_bits_every_time_and_on_another_stream(ag):
             torch.cuda.synchronize()
             assert torch.equal(out, ag.mx4_linear(x, w, b))
             assert torch.equal(back, ag.mx4_dequantize(ag.mx4_quantize(x)))
+
+
+@pytest.mark.parametrize("M", [16, 17, 31, 32, 33, 48, 64, 65])
+@pytest.mark.parametrize("N,K", [(70, 300), (100, 4096), (33, 4129), (4100, 2048)])
+def test_linear_rows_about_the_limits_of_the_kernels(ag, M, N, K):
+    """The kernel of few rows, whole tiles and parts of K take over from each other about here."""
+    check_linear(ag, M, N, K, bias=M % 2 == 0, relu=M == 33)
