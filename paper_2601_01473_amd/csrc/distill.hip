@@ -182,7 +182,10 @@ __device__ __forceinline__ int64_t load_label(const DistillArgs& a, int64_t r) {
 
 // The teacher's distribution over lanes gl = 0 .. L - 1, entries e = gl (loaded
 // before: first), gl + L, ...: classes (-1: padding) to cls, probabilities to
-// prob.  Every lane gets the terms.
+// prob.  Every lane gets the terms.  The largest logit is subtracted before the
+// division by T, as for the student: a quotient would overflow at T < 1 where
+// logits are the type's lowest or highest value, and lose digits where all of
+// a row's logits are large.
 __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float w, Entry first, int64_t y, int gl,
                                          int L, int32_t* cls, float* prob) {
     float tm = -INFINITY;
@@ -190,7 +193,7 @@ __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float 
     for (int e = gl; e < a.k; e += L) {
         if (e != gl) n = load_entry(a, r, e);
         const bool ok = n.c >= 0 && n.c < a.C;
-        const float x = ok ? n.t * a.inv_t : -INFINITY;
+        const float x = ok ? n.t : -INFINITY;
         cls[e] = ok ? (int32_t)n.c : -1;
         prob[e] = x;
         tm = x != x ? INFINITY : fmaxf(tm, x);   // NaN: as +inf, which makes the sum NaN
@@ -201,7 +204,7 @@ __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float 
     q.some = a.soft > 0.f && tm != -INFINITY;
     float ts = 0.f;
     for (int e = gl; e < a.k; e += L) {
-        const float p = q.some ? pow2((prob[e] - tm) * kLog2e) : 0.f;
+        const float p = q.some ? pow2((prob[e] - tm) * a.ct) : 0.f;
         prob[e] = p;
         ts += p;
     }

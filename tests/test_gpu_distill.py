@@ -275,3 +275,33 @@ def test_another_stream_and_a_graph(ag):
             l3, s3 = ag.distill_loss(z, t, cls, **args)
             assert torch.equal(l2, l3) and torch.equal(stats, s3)
             assert torch.equal(g2, ag.distill_grad(z, t, cls, s3, **args))
+
+
+@pytest.mark.parametrize("C,k", [(40, 5), (700, 5), (5000, 100), (70001, 5)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_teacher_logits_at_the_ends_of_their_type(ag, dtype, C, k):
+    """A row whose valid entries are all the type's lowest (or highest) finite value has a uniform teacher at any
+    temperature; one highest value takes everything."""
+    z, t, cls, y, w = make(6, C, k, dtype, seed=16)
+    t = t.to(dtype)
+    w[:] = 1
+    cls[:] = torch.arange(k, device="cuda")
+    cls[1, 2:] = -1
+    cls[2, 0] = C
+    t[0], t[1], t[2] = torch.finfo(dtype).min, torch.finfo(dtype).min, torch.finfo(dtype).max
+    t[3, 1] = torch.finfo(dtype).max
+    t[4, 1:] = torch.finfo(dtype).min
+    for T in (0.25, 0.5, 1.0, 3.0):
+        loss, grad = check(ag, z, t, cls, y, w, T=T, soft=0.5, hard=0.5)
+        assert bool(torch.isfinite(loss).all())
+        check(ag, z, t, cls, None, w, T=T)
+
+
+@pytest.mark.parametrize("C,k", [(40, 8), (700, 8), (5000, 100), (70001, 8)])
+@pytest.mark.parametrize("offset", [-4000.0, 3000.0, 2.0 ** 20])
+def test_teacher_logits_with_a_common_offset(ag, C, k, offset):
+    """The softmax does not see what all logits share: its error grows with their differences alone."""
+    z, t, cls, y, w = make(6, C, k, F32, seed=17)
+    t = (t * 8).round() / 8                                   # the sum is exact
+    for T in (3.0, 0.7):
+        check(ag, z, t + offset, cls, y, w, T=T, soft=0.5, hard=0.5)
