@@ -41,7 +41,7 @@ struct DistillArgs {
     agnes_dtype ttype, gtype;
     bool wide;                     // 64-bit classes and labels
     bool nt;                       // gradient past the caches
-    float temp, inv_t, soft, hard; // T, 1 / T, a, b
+    float temp, soft, hard;        // T, a, b
     float ct;                      // log2(e) / T: exp(x / T) = 2^(x ct)
 };
 
@@ -224,22 +224,29 @@ __device__ __forceinline__ Terms teacher(const DistillArgs& a, int64_t r, float 
     return teacher(a, r, w, load_entry(a, r, gl), load_label(a, r), gl, L, cls, prob);
 }
 
-// sum_e p_e (ln p_e - ln q_{c_e}) over the lanes, from z_{c_e} in zc.
+// An entry's part of the divergence: T p (ln p - ln q_c), from z - m of its class
+// and the logarithm of S_T.  The difference is not divided by T: at T < 1 that
+// overflows for a logit at the type's lowest value.
+__device__ __forceinline__ float divergence_term(const DistillArgs& a, float p, float zm, float lt) {
+    return p * (a.temp * (logf(p) + lt) - zm);
+}
+
+// T sum_e p_e (ln p_e - ln q_{c_e}) over the lanes, from z_{c_e} in zc.
 __device__ __forceinline__ float divergence(const DistillArgs& a, const Sums& s, const float* prob, const float* zc,
                                             int gl, int L) {
     const float lt = logf(s.st);
     float part = 0.f;
     for (int e = gl; e < a.k; e += L) {
         const float p = prob[e];
-        if (p != 0.f) part += p * (logf(p) - ((zc[e] - s.m) * a.inv_t - lt));
+        if (p != 0.f) part += divergence_term(a, p, zc[e] - s.m, lt);
     }
     return lanes_sum(part, L);
 }
 
-// dy = z_y - m.
+// div: T times the divergence; dy = z_y - m.
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Terms& q, const Sums& s, float div, float dy) {
     if (no_logits(s)) return q.some || q.named ? q.w * INFINITY : 0.f;
-    float L = q.some ? a.soft * a.temp * a.temp * div : 0.f;
+    float L = q.some ? a.soft * a.temp * div : 0.f;
     if (q.named) L += a.hard * (logf(s.s1) - dy);
     return q.w * L;
 }
@@ -415,10 +422,7 @@ __global__ __launch_bounds__(kBlock) void k_distill_lanes(DistillArgs a, int L) 
                 const float lt = logf(s.st);
                 for (int e = gl; e < a.k; e += L) {
                     const float p = prob[e];
-                    if (p != 0.f) {
-                        const float z = (float)zrow[cls[e]];
-                        div += p * (logf(p) - ((z - s.m) * a.inv_t - lt));
-                    }
+                    if (p != 0.f) div += divergence_term(a, p, (float)zrow[cls[e]] - s.m, lt);
                 }
                 div = lanes_sum(div, L);
             }
@@ -690,7 +694,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_apply(DistillArgs a, i
             for (int e = lane; e < a.k; e += kWave)
                 if (prob[e] != 0.f) part += prob[e] * logf(prob[e]);
             part = lanes_sum(part, kWave);
-            const float div = part - (cross * a.inv_t - mass * logf(s.st));
+            const float div = a.temp * (part + mass * logf(s.st)) - cross;
             if (lane == 0) a.loss[r] = row_loss(a, q, s, q.some ? div : 0.f, label);
         }
         if (first && lane == 0 && a.stats) {
@@ -799,7 +803,6 @@ static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* gra
     a.C = (int32_t)C;
     a.k = (int32_t)k;
     a.temp = d->temperature;
-    a.inv_t = 1.f / d->temperature;
     a.ct = kLog2e / d->temperature;
     a.soft = d->soft;
     a.hard = d->labels ? d->hard : 0.f;

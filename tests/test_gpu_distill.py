@@ -305,3 +305,17 @@ def test_teacher_logits_with_a_common_offset(ag, C, k, offset):
     t = (t * 8).round() / 8                                   # the sum is exact
     for T in (3.0, 0.7):
         check(ag, z, t + offset, cls, y, w, T=T, soft=0.5, hard=0.5)
+
+
+@pytest.mark.parametrize("C", [40, 700, 5000, 70001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_teacher_asks_for_a_logit_at_its_types_lowest_value(ag, dtype, C):
+    """The loss is large, and finite wherever T (z - m) p is: the difference is not divided by T < 1 on its own."""
+    z, t, cls, y, w = make(4, C, 4, dtype, seed=18)
+    w[:] = 1
+    t[:] = 0                                                  # p = 1 / 4 each
+    cls[:] = torch.arange(4, device="cuda")
+    z[0, 1] = z[1, 0] = z[2, 3] = torch.finfo(dtype).min
+    for T in (0.25, 0.5, 1.0):
+        loss, _ = check(ag, z, t, cls, y, w, T=T)
+        assert bool(torch.isfinite(loss).all()) and bool((loss[:3] > 1e37).all())
