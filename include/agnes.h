@@ -550,7 +550,8 @@ agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_mat
  *   labels: index_dtype [rows], or NULL (no second term).
  *   weight: float32 [rows], or NULL (1).  The gradient of a loss that is
  *     not a weighted sum: pass its row factors here to agnes_distill_grad.
- *   temperature > 0, soft >= 0, hard >= 0, all finite.
+ *   temperature > 0, soft >= 0, hard >= 0, all finite, and log2(e) / temperature
+ *     finite in float32 (temperature above 4.24e-39).
  * agnes_distill_loss: loss [rows] and, unless NULL, stats [rows][3]: the row's
  *   largest logit m, sum exp((z - m) / T) and, where there is a second term,
  *   sum exp(z - m); zeros for a row of weight 0.

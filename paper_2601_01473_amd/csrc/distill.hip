@@ -773,8 +773,8 @@ static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* gra
     AGNES_REQUIRE(is_index(d->index_dtype), AGNES_ERR_INVALID, "classes and labels must be int32 or int64");
     AGNES_REQUIRE(d->classes || k == 0 || rows == 0, AGNES_ERR_INVALID, "classes must not be NULL");
     AGNES_REQUIRE(d->classes_stride >= 0, AGNES_ERR_INVALID, "classes_stride must not be negative");
-    AGNES_REQUIRE(std::isfinite(d->temperature) && d->temperature > 0.f && std::isfinite(1.f / d->temperature),
-                  AGNES_ERR_INVALID, "the temperature must be positive and finite");
+    AGNES_REQUIRE(std::isfinite(d->temperature) && d->temperature > 0.f && std::isfinite(kLog2e / d->temperature),
+                  AGNES_ERR_INVALID, "the temperature must be positive and finite, and so must log2(e) / temperature");
     AGNES_REQUIRE(std::isfinite(d->soft) && d->soft >= 0.f && std::isfinite(d->hard) && d->hard >= 0.f,
                   AGNES_ERR_INVALID, "soft and hard must be finite and not negative");
     DistillArgs a{};

@@ -200,3 +200,12 @@ def test_tensors_of_the_wrong_kind_are_refused():
         ag.mx4_linear(x[:, :3], q)
     with pytest.raises(ag.AgnesError):
         ag.distill_loss(x, x, c, temperature=0.0)
+
+
+def test_distill_temperature_too_small_for_its_factor():
+    """exp(x / T) is computed as 2^(x log2(e) / T): the factor has to be finite, or an x of 0 gives NaN."""
+    for soft, hard in ((1.0, 0.0), (0.0, 1.0)):
+        d = dis(T=3.5e-39, soft=soft, hard=hard, labels=P)       # 1 / T is finite
+        refused(lambda: B.agnes_distill_loss(d, P, P, P, BIG), "temperature")
+        refused(lambda: B.agnes_distill_grad(d, P, mat(4, 9)), "temperature")
+        refused(lambda: B.agnes_distill_loss_grad(d, P, mat(4, 9), P, BIG), "temperature")
