@@ -735,6 +735,7 @@ constexpr int64_t kSplitPieces = 1024;           // rows that may be split
 constexpr int64_t kBlockPieces = 16 * 1024;      // a workgroup's rows
 constexpr int64_t kSplitRows = 512;              // fewer rows leave too many compute units idle
 constexpr int64_t kSplitGroups = 1024;           // workgroups that a split aims at
+constexpr int64_t kLaunchRows = 1 << 21;         // rows per launch of a workgroup each: a launch holds fewer than 2^32 threads
 
 // Parts of a row of C logits of `size` bytes, or 1 and span 0: not split.  A
 // part has at least one round of its workgroup.
@@ -809,6 +810,22 @@ static DistillArgs check_distill(const agnes_distill* d, const agnes_matrix* gra
     return a;
 }
 
+// The n rows from row r on.
+template <typename T> static DistillArgs rows_from(const DistillArgs& a, int64_t r, int64_t n) {
+    DistillArgs b = a;
+    b.z = (const T*)a.z + r * a.zstride;
+    b.t = (const char*)a.t + r * a.tstride * (int64_t)elem_size(a.ttype);
+    b.classes = (const char*)a.classes + r * a.cstride * (a.wide ? 8 : 4);
+    if (a.labels) b.labels = (const char*)a.labels + r * (a.wide ? 8 : 4);
+    if (a.weight) b.weight = a.weight + r;
+    if (a.loss) b.loss = a.loss + r;
+    if (a.stats) b.stats = a.stats + 3 * r;
+    if (a.stats_in) b.stats_in = a.stats_in + 3 * r;
+    if (a.grad) b.grad = (char*)a.grad + r * a.gstride * (int64_t)elem_size(a.gtype);
+    b.rows = n;
+    return b;
+}
+
 template <typename T, int MODE> static void launch(const DistillArgs& a, void* ws, hipStream_t st) {
     constexpr int E = 16 / (int)sizeof(T);
     const int64_t pieces = (a.C + E - 1) / E, rows = a.rows;
@@ -834,18 +851,8 @@ template <typename T, int MODE> static void launch(const DistillArgs& a, void* w
     if (span) {
         // blockIdx.y holds at most 65535 rows
         for (int64_t r = 0; r < rows; r += 65535) {
-            DistillArgs b = a;
             const int64_t n = std::min<int64_t>(65535, rows - r);
-            b.z = (const T*)a.z + r * a.zstride;
-            b.t = (const char*)a.t + r * a.tstride * (int64_t)elem_size(a.ttype);
-            b.classes = (const char*)a.classes + r * a.cstride * (a.wide ? 8 : 4);
-            if (a.labels) b.labels = (const char*)a.labels + r * (a.wide ? 8 : 4);
-            if (a.weight) b.weight = a.weight + r;
-            if (a.loss) b.loss = a.loss + r;
-            if (a.stats) b.stats = a.stats + 3 * r;
-            if (a.stats_in) b.stats_in = a.stats_in + 3 * r;
-            if (a.grad) b.grad = (char*)a.grad + r * a.gstride * (int64_t)elem_size(a.gtype);
-            b.rows = n;
+            const DistillArgs b = rows_from<T>(a, r, n);
             Part* p = (Part*)ws + r * parts;
             const dim3 grid((unsigned)parts, (unsigned)n);
             if (!a.stats_in) AGNES_LAUNCH((k_distill_part<T, MODE>), grid, dim3(kPartThreads), 0, st, b, span, p);
@@ -855,12 +862,16 @@ template <typename T, int MODE> static void launch(const DistillArgs& a, void* w
         }
         return;
     }
-    const dim3 grid((unsigned)rows);
-    if (pieces <= 4 * 256) AGNES_LAUNCH((k_distill_block<T, 256, 4, MODE>), grid, dim3(256), 0, st, a);
-    else if (pieces <= 8 * 256) AGNES_LAUNCH((k_distill_block<T, 256, 8, MODE>), grid, dim3(256), 0, st, a);
-    else if (pieces <= 8 * 512) AGNES_LAUNCH((k_distill_block<T, 512, 8, MODE>), grid, dim3(512), 0, st, a);
-    else if (pieces <= 8 * 1024) AGNES_LAUNCH((k_distill_block<T, 1024, 8, MODE>), grid, dim3(1024), 0, st, a);
-    else AGNES_LAUNCH((k_distill_block<T, 1024, 16, MODE>), grid, dim3(1024), 0, st, a);
+    for (int64_t r = 0; r < rows; r += kLaunchRows) {
+        const int64_t n = std::min(kLaunchRows, rows - r);
+        const DistillArgs b = rows_from<T>(a, r, n);
+        const dim3 grid((unsigned)n);
+        if (pieces <= 4 * 256) AGNES_LAUNCH((k_distill_block<T, 256, 4, MODE>), grid, dim3(256), 0, st, b);
+        else if (pieces <= 8 * 256) AGNES_LAUNCH((k_distill_block<T, 256, 8, MODE>), grid, dim3(256), 0, st, b);
+        else if (pieces <= 8 * 512) AGNES_LAUNCH((k_distill_block<T, 512, 8, MODE>), grid, dim3(512), 0, st, b);
+        else if (pieces <= 8 * 1024) AGNES_LAUNCH((k_distill_block<T, 1024, 8, MODE>), grid, dim3(1024), 0, st, b);
+        else AGNES_LAUNCH((k_distill_block<T, 1024, 16, MODE>), grid, dim3(1024), 0, st, b);
+    }
 }
 
 static void run(const agnes_distill* d, const DistillArgs& a, void* ws, hipStream_t st) {

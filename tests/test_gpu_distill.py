@@ -319,3 +319,24 @@ def test_teacher_asks_for_a_logit_at_its_types_lowest_value(ag, dtype, C):
     for T in (0.25, 0.5, 1.0):
         loss, _ = check(ag, z, t, cls, y, w, T=T)
         assert bool(torch.isfinite(loss).all()) and bool((loss[:3] > 1e37).all())
+
+
+def test_more_rows_than_one_launch_holds(ag):
+    """2^24 workgroups of 256 threads are one launch too large: short rows with more than 64 entries take one each."""
+    rows, C, k = (1 << 24) + 5, 9, 65
+    g = torch.Generator(device="cuda").manual_seed(22)
+    z = torch.randn(rows, C, device="cuda", generator=g).to(BF16)
+    t = torch.randn(1, k, device="cuda", generator=g).expand(rows, k)
+    cls = torch.randint(0, C, (1, k), device="cuda", generator=g).expand(rows, k)
+    y = torch.randint(0, C, (rows,), device="cuda", generator=g)
+    w = torch.rand(rows, device="cuda", generator=g)
+    args = dict(temperature=2.0, soft=0.5, hard=0.5)
+    loss, grad = ag.distill_loss_grad(z, t, cls, labels=y, weight=w, **args)
+    alone, stats = ag.distill_loss(z, t, cls, labels=y, weight=w, **args)
+    later = ag.distill_grad(z, t, cls, stats, labels=y, weight=w, **args)
+    some = [0, 1, 65534, 65535, 65536, (1 << 21) - 1, 1 << 21, (1 << 21) + 1, 1 << 23, (1 << 24) - 1, 1 << 24, rows - 1]
+    L, eL, G, eG = ref.distill(z[some], t[some], cls[some], y[some], w[some], **args)
+    ref.within(loss[some], L, eL, "loss")
+    ref.within(grad[some], G, eG, "gradient")
+    ref.within(alone[some], L, eL, "loss alone")
+    ref.within(later[some], G, eG, "gradient from the statistics")
