@@ -613,22 +613,32 @@ static void check_mx4(const agnes_mx4* q, const char* name) {
     AGNES_REQUIRE(((uintptr_t)q->codes & 15) == 0, AGNES_ERR_INVALID, n + ": codes must be 16-byte aligned");
 }
 
-static unsigned grid_of(int64_t n, int64_t per) {
-    const int64_t g = (n + per - 1) / per;
-    AGNES_REQUIRE(g < ((int64_t)1 << 31), AGNES_ERR_RANGE, "the matrix is too large");
-    return (unsigned)g;
+// Calls launch(first row, pieces, workgroups) for parts of `rows` rows of
+// per_row <= 2^28 pieces, each of at most kLaunchGroups workgroups: a launch
+// holds fewer than 2^32 threads.
+constexpr int64_t kLaunchGroups = 1 << 22;
+template <typename F> static void launch_pieces(int64_t rows, int64_t per_row, F&& launch) {
+    constexpr int64_t kGroup = kBlock * kPieces;
+    const int64_t most = kLaunchGroups * kGroup / per_row;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = std::min(most, rows - r), pieces = n * per_row;
+        launch(r, pieces, (unsigned)((pieces + kGroup - 1) / kGroup));
+    }
 }
 
 void mx4_quantize(const agnes_matrix* x, const agnes_mx4* q, hipStream_t st) {
     check_matrix(x, false, "x");
     check_mx4(q, "q");
     AGNES_REQUIRE(q->rows == x->rows && q->cols == x->cols, AGNES_ERR_INVALID, "x and q must have equal shapes");
-    const int64_t per_row = mx_blocks(x->cols) * 4, pieces = x->rows * per_row;
-    if (pieces == 0) return;
+    const int64_t blocks = mx_blocks(x->cols), per_row = blocks * 4;
+    if (x->rows == 0 || per_row == 0) return;
     with_float(x->dtype, [&](auto t) {
         typedef decltype(t) T;
-        AGNES_LAUNCH((k_mx4_quantize<T>), dim3(grid_of(pieces, kBlock * kPieces)), dim3(kBlock), 0, st,
-                     (const T*)x->data, x->stride, pieces, x->cols, (uint32_t)per_row, q->codes, q->scales);
+        launch_pieces(x->rows, per_row, [&](int64_t r, int64_t pieces, unsigned groups) {
+            AGNES_LAUNCH((k_mx4_quantize<T>), dim3(groups), dim3(kBlock), 0, st, (const T*)x->data + r * x->stride,
+                         x->stride, pieces, x->cols, (uint32_t)per_row, q->codes + r * blocks * 16,
+                         q->scales + r * blocks);
+        });
     });
 }
 
@@ -636,13 +646,15 @@ void mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, hipStream_t st) {
     check_matrix(x, true, "x");
     check_mx4(q, "q");
     AGNES_REQUIRE(q->rows == x->rows && q->cols == x->cols, AGNES_ERR_INVALID, "x and q must have equal shapes");
-    const int64_t per_row = mx_blocks(x->cols) * 4, pieces = x->rows * per_row;
-    if (pieces == 0) return;
+    const int64_t blocks = mx_blocks(x->cols), per_row = blocks * 4;
+    if (x->rows == 0 || per_row == 0) return;
     with_float(x->dtype, [&](auto t) {
         typedef decltype(t) T;
-        AGNES_LAUNCH((k_mx4_dequantize<T>), dim3(grid_of(pieces, kBlock * kPieces)), dim3(kBlock), 0, st, q->codes,
-                     q->scales, pieces, x->cols, (uint32_t)per_row, (T*)x->data, x->stride,
-                     x->rows * x->cols * (int64_t)sizeof(T) > kStreamBytes);
+        launch_pieces(x->rows, per_row, [&](int64_t r, int64_t pieces, unsigned groups) {
+            AGNES_LAUNCH((k_mx4_dequantize<T>), dim3(groups), dim3(kBlock), 0, st, q->codes + r * blocks * 16,
+                         q->scales + r * blocks, pieces, x->cols, (uint32_t)per_row, (T*)x->data + r * x->stride,
+                         x->stride, x->rows * x->cols * (int64_t)sizeof(T) > kStreamBytes);
+        });
     });
 }
 

@@ -228,3 +228,30 @@ def test_linear_same_bits_every_time_and_on_another_stream(ag):
 def test_linear_rows_about_the_limits_of_the_kernels(ag, M, N, K):
     """The kernel of few rows, whole tiles and parts of K take over from each other about here."""
     check_linear(ag, M, N, K, bias=M % 2 == 0, relu=M == 33)
+
+
+def test_quantize_more_than_one_launch_holds(ag):
+    """One row of 8192 for 2^24 + 5 rows: a workgroup each, more than a launch takes; 69 GB of codes."""
+    rows, K = (1 << 24) + 5, 8192
+    torch.cuda.empty_cache()
+    one = normal((1, K), BF16, 22, spread=1.0)
+    codes, scales = ref.mx4(one)
+    q = ag.mx4_quantize(one.expand(rows, K))
+    for r in range(0, rows, 1 << 20):
+        assert bool((q.codes[r:r + (1 << 20)] == codes.cuda()).all()), r
+        assert bool((q.scales[r:r + (1 << 20)] == scales.cuda()).all()), r
+    del q
+    torch.cuda.empty_cache()
+
+
+def test_rows_on_both_sides_of_a_launch(ag):
+    """Narrow rows, 2^30 of them in a launch: back and forth across the boundary."""
+    rows, at = (1 << 30) + 3, (1 << 30) - 2
+    torch.cuda.empty_cache()
+    x = torch.zeros(rows, 1, dtype=BF16, device="cuda")
+    x[:3, 0], x[at:, 0] = torch.tensor([1.5, -3.0, 0.25]).to(BF16).cuda(), torch.tensor([0.5, -6.0, 4.0, -1.0, 3.0]).to(BF16).cuda()
+    v = ag.mx4_dequantize(ag.mx4_quantize(x), dtype=BF16)
+    assert torch.equal(v[:3], x[:3]) and torch.equal(v[at:], x[at:])      # of the format's values, each its block's largest
+    assert int((v != 0).sum()) == 8
+    del x, v
+    torch.cuda.empty_cache()
