@@ -732,7 +732,8 @@ template <typename T> static void launch_gemm(const MxPlan& p, const MxArgs& a, 
 
 template <typename S, typename T> static void launch_few(const MxArgs& a, const FewRows<S>& f, hipStream_t st) {
     const int64_t groups = (a.N + 15) / 16;
-    AGNES_REQUIRE(groups < (1 << 22), AGNES_ERR_RANGE, "the product has too many columns");
+    // above 512 workgroups they have at most 512 threads: a launch holds fewer than 2^32
+    AGNES_REQUIRE(groups < (1 << 23), AGNES_ERR_RANGE, "the product has too many columns");
     // more waves where there are few workgroups, but a step for each
     const int steps = (a.blocks + 7) / 8;
     int waves = groups <= 512 ? 16 : 8;

@@ -255,3 +255,18 @@ def test_rows_on_both_sides_of_a_launch(ag):
     assert int((v != 0).sum()) == 8
     del x, v
     torch.cuda.empty_cache()
+
+
+def test_linear_of_more_than_2_to_26_columns(ag):
+    """The header's limit is 2^23 tiles; of one row a tile is 16 columns wide."""
+    N, K = (1 << 26) + 37, 32
+    g = torch.Generator(device="cuda").manual_seed(23)
+    codes = torch.randint(0, 256, (N, 16), dtype=torch.uint8, device="cuda", generator=g)
+    scales = torch.full((N, 1), 127, dtype=torch.uint8, device="cuda")
+    x = normal((2, K), BF16, 24)
+    vx = ref.mx4_values(*ag.mx4_quantize(x))
+    for rows in (x[:1], ag.mx4_quantize(x)):
+        out = ag.mx4_linear(rows, ag.Mx4(codes, scales, K), dtype=F32)
+        at = torch.tensor([0, 1, 15, 16, (1 << 25) - 1, (1 << 26) - 1, 1 << 26, N - 17, N - 1], device="cuda")
+        want, err = ref.product(vx[:out.shape[0]], ref.mx4_values(codes[at], scales[at], K), None, False)
+        ref.within(out[:, at], want, err, "many columns")
