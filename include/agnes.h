@@ -608,9 +608,9 @@ agnes_status agnes_mx4_dequantize(const agnes_mx4* q, const agnes_matrix* x, voi
  * stays NaN): 4-bit operands, float32 sums, one rounding to out's type.  bias:
  * float32 [N] or NULL.  agnes_mx4_linear quantises its float rows x first
  * (into the workspace); w is laid out once by agnes_mx4_quantize.
- * M, N < 2^31, K <= 2^24.  Errors: INVALID, RANGE (2^23 or more tiles, which
+ * M, N < 2^31, K <= 2^24.  Errors: INVALID, RANGE (more than 2^23 - 8 tiles, which
  * are 16 columns of out for up to 16 rows of x, and 256 x 256 elements of out
- * for many). */
+ * for many; nothing is enqueued then). */
 agnes_status agnes_mx4_product_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
 agnes_status agnes_mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, int32_t relu,
                                const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);

@@ -687,14 +687,22 @@ struct MxPlan {
     int parts;                                     // of K
 };
 
+// Refuses what one launch cannot hold (2^32 threads), so that callers do before
+// they enqueue anything: a tile has at most 512 threads, and their number is
+// rounded up to one for each XCD.
 static MxPlan plan_product(int64_t M, int64_t N, int64_t K) {
+    auto fits = [](MxPlan p, int64_t tiles) {
+        AGNES_REQUIRE(tiles <= (1 << 23) - kXcds, AGNES_ERR_RANGE, "the product has too many tiles");
+        return p;
+    };
     const int64_t rounds = (N + 16 * kFullGrid - 1) / (16 * kFullGrid);
-    if (M <= kFewTile || (M <= kFewRows && K <= kFewWork && M * K * rounds <= kFewWork)) return {0, 0, 1};
+    if (M <= kFewTile || (M <= kFewRows && K <= kFewWork && M * K * rounds <= kFewWork))
+        return fits({0, 0, 1}, (N + 15) / 16);
     // the largest tile that still gives every compute unit one (8192^3: 305 us in
     // tiles of 256, 407 in tiles of 128)
     auto tiles = [&](int64_t r) { return ((M + r - 1) / r) * ((N + r - 1) / r); };
     for (int r : {256, 128})
-        if (tiles(r) >= kFullGrid) return {r, r, 1};
+        if (tiles(r) >= kFullGrid) return fits({r, r, 1}, tiles(r));
     // else small tiles, and K in parts of at least kPartSteps steps
     const int64_t steps = mx_blocks(K) / kStep;
     const int64_t parts = std::min<int64_t>(kPartGrid / tiles(64), steps / kPartSteps);
@@ -719,7 +727,6 @@ uint64_t mx4_linear_bytes(int64_t M, int64_t N, int64_t K) {
 template <typename T, int WM, int WN, int F, int G> static void launch_tile(const MxArgs& a, int parts, hipStream_t st) {
     constexpr int R = MxSide<WM, F>::ROWS, C = MxSide<WN, G>::ROWS;
     const int64_t tiles = ((a.M + R - 1) / R) * ((a.N + C - 1) / C);
-    AGNES_REQUIRE(tiles < (1 << 23), AGNES_ERR_RANGE, "the product has too many tiles");
     const unsigned grid = (unsigned)((tiles + kXcds - 1) / kXcds * kXcds);
     AGNES_LAUNCH((k_mx4_gemm<T, WM, WN, F, G>), dim3(grid, (unsigned)parts), dim3(kWave * WM * WN), 0, st, a);
 }
@@ -732,9 +739,8 @@ template <typename T> static void launch_gemm(const MxPlan& p, const MxArgs& a, 
 
 template <typename S, typename T> static void launch_few(const MxArgs& a, const FewRows<S>& f, hipStream_t st) {
     const int64_t groups = (a.N + 15) / 16;
-    // above 512 workgroups they have at most 512 threads: a launch holds fewer than 2^32
-    AGNES_REQUIRE(groups < (1 << 23), AGNES_ERR_RANGE, "the product has too many columns");
-    // more waves where there are few workgroups, but a step for each
+    // more waves where there are few workgroups, but a step for each; above 512
+    // workgroups at most 512 threads
     const int steps = (a.blocks + 7) / 8;
     int waves = groups <= 512 ? 16 : 8;
     while (waves > 1 && waves / 2 >= steps) waves /= 2;

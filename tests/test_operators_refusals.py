@@ -209,3 +209,12 @@ def test_distill_temperature_too_small_for_its_factor():
         refused(lambda: B.agnes_distill_loss(d, P, P, P, BIG), "temperature")
         refused(lambda: B.agnes_distill_grad(d, P, mat(4, 9)), "temperature")
         refused(lambda: B.agnes_distill_loss_grad(d, P, mat(4, 9), P, BIG), "temperature")
+
+
+def test_mx4_products_of_too_many_tiles():
+    """2^23 tiles of 16 columns, or of 256 x 256 elements, are refused before any work."""
+    for rows, N in ((1, (1 << 27) - 15), (16, 1 << 30), (33, (1 << 31) - 1)):
+        for call, a in ((B.agnes_mx4_linear, mat(rows, 32)), (B.agnes_mx4_product, mx(rows, 32))):
+            with pytest.raises(B.AgnesError) as e:
+                call(a, mx(N, 32), None, 0, mat(rows, N), P, BIG)
+            assert e.value.status == B.AGNES_ERR_RANGE, e.value
