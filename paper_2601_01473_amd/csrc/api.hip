@@ -174,6 +174,7 @@ static void release_batch(Batch* b) {
             if (b->state == kGathering && b->gathered_at) (void)hipEventSynchronize(b->gathered_at);
         }
         if (b->sage_pending && b->sage_done) (void)hipEventSynchronize(b->sage_done);
+        if (b->lookup_pending && b->lookup_done) (void)hipEventSynchronize(b->lookup_done);
         b->magic = 0;
         delete b;
     }

@@ -716,13 +716,13 @@ void embedding_grad_rows(const agnes_matrix* grad_out, const void* ids, agnes_dt
 static int64_t enter_batch(Batch& b, hipStream_t st) {
     AGNES_REQUIRE(b.state == kGathering || b.state == kDone, AGNES_ERR_INVALID, "the batch holds no finished hyperbatch");
     AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.gathered_at, 0));
-    if (b.sage_pending) AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.sage_done, 0));
+    if (b.lookup_pending) AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.lookup_done, 0));
     return b.node_off[b.H];
 }
 
 static void leave_batch(Batch& b, hipStream_t st) {
-    AGNES_CHECK_HIP(hipEventRecord(b.sage_done, st));
-    b.sage_pending = true;
+    AGNES_CHECK_HIP(hipEventRecord(b.lookup_done, st));
+    b.lookup_pending = true;
 }
 
 void batch_embedding_lookup(Batch& b, const agnes_matrix* table, float scale, const agnes_matrix* out,

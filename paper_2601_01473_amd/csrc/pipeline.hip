@@ -1894,9 +1894,10 @@ void begin_hyperbatch(const Store& s, Batch& b, const int32_t* targets, bool tar
     // a batch still gathering: its buffers are in use until the gather ends
     if (b.state == kGathering) wait_batch(b);
     b.state = kIdle;
-    // a forward still reading the batch's CSR and rows: this hyperbatch's
-    // kernels overwrite them, so they queue behind it
+    // a forward still reading the batch's CSR and rows, or an embedding call its
+    // node list: this hyperbatch's kernels overwrite them, so they queue behind it
     if (b.sage_pending) AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.sage_done, 0));
+    if (b.lookup_pending) AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.lookup_done, 0));
     AGNES_REQUIRE(join_write_lds(H, kJoinGroupTilesMax + 2) <= (size_t)s.max_lds &&
                       join_count_lds(H, kJoinGroupTilesMax + 2) <= (size_t)s.max_lds,
                   AGNES_ERR_RANGE, "H is too large for the device's workgroup memory");
@@ -1908,6 +1909,7 @@ void begin_hyperbatch(const Store& s, Batch& b, const int32_t* targets, bool tar
     if (!b.listed) AGNES_CHECK_HIP(hipEventCreateWithFlags(&b.listed, hipEventDisableTiming));
     if (!b.gathered) AGNES_CHECK_HIP(hipEventCreateWithFlags(&b.gathered, hipEventDisableTiming));
     if (!b.sage_done) AGNES_CHECK_HIP(hipEventCreateWithFlags(&b.sage_done, hipEventDisableTiming));
+    if (!b.lookup_done) AGNES_CHECK_HIP(hipEventCreateWithFlags(&b.lookup_done, hipEventDisableTiming));
     b.d_lsz = (const int32_t*)((const char*)w.sync.ptr + y.lsz);
     b.d_ecount = (const int64_t*)((const char*)w.sync.ptr + y.ecount);
     b.store = &s;

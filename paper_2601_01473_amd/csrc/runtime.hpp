@@ -343,6 +343,11 @@ struct Batch {
     // and the next forward wait for it before they overwrite what it reads.
     hipEvent_t sage_done = nullptr;
     bool sage_pending = false;
+    // The end of the last embedding call that reads the node list, for the next
+    // hyperbatch.  Not sage_done: a forward without allocations records that
+    // without waiting for it, which would drop a call on another stream.
+    hipEvent_t lookup_done = nullptr;
+    bool lookup_pending = false;
     // Device copies of the layer sizes [H][L+1] and per-hop edge counts [H][L]
     // (inside ws.sync), valid once the hyperbatch's sampling has finished.
     const int32_t* d_lsz = nullptr;
@@ -363,6 +368,7 @@ struct Batch {
         if (needed) (void)hipEventDestroy(needed);
         if (sage_ev) (void)hipEventDestroy(sage_ev);
         if (sage_done) (void)hipEventDestroy(sage_done);
+        if (lookup_done) (void)hipEventDestroy(lookup_done);
         for (auto& e : ws.ev)
             if (e) (void)hipEventDestroy(e);
     }

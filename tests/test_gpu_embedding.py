@@ -347,3 +347,71 @@ def test_grad_runs_across_chunks(ag, n, length, D):
     g = normal((len(ids), D), F32, 60 + length)
     check_dense(ag, g, ids, V)
     check_rows(ag, g, ids, V)
+
+
+# ----------------------------------------------------------------- order against the batch's other work
+
+def keep_busy(stream):
+    """Some milliseconds of work in front of what is enqueued on the stream next."""
+    with torch.cuda.stream(stream):
+        a = torch.ones(8192, 8192, dtype=BF16, device="cuda")
+        for _ in range(4):
+            a = a @ a
+
+
+def nodes_of(store, targets, seed):
+    batch = store.prepare(targets, [6, 4], seed=seed)
+    nodes = torch.from_numpy(np.concatenate([m["nodes"] for m in batch.to_host(features=False)]))
+    batch.close()
+    return nodes
+
+
+def test_batch_embedding_is_ordered_behind_the_gather_and_before_the_next_hyperbatch(ag):
+    off, idx = random_graph(3000, 9, seed=2, hubs=3, hub_deg=900)
+    store = ag.Store(off, idx, features(3000, 16, 3), 256)
+    targets = [distinct_targets(3000, 5, 30, 70 + k) for k in range(4)]
+    nodes = [nodes_of(store, t, k) for k, t in enumerate(targets)]
+    table = normal((3000, 40), F32, 43)
+    grads = [normal((len(n), 40), F32, 44) for n in nodes]
+    torch.cuda.synchronize()
+    main, sides, batch, results = torch.cuda.Stream(), [torch.cuda.Stream(), torch.cuda.Stream()], None, []
+    for k, t in enumerate(targets):
+        keep_busy(main)
+        batch = store.begin(t, [6, 4], seed=k, batch=batch, stream=main)
+        batch.finish(stream=main)                             # the gather is on its way, nobody waits for it
+        keep_busy(sides[0])
+        first = batch.embedding(table, stream=sides[0])       # a reader that is late,
+        rows = batch.embedding_grad_rows(grads[k], max_rows=len(nodes[k]), stream=sides[1])    # and one that follows it
+        results.append((first, rows))
+    batch.close()                                             # waits for both
+    torch.cuda.synchronize()
+    for n, g, (first, (row_ids, rows, count)) in zip(nodes, grads, results):
+        ref.within(first, *ref.lookup(table, n, 1.0))
+        names, want, err = ref.grad(g, n, 3000, 1.0)
+        m = len(names)
+        assert int(count) == m and torch.equal(row_ids[:m].cpu().long(), names)
+        ref.within(rows[:m], want, err)
+    store.close()
+
+
+def test_a_forward_does_not_drop_an_embedding_call_on_another_stream(ag):
+    """The next hyperbatch waits for the lookup, also where a forward was enqueued behind it elsewhere."""
+    off, idx = random_graph(3000, 9, seed=4, hubs=3, hub_deg=900)
+    store = ag.Store(off, idx, features(3000, 32, 5), 256)
+    targets = [distinct_targets(3000, 5, 30, 80 + k) for k in range(4)]
+    nodes = [nodes_of(store, t, k) for k, t in enumerate(targets)]
+    table = normal((3000, 40), F32, 45)
+    ws = [normal((32, 64), BF16, 46).view(torch.int16), normal((32, 64), BF16, 47).view(torch.int16)]
+    bs = [torch.zeros(32, device="cuda") for _ in ws]
+    torch.cuda.synchronize()
+    side, batch, results = torch.cuda.Stream(), None, []
+    for k, t in enumerate(targets):
+        batch = store.prepare(t, [6, 4], seed=k, batch=batch)
+        keep_busy(side)
+        results.append(batch.embedding(table, stream=side))
+        batch.sage_forward(ws, bs, noalloc=k % 2 == 0)
+    torch.cuda.synchronize()
+    for n, got in zip(nodes, results):
+        ref.within(got, *ref.lookup(table, n, 1.0))
+    batch.close()
+    store.close()
