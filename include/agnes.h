@@ -461,12 +461,13 @@ agnes_status agnes_sage_forward_noalloc(agnes_batch* batch, const agnes_sage_mod
  *
  * Shared conventions: every pointer is device memory of the current device
  * unless said otherwise; every call enqueues on hip_stream and returns without
- * waiting; it keeps nothing between calls, so calls on different streams do
- * not disturb each other.  A call that needs scratch memory takes it from its
+ * waiting; it keeps nothing between calls (agnes_batch_embedding_* mark their
+ * batch as being read), so calls on different streams do not disturb each
+ * other.  A call that needs scratch memory takes it from its
  * caller: `workspace` (device, 256-byte aligned) of at least the bytes that
  * its *_bytes function returns for the same sizes, in use until the call's work
  * on hip_stream is done.  The calls allocate nothing and may be captured in a HIP
- * graph.  Results are the same on every run: sums have a fixed order.
+ * graph, except agnes_batch_embedding_*.  Results are the same on every run: sums have a fixed order.
  * ------------------------------------------------------------------------- */
 
 /* A row-major matrix: element (i, j) is data[i * stride + j] (stride in
@@ -519,8 +520,10 @@ agnes_status agnes_embedding_grad_rows(const agnes_matrix* grad_out, const void*
 /* The same for a batch's node list: ids = the batch's nodes (minibatch-major,
  * agnes_batch_view.nodes), n = node_off[H], table rows = the store's nodes.
  * The call is ordered after the batch's gather on whatever stream that runs,
- * and the next hyperbatch begun on the batch waits for it.  Errors: INVALID
- * (also a batch without a finished hyperbatch). */
+ * and the next hyperbatch begun on the batch waits for it.  A replayed graph
+ * would be ordered against neither, so the calls cannot be captured.  Errors:
+ * INVALID (also a batch without a finished hyperbatch, and a stream that is
+ * being captured). */
 agnes_status agnes_batch_embedding_lookup(agnes_batch* batch, const agnes_matrix* table, float scale,
                                           const agnes_matrix* out, void* hip_stream);
 agnes_status agnes_batch_embedding_grad_rows(agnes_batch* batch, const agnes_matrix* grad_out, float scale,

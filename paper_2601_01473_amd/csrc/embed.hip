@@ -712,9 +712,15 @@ void embedding_grad_rows(const agnes_matrix* grad_out, const void* ids, agnes_dt
 // ----------------------------------------------------------------- a batch's nodes
 
 // Orders `st` behind the batch's gather and behind an earlier reader on another
-// stream, so that the event recorded after the work covers both.
+// stream, so that the event recorded after the work covers both.  Neither can be
+// captured: the gather's event lies outside the graph, and one recorded inside
+// it says nothing about a replay.
 static int64_t enter_batch(Batch& b, hipStream_t st) {
     AGNES_REQUIRE(b.state == kGathering || b.state == kDone, AGNES_ERR_INVALID, "the batch holds no finished hyperbatch");
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    AGNES_CHECK_HIP(hipStreamIsCapturing(st, &cs));
+    AGNES_REQUIRE(cs == hipStreamCaptureStatusNone, AGNES_ERR_INVALID,
+                  "a batch's embedding calls cannot be captured in a graph; take its node list and the calls on ids");
     AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.gathered_at, 0));
     if (b.lookup_pending) AGNES_CHECK_HIP(hipStreamWaitEvent(st, b.lookup_done, 0));
     return b.node_off[b.H];

@@ -415,3 +415,29 @@ def test_a_forward_does_not_drop_an_embedding_call_on_another_stream(ag):
         ref.within(got, *ref.lookup(table, n, 1.0))
     batch.close()
     store.close()
+
+
+def test_batch_embedding_refuses_a_capture_and_leaves_it_intact(ag):
+    off, idx = random_graph(2000, 7, seed=6)
+    store = ag.Store(off, idx, features(2000, 16, 7), 256)
+    batch = store.prepare(distinct_targets(2000, 3, 20, 90), [5], seed=1)
+    nodes = torch.from_numpy(np.concatenate([m["nodes"] for m in batch.to_host(features=False)])).cuda()
+    table, g = normal((2000, 24), F32, 48), normal((len(nodes), 24), F32, 49)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in (lambda: batch.embedding(table), lambda: batch.embedding_grad_rows(g, max_rows=len(nodes))):
+            with pytest.raises(ag.AgnesError) as e:
+                call()
+            assert e.value.status == 1 and "captured" in str(e.value)
+        out = ag.embedding_lookup(table, nodes)               # the node list's ids serve instead
+    for k in range(3):
+        table.copy_(normal((2000, 24), F32, 100 + k))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, batch.embedding(table))
+    batch = store.prepare(distinct_targets(2000, 3, 20, 91), [5], seed=2, batch=batch)
+    torch.cuda.synchronize()
+    batch.close()
+    store.close()
