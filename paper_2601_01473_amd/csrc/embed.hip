@@ -717,6 +717,9 @@ void embedding_grad_rows(const agnes_matrix* grad_out, const void* ids, agnes_dt
 // it says nothing about a replay.
 static int64_t enter_batch(Batch& b, hipStream_t st) {
     AGNES_REQUIRE(b.state == kGathering || b.state == kDone, AGNES_ERR_INVALID, "the batch holds no finished hyperbatch");
+    int dev = 0;
+    AGNES_CHECK_HIP(hipGetDevice(&dev));
+    AGNES_REQUIRE(dev == b.store->device, AGNES_ERR_INVALID, "the current device is not the batch's device");
     hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
     AGNES_CHECK_HIP(hipStreamIsCapturing(st, &cs));
     AGNES_REQUIRE(cs == hipStreamCaptureStatusNone, AGNES_ERR_INVALID,

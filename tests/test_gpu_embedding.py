@@ -441,3 +441,19 @@ def test_batch_embedding_refuses_a_capture_and_leaves_it_intact(ag):
     torch.cuda.synchronize()
     batch.close()
     store.close()
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
+def test_batch_embedding_refuses_another_device_than_the_batchs(ag):
+    off, idx = random_graph(500, 5, seed=8)
+    store = ag.Store(off, idx, features(500, 16, 9), 256)
+    batch = store.prepare(distinct_targets(500, 2, 10, 92), [3], seed=1)
+    rows = len(np.concatenate([m["nodes"] for m in batch.to_host(features=False)]))
+    with torch.cuda.device(1):
+        table, g = torch.zeros(500, 8, device="cuda"), torch.zeros(rows, 8, device="cuda")
+        for call in (lambda: batch.embedding(table), lambda: batch.embedding_grad_rows(g, max_rows=rows)):
+            with pytest.raises(ag.AgnesError) as e:
+                call()
+            assert e.value.status == 1 and "device" in str(e.value)
+    batch.close()
+    store.close()
