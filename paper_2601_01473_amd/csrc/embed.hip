@@ -255,7 +255,7 @@ template <typename TO> struct Sink {
         store_piece<TO, E>(p, c, D, acc, nt);
     }
     template <int E> __device__ __forceinline__ void leave(int64_t entry, int64_t c, const float (&acc)[E]) const {
-        if (c < dpad) Vec<float, E>::store(part + entry * dpad + c, acc);   // dpad is a multiple of E
+        if (c < D) Vec<float, E>::store(part + entry * dpad + c, acc);      // dpad is a multiple of E
     }
 };
 
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Sorted<TI> s, Sink<TO> o, 
             for (int e = 0; e < E; e++) acc[e] += (float)x[j][e];
         }
     };
-    Raw xa[kRows], xb[kRows];
+    Raw xa[kRows] = {}, xb[kRows] = {};                             // lanes behind the last column load nothing
     fetch(0, xa);
     for (int q = 0; q < s.chunk; q += 2 * kRows) {                  // chunk is a multiple of 2 kRows
         fetch(q + kRows, xb);
@@ -486,10 +486,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(const float* __restrict__
     const int64_t c = (int64_t)blockIdx.x / tiles * groups + g;
     const int tile = blockIdx.x % tiles;
     const int64_t q0 = c * chunk;
-    if (q0 >= entries) return;
-    const int64_t q1 = min(entries, q0 + chunk);
     const int64_t col = ((int64_t)tile * lanes + gl) * E;
-    const bool live = col < o.dpad;
+    if (q0 >= entries || col >= o.D) return;                        // D > 0, and lanes do not exchange anything
+    const int64_t q1 = min(entries, q0 + chunk);
     int32_t cur = -1, head = -1, tail = -1;
     bool continued = false, open = true;
     float acc[E] = {0.f, 0.f, 0.f, 0.f};
@@ -501,7 +500,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(const float* __restrict__
         for (int j = 0; j < R; j++) row[j] = q + j < entries ? in_row[q + j] : -1;
 #pragma unroll
         for (int j = 0; j < R; j++)
-            if (row[j] >= 0 && live) Vec<float, E>::load(in + (q + j) * o.dpad + col, x[j]);
+            if (row[j] >= 0) Vec<float, E>::load(in + (q + j) * o.dpad + col, x[j]);
 #pragma unroll
         for (int j = 0; j < R; j++) {
             if (!open) continue;
@@ -552,7 +551,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(const float* __restrict__
 
 // ----------------------------------------------------------------- gradient: host
 
-constexpr int kLevels = 8;                  // 2^31 ids: 2^27 entries, then 1/32 each
+constexpr int kLevels = 8;                  // 2^31 ids: 2^27 entries, then 1/8 of them at each level, 2^9 at the seventh
 struct GradPlan {
     uint32_t *keys[2], *perm[2], *hist, *dtot;
     int64_t *sizes, *rank, *partials;

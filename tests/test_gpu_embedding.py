@@ -457,3 +457,32 @@ def test_batch_embedding_refuses_another_device_than_the_batchs(ag):
             assert e.value.status == 1 and "device" in str(e.value)
     batch.close()
     store.close()
+
+
+@pytest.mark.parametrize("D", [1, 4, 5, 9, 70])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [40, 3000, 20000])
+def test_grad_does_not_see_what_the_workspace_holds(ag, n, D, dtype):
+    """Partial sums have padded rows; a workspace full of NaN gives the bits that one full of zeros gives."""
+    from paper_2601_01473_amd import _binding as B
+    V = 60
+    g, ids = normal((n, D), dtype, 50), make_ids(n, V, 3.0, torch.int32, 51)
+    code = {F32: B.AGNES_FLOAT32, BF16: B.AGNES_BFLOAT16}[dtype]
+    need = B.agnes_embedding_grad_bytes(n, V, D)
+    results = []
+    for fill in (0, 255):
+        ws = torch.full((need,), fill, dtype=torch.uint8, device="cuda")
+        dense, rows = torch.zeros(V, D, device="cuda"), torch.zeros(V, D, device="cuda")
+        row_ids, count = torch.zeros(V, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+        st = torch.cuda.current_stream().cuda_stream
+        mat = lambda t: B.agnes_matrix(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0),   # noqa: E731
+                                       B.AGNES_FLOAT32 if t.dtype == F32 else code)
+        B.agnes_embedding_grad(mat(g), ids.data_ptr(), B.AGNES_INT32, 1.5, 0, mat(dense), ws.data_ptr(), need, st)
+        ws.fill_(fill)
+        B.agnes_embedding_grad_rows(mat(g), ids.data_ptr(), B.AGNES_INT32, 1.5, V, row_ids.data_ptr(), mat(rows),
+                                    count.data_ptr(), ws.data_ptr(), need, st)
+        results.append((dense, rows, row_ids, count))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    names, want, err = ref.grad(g, ids, V, 1.5)
+    ref.within(results[1][0][names.cuda()], want, err)
+    ref.within(results[1][1][:len(names)], want, err)
