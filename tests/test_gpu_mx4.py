@@ -270,3 +270,48 @@ def test_linear_of_more_than_2_to_26_columns(ag):
         at = torch.tensor([0, 1, 15, 16, (1 << 25) - 1, (1 << 26) - 1, 1 << 26, N - 17, N - 1], device="cuda")
         want, err = ref.product(vx[:out.shape[0]], ref.mx4_values(codes[at], scales[at], K), None, False)
         ref.within(out[:, at], want, err, "many columns")
+
+
+# 128 x 128 tiles serve products with at least 256 of them and fewer than 256 of 256 x 256, which serve the rest.  A
+# step is 256 columns: none, one, even and odd numbers of them, with and without a part of one behind.
+TILES_128 = [(2100, 2100, 1100), (2049, 2047, 1280), (2048, 2048, 512), (1300, 3500, 700), (2100, 2100, 200),
+             (2049, 2100, 256)]
+TILES_256 = [(4100, 4100, 300), (4100, 4100, 800), (4097, 4095, 1056), (4096, 4096, 2048), (4097, 4200, 250),
+             (8200, 2050, 512), (4351, 4097, 256), (4100, 4100, 1792)]
+
+
+@pytest.mark.parametrize("M,N,K", TILES_128 + TILES_256)
+def test_linear_large_tiles(ag, M, N, K):
+    check_linear(ag, M, N, K)
+    check_linear(ag, M, N, K, dtype=F16, out=F32, bias=False, relu=True, seed=31)
+
+
+@pytest.mark.parametrize("M,N,K", [TILES_128[0], TILES_128[1], TILES_256[1], TILES_256[2], TILES_256[7]])
+def test_linear_large_tiles_whole_numbers_are_exact(ag, M, N, K):
+    g = torch.Generator().manual_seed(25)
+    grid = torch.tensor(ref.MAGNITUDES + [-m for m in ref.MAGNITUDES])
+    x, w = grid[torch.randint(0, 16, (M, K), generator=g)], grid[torch.randint(0, 16, (N, K), generator=g)]
+    x[:, ::32], w[:, ::32] = 6, 4                            # every block's scale is 1
+    got = ag.mx4_linear(x.cuda(), ag.mx4_quantize(w.cuda()))
+    assert torch.equal(got.cpu().double(), x.double() @ w.double().T)
+    # rows at other strides, 16-bit results
+    out = torch.full((M, N + 9), 5.0, dtype=F16, device="cuda")
+    ag.mx4_linear(x.cuda(), ag.mx4_quantize(w.cuda()), out=out[:, 3:3 + N])
+    assert torch.equal(out[:, 3:3 + N], got.half())
+    assert bool((out[:, :3] == 5).all()) and bool((out[:, 3 + N:] == 5).all())
+
+
+@pytest.mark.parametrize("M,N", [(2100, 2100), (4100, 4100)])
+@pytest.mark.parametrize("blocks", [70, 33])
+def test_linear_large_tiles_every_scale_reaches_its_block(ag, M, N, blocks):
+    """One nonzero block per row, with a scale of its own, and columns of other scales."""
+    K = 32 * blocks
+    r, n = torch.arange(M), torch.arange(N)
+    x, w = torch.zeros(M, blocks, 32), torch.ones(N, blocks, 32)
+    size = 2.0 ** (r * 7 % 101 - 50).double()
+    x[r, r % blocks] = size.float().unsqueeze(1)
+    power = (n.unsqueeze(1) * 3 + torch.arange(blocks) * 5) % 19 - 9
+    w *= (2.0 ** power.double()).float().unsqueeze(2)
+    got = ag.mx4_linear(x.view(M, K).cuda(), ag.mx4_quantize(w.view(N, K).cuda()))
+    want = 32 * size.unsqueeze(1) * (2.0 ** power.double()).T[r % blocks]
+    assert torch.equal(got.cpu().double(), want)
