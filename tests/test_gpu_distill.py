@@ -340,3 +340,85 @@ def test_more_rows_than_one_launch_holds(ag):
     ref.within(grad[some], G, eG, "gradient")
     ref.within(alone[some], L, eL, "loss alone")
     ref.within(later[some], G, eG, "gradient from the statistics")
+
+
+def sharp(a, b):
+    """Equal bits, NaN included."""
+    return torch.equal(a.contiguous().view(torch.int32 if a.dtype == F32 else torch.int16),
+                       b.contiguous().view(torch.int32 if b.dtype == F32 else torch.int16))
+
+
+@pytest.mark.parametrize("pieces", [1025, 2048, 2049, 4096, 4097, 8192, 8193, 16384, 16385])
+@pytest.mark.parametrize("dtype,T,soft,hard", [(F32, 1.0, 1.0, 0.0), (F32, 3.0, 0.7, 0.3), (BF16, 2.0, 0.5, 0.5),
+                                               (F16, 0.6, 0.4, 0.6)])
+def test_many_long_rows(ag, pieces, dtype, T, soft, hard):
+    """Rows long enough to be split, and enough of them (512) not to be: widths of `pieces` times 16 bytes, the odd ones
+    with one logit in the last piece.  The first rows hold what a row can hold; the rest only has to be there."""
+    E, rows, k = 16 // torch.empty(0, dtype=dtype).element_size(), 515, 20
+    C = pieces * E if pieces % 2 == 0 else (pieces - 1) * E + 1
+    g = torch.Generator(device="cuda").manual_seed(pieces)
+    z = (2 * torch.randn(rows, C, device="cuda", generator=g)).to(dtype)
+    cls = torch.randint(0, C, (rows, k), device="cuda", generator=g).int()
+    t = torch.gather(z.float(), 1, cls.long()) + torch.randn(rows, k, device="cuda", generator=g)
+    y = torch.randint(0, C, (rows,), device="cuda", generator=g).int()
+    w = torch.rand(rows, device="cuda", generator=g) + 0.1
+    cls[0], cls[1, 3:], cls[2, 5:] = -1, C, 7                # no entry, few, one class many times
+    y[1], y[2], y[3] = C, 7, cls[3, 0]
+    cls[4, :] = torch.arange(k, device="cuda")
+    z[4, k:], y[4] = -INF, 0                                 # everything but the listed classes masked
+    z[5, C // 2:], cls[5, :], y[5] = torch.finfo(dtype).min, 0, C // 2 - 1
+    z[6, C - 1], cls[6, 0], y[6] = 3.0, C - 1, C - 1         # the last logit
+    w[7], z[7] = 0, float("nan")
+    z[8] = -INF
+    z[9, C - 1], z[10, 0] = float("nan"), INF
+    args = dict(labels=y, weight=w, temperature=T, soft=soft, hard=hard)
+    loss, grad = ag.distill_loss_grad(z, t, cls, **args)
+    some = [0, 1, 2, 3, 4, 5, 6, 11, 300, rows - 1]
+    L, eL, G, eG = ref.distill(z[some], t[some], cls[some], y[some], w[some], T, soft, hard)
+    ref.within(loss[some], L, eL, "loss")
+    ref.within(grad[some], G, eG, "gradient")
+    assert float(loss[7]) == 0 and bool((grad[7] == 0).all())
+    assert float(loss[8]) == INF and bool((grad[8] == 0).all())
+    for r in (9, 10):
+        assert bool(loss[r].isnan()) and bool(grad[r].isnan().all())
+    finite = torch.ones(rows, dtype=torch.bool, device="cuda")
+    finite[8:11] = False
+    assert bool(torch.isfinite(loss[finite]).all()) and bool(torch.isfinite(grad[finite]).all())
+    alone, stats = ag.distill_loss(z, t, cls, **args)
+    assert sharp(alone, loss)                                # the same sums, with and without a gradient
+    ref.within(ag.distill_grad(z, t, cls, stats, **args)[some], G, eG, "gradient from the statistics")
+    over, same = ag.distill_loss_grad(z, t, cls, out=z, **args)
+    assert same is z and sharp(over, loss) and sharp(z, grad)
+
+
+@pytest.mark.parametrize("k", [65, 128, 129, 300, 1024])
+@pytest.mark.parametrize("rows,C", [(5, 100), (5, 700), (520, 4099), (5, 5000), (3, 70001)])
+def test_many_teacher_entries(ag, rows, C, k):
+    """Up to the limit of entries, more than classes included: the classes then recur."""
+    z, t, cls, y, w = make(rows, C, 4, F32, seed=19)
+    g = torch.Generator().manual_seed(20)
+    cls = torch.randint(-2, C + 2, (rows, k), generator=g)
+    t = 3 * torch.randn(rows, k, generator=g)
+    cls[0, 1:] = -1
+    cls, t = cls.int().cuda(), t.cuda()
+    some = list(range(min(rows, 5))) + [rows - 1]
+    args = dict(temperature=2.5, soft=0.6, hard=0.4)
+    L, eL, G, eG = ref.distill(z[some], t[some], cls[some], y[some], w[some], **args)
+    loss, grad = ag.distill_loss_grad(z, t, cls, labels=y, weight=w, **args)
+    ref.within(loss[some], L, eL, "loss")
+    ref.within(grad[some], G, eG, "gradient")
+    alone, stats = ag.distill_loss(z, t, cls, labels=y, weight=w, **args)
+    assert sharp(alone, loss)
+    ref.within(ag.distill_grad(z, t, cls, stats, labels=y, weight=w, **args)[some], G, eG, "from the statistics")
+
+
+@pytest.mark.parametrize("rows,C,k", [(64, 47, 8), (9, 700, 20), (3, 1024, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
+def test_entry_points_agree(ag, rows, C, k, dtype, T):
+    """Rows of a wave's lanes: one kernel serves all three entry points, and float32 statistics lose nothing."""
+    z, t, cls, y, w = make(rows, C, k, dtype, seed=21)
+    args = dict(labels=y, weight=w, temperature=T, soft=0.5, hard=0.5)
+    loss, grad = ag.distill_loss_grad(z, t, cls, **args)
+    alone, stats = ag.distill_loss(z, t, cls, **args)
+    assert sharp(alone, loss) and sharp(ag.distill_grad(z, t, cls, stats, **args), grad)
