@@ -17,3 +17,9 @@ def test_distill_nodes():
     # K products are independent: far below one in the sum
     assert 0 < r["error_4bit"] < 0.5
     assert distill_nodes.main(SMALL)["first_loss"] == r["first_loss"]
+
+
+def test_distill_nodes_two_runs_agree_to_the_end():
+    """Sums in a fixed order, products and updates of distinct rows: every figure of a second run is the first's."""
+    from examples import distill_nodes
+    assert distill_nodes.main(SMALL) == distill_nodes.main(SMALL)
