@@ -422,3 +422,16 @@ def test_entry_points_agree(ag, rows, C, k, dtype, T):
     loss, grad = ag.distill_loss_grad(z, t, cls, **args)
     alone, stats = ag.distill_loss(z, t, cls, **args)
     assert sharp(alone, loss) and sharp(ag.distill_grad(z, t, cls, stats, **args), grad)
+
+
+@pytest.mark.parametrize("rows,C,k", [(5, 1000, 16), (3, 4097, 20), (600, 5000, 20), (2, 33000, 64), (1, 100003, 40),
+                                      (20, 100, 100)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("T,hard", [(1.0, 0.0), (2.0, 0.3), (3.0, 0.3)])
+def test_entry_points_agree_across_kernels(ag, rows, C, k, dtype, T, hard):
+    """Also where the gradient from statistics is another kernel's than the gradient with the loss."""
+    z, t, cls, y, w = make(rows, C, k, dtype, seed=23)
+    args = dict(labels=y, weight=w, temperature=T, soft=0.7, hard=hard)
+    loss, grad = ag.distill_loss_grad(z, t, cls, **args)
+    alone, stats = ag.distill_loss(z, t, cls, **args)
+    assert sharp(alone, loss) and sharp(ag.distill_grad(z, t, cls, stats, **args), grad)
