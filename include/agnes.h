@@ -473,7 +473,8 @@ agnes_status agnes_sage_forward_noalloc(agnes_batch* batch, const agnes_sage_mod
 /* A row-major matrix: element (i, j) is data[i * stride + j] (stride in
  * elements, not bytes).  An input's rows may overlap (stride >= 0; 0 = one row
  * for all); an output needs stride >= cols.  data needs only its element
- * type's own alignment; it may be NULL when rows * cols is 0. */
+ * type's own alignment; it may be NULL when rows * cols is 0.  An output may
+ * not overlap an input, unless the call says so. */
 typedef struct {
     void* data;
     int64_t rows;
@@ -495,7 +496,7 @@ agnes_status agnes_embedding_lookup(const agnes_matrix* table, const void* ids, 
  * summed in float32 and rounded once; padding ids add nothing.  The ids are
  * sorted (stably) and each run of equal ids is summed; long runs are summed in
  * pieces of fixed length that are then added in order.
- * n = grad_out->rows < 2^31, num_rows < 2^31 - 1.
+ * n = grad_out->rows and num_rows below 2^31 - 1.
  *
  * agnes_embedding_grad writes the whole gradient, grad_table [num_rows][dim]:
  * rows that no id names become zero.  With accumulate != 0 the sums are added

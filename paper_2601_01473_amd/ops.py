@@ -9,6 +9,11 @@ With another stream than the current one, outputs and workspace are allocated
 for that stream and the inputs are recorded on it, so their memory is not
 handed out again while the call reads it; ordering the stream after the work
 that makes the inputs is the caller's, as for any stream.
+
+Autograd does not see these calls: a result has no history, also where an input
+requires a gradient.  A backward pass calls embedding_grad or
+embedding_grad_rows and distill_grad or distill_loss_grad itself (or wraps them
+in a torch.autograd.Function); 4-bit products have no backward pass.
 """
 from __future__ import annotations
 
