@@ -457,7 +457,8 @@ agnes_status agnes_sage_forward_noalloc(agnes_batch* batch, const agnes_sage_mod
 /* ---------------------------------------------------------------------------
  * Operators of a training or serving step beside the hyperbatch path: rows of a
  * learned table for the sampled nodes and their gradient, the loss against a
- * teacher's top logits, and 4-bit products for a frozen model.
+ * teacher's top logits, the policy loss of drawn actions, 4-bit and 8-bit
+ * products for a frozen model, and layers' inputs kept in 8 bits for training.
  *
  * Shared conventions: every pointer is device memory of the current device
  * unless said otherwise; every call enqueues on hip_stream and returns without
@@ -586,6 +587,63 @@ agnes_status agnes_distill_grad(const agnes_distill* d, const float* stats, cons
 agnes_status agnes_distill_loss_grad(const agnes_distill* d, float* loss, const agnes_matrix* grad, void* workspace,
                                      uint64_t workspace_bytes, void* hip_stream);
 
+/* The clipped policy loss with a penalty for leaving a reference policy.  Row i
+ * is one decision: C = logits.cols logits z of the classes, the action y that
+ * was drawn, its log-probability old_logp under the policy that drew it, its
+ * advantage A and a weight w; with kl > 0 also the action's log-probability
+ * ref_logp under the reference.  With q = softmax(z / T):
+ *     logp  = ln q_y,   r = exp(logp - old_logp),   d = ref_logp - logp
+ *     L_i   = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl * (exp d - d - 1)
+ *     loss  = w L_i,   grad = w dL_i / dz = w / T * dL_i / dlogp * ([j = y] - q_j)
+ * The first term's derivative by logp is -r A where r A is the smaller (or
+ * equal) one of the two, else 0; a row with A = 0 has no first term.
+ * A row of weight 0, and one whose action lies outside [0, C) (padding), is
+ * skipped: loss 0, logp 0, gradient 0, whatever else the row holds.  Logits may
+ * be -inf (classes that are not allowed: q = 0, gradient 0).  A row whose
+ * action's logit is -inf, also one whose logits are all -inf, has logp = -inf,
+ * r = 0, an infinite last term (with kl > 0) and the gradient 0.  NaN or +inf
+ * logits make the row's loss, logp and gradient NaN.  The row's largest logit and the
+ * sum of exp((z - m) / T) are float32; what follows from them for the row (logp,
+ * r, whether it is clipped, L_i) is computed in 64 bits, the gradient in float32 and
+ * rounded once to its type.
+ *   logits.cols in [1, 2^31 - 2^16).  actions: index_dtype (AGNES_INT32 or
+ *   AGNES_INT64) [rows].  advantage, old_logp: float32 [rows].  ref_logp:
+ *   float32 [rows] (may be NULL with kl = 0).  weight: float32 [rows], or NULL (1).
+ *   temperature > 0 and finite, and so is log2(e) / temperature in float32.
+ *   clip_low in [0, 1], clip_high >= 0, kl >= 0, all finite.
+ * agnes_policy_logprob: logp [rows] alone (how old_logp and ref_logp are made);
+ *   advantage, old_logp and ref_logp are not read and may be NULL.
+ * agnes_policy_loss: loss [rows], logp [rows] and, unless NULL, stats [rows][2]:
+ *   the row's largest logit m and sum exp((z - m) / T); zeros for a skipped row.
+ * agnes_policy_grad: the gradient from those statistics, for the same
+ *   descriptor (weights may differ in rows that were not skipped): as the
+ *   backward pass of per-row losses, weight is the gradient that arrives.
+ * agnes_policy_loss_grad: loss, logp and gradient in one pass over the logits.
+ * grad: the logits' shape, any type; it may be the logits' own memory (same
+ *   data, stride and type).  Errors: INVALID. */
+typedef struct {
+    agnes_matrix logits;
+    const void* actions;
+    agnes_dtype index_dtype;
+    const float* advantage;
+    const float* old_logp;
+    const float* ref_logp;
+    const float* weight;
+    float temperature;
+    float clip_low;
+    float clip_high;
+    float kl;
+} agnes_policy;
+
+agnes_status agnes_policy_bytes(int64_t rows, int64_t classes, uint64_t* bytes);
+agnes_status agnes_policy_logprob(const agnes_policy* p, float* logp, void* workspace, uint64_t workspace_bytes,
+                                  void* hip_stream);
+agnes_status agnes_policy_loss(const agnes_policy* p, float* loss, float* logp, float* stats, void* workspace,
+                               uint64_t workspace_bytes, void* hip_stream);
+agnes_status agnes_policy_grad(const agnes_policy* p, const float* stats, const agnes_matrix* grad, void* hip_stream);
+agnes_status agnes_policy_loss_grad(const agnes_policy* p, float* loss, float* logp, const agnes_matrix* grad,
+                                    void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
 /* Microscaled 4-bit floating point (the MXFP4 format of the OCP Microscaling
  * specification): a row of cols elements is cut into blocks of 32 (the last
  * one padded with zeros); a block has one scale, 2^(code - 127) as a byte,
@@ -621,6 +679,95 @@ agnes_status agnes_mx4_product(const agnes_mx4* x, const agnes_mx4* w, const flo
 agnes_status agnes_mx4_linear_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
 agnes_status agnes_mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const float* bias, int32_t relu,
                               const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Rows in 8-bit integers with one scale each: element (i, j) stands for
+ * scales[i] * codes[i][j].
+ *   codes: [rows][16 * ceil(cols / 16)] bytes, zeros behind column cols; 16-byte
+ *     aligned.   scales: float32 [rows].
+ * Quantisation: scale = max|x| times the float32 next to 1 / 127, rounded to
+ * float32; code = x / scale (the quotient of these two float32 numbers, not
+ * rounded before) rounded to nearest, ties to even, magnitudes above 127 to 127.  A row of zeros, or of
+ * numbers so small that the scale is 0, has codes 0.  A row with an infinity or
+ * NaN has the scale NaN: all its values are NaN, and so is every product that takes part in it. */
+typedef struct {
+    int8_t* codes;
+    float* scales;
+    int64_t rows;
+    int64_t cols;
+} agnes_int8;
+
+/* x -> q and q -> x (equal shapes; values are computed in float32 and rounded
+ * once).  Errors: INVALID. */
+agnes_status agnes_int8_quantize(const agnes_matrix* x, const agnes_int8* q, void* hip_stream);
+agnes_status agnes_int8_dequantize(const agnes_int8* q, const agnes_matrix* x, void* hip_stream);
+
+/* out[M][N] = x[M][K] w[N][K]^T + bias, then max(., 0) with relu != 0 (NaN
+ * stays NaN).  The sums over K are whole numbers, exact in 32 bits; then, in
+ * float32, sum * x's scale * w's scale + bias, rounded once to out's type.
+ * bias: float32 [N] or NULL.  agnes_int8_linear quantises its float rows x
+ * first; w is laid out once by agnes_int8_quantize (a scale for each output
+ * column).  M, N < 2^31, K < 2^17.  Errors: INVALID, RANGE (more than 2^23 - 8
+ * tiles, which are 16 columns of out for up to 32 rows of x, and 256 x 256
+ * elements of out for many; nothing is enqueued then). */
+agnes_status agnes_int8_product_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
+agnes_status agnes_int8_product(const agnes_int8* x, const agnes_int8* w, const float* bias, int32_t relu,
+                                const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+agnes_status agnes_int8_linear_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
+agnes_status agnes_int8_linear(const agnes_matrix* x, const agnes_int8* w, const float* bias, int32_t relu,
+                               const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Microscaled 8-bit integers (the MXINT8 format of the OCP Microscaling
+ * specification), for what a layer keeps of its input until the backward pass:
+ * a row is cut into blocks of 32 elements (the last one padded with zeros); a
+ * block has one scale, 2^(code - 127) as a byte, and 32 whole numbers, in
+ * units of 1/64 of the scale.
+ *   codes: [rows][32 * ceil(cols / 32)] bytes, two's complement; 16-byte
+ *     aligned.   scales: [rows][ceil(cols / 32)] bytes.
+ * Quantisation: scale = 2^floor(log2 max|x|), not below 2^-127; code = 64 x /
+ * scale rounded to nearest, ties to even, magnitudes above 127 to 127.  A block
+ * with an infinity or NaN has the scale code 255: all its values are NaN. */
+typedef struct {
+    int8_t* codes;
+    uint8_t* scales;
+    int64_t rows;
+    int64_t cols;
+} agnes_mx8;
+
+/* x -> q and q -> x (equal shapes).  Errors: INVALID. */
+agnes_status agnes_mx8_quantize(const agnes_matrix* x, const agnes_mx8* q, void* hip_stream);
+agnes_status agnes_mx8_dequantize(const agnes_mx8* q, const agnes_matrix* x, void* hip_stream);
+
+/* An activation that keeps its input in 8 bits for the backward pass.
+ *   AGNES_SILU: act(x) = x / (1 + exp(-x));  AGNES_GELU: act(x) = x Phi(x), Phi
+ *   the normal distribution (no approximation by tanh).
+ * agnes_mx8_activation: y = act(x), or with gated != 0 and x [rows][2 F]:
+ *   y = act(x[:, 0..F-1]) * x[:, F..2F-1]; kept receives x in 8 bits (kept may be
+ *   NULL: y alone).  One pass over x, or two where gated halves meet inside a block
+ *   (F not a multiple of 32).
+ * agnes_mx8_activation_grad: grad_x from grad_y and the kept values k:
+ *   grad_y * act'(k), or with gated != 0  [grad_y * b * act'(a), grad_y * act(a)]
+ *   for k = [a, b].  A block of NaN gives NaN.
+ * All in float32, rounded once.  Types may differ.  Errors: INVALID. */
+typedef enum { AGNES_SILU = 0, AGNES_GELU = 1 } agnes_act;
+
+agnes_status agnes_mx8_activation(const agnes_matrix* x, agnes_act act, int32_t gated, const agnes_matrix* y,
+                                  const agnes_mx8* kept, void* hip_stream);
+agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int32_t gated, const agnes_matrix* grad_y,
+                                       const agnes_matrix* grad_x, void* hip_stream);
+
+/* Gradient of a linear layer's weight from its input as it was kept: with
+ * grad_out [M][N] and kept [M][K],
+ *     grad_weight[N][K] = grad_out^T kept,   grad_bias[n] = sum over rows of grad_out[.][n]
+ * (grad_bias: float32 [N], or NULL).  Kept values are exact in bfloat16 and
+ * grad_out enters as one, two or three bfloat16 (bfloat16, float16, float32) that add up to
+ * it, so that every product is exact; sums are float32, in an order that the sizes alone
+ * decide, and grad_weight is rounded once.  accumulate != 0: the sums are added
+ * (in float32) to what grad_weight and grad_bias hold.  M = 0 gives zeros.
+ * M, N, K < 2^31; errors: INVALID, RANGE (more than 2^23 - 8 tiles of 256 x 256 elements of grad_weight). */
+agnes_status agnes_mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
+agnes_status agnes_mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, int32_t accumulate,
+                                   const agnes_matrix* grad_weight, float* grad_bias, void* workspace,
+                                   uint64_t workspace_bytes, void* hip_stream);
 
 /* Store facts: out[0] num_nodes, out[1] num_edges, out[2] topology blocks,
  * out[3] edges per topology block, out[4] feature blocks, out[5] rows per

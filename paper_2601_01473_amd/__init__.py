@@ -13,8 +13,12 @@ Operators of the step that follows (ops.py), on torch CUDA tensors: rows of a
 learned table for a batch's nodes and their gradient (embedding_lookup,
 embedding_grad, embedding_grad_rows, Batch.embedding, Batch.embedding_grad_rows),
 the loss against a teacher's top logits with its gradient (distill_loss,
-distill_grad, distill_loss_grad), and products with 4-bit weights
-(mx4_quantize, mx4_dequantize, mx4_linear).
+distill_grad, distill_loss_grad), the clipped policy loss of drawn actions with
+its gradient (policy_logprob, policy_loss, policy_grad, policy_loss_grad),
+products with 4-bit weights (mx4_quantize, mx4_dequantize, mx4_linear) and with
+8-bit weights (int8_quantize, int8_dequantize, int8_linear), and layers' inputs
+kept in 8 bits for the backward pass (mx8_quantize, mx8_dequantize,
+mx8_activation, mx8_activation_grad, mx8_weight_grad).
 """
 from __future__ import annotations
 
@@ -34,6 +38,9 @@ from ._binding import agnes_build_blocks_cached, agnes_philox4x64_10, agnes_set_
 from . import ops
 from .ops import Mx4, distill_grad, distill_loss, distill_loss_grad, embedding_grad  # noqa: F401
 from .ops import embedding_grad_rows, embedding_lookup, mx4_dequantize, mx4_linear, mx4_quantize  # noqa: F401
+from .ops import Int8, Mx8, int8_dequantize, int8_linear, int8_quantize, mx8_activation  # noqa: F401
+from .ops import mx8_activation_grad, mx8_dequantize, mx8_quantize, mx8_weight_grad, policy_grad  # noqa: F401
+from .ops import policy_logprob, policy_loss, policy_loss_grad  # noqa: F401
 
 _FEAT_DTYPES = {np.dtype(np.float32): B.AGNES_FLOAT32, np.dtype(np.float16): B.AGNES_FLOAT16}
 

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libagnes.san.so" if os.environ.get("AGNES_SANITI
 AGNES_OK, AGNES_ERR_INVALID, AGNES_ERR_NOMEM, AGNES_ERR_DEVICE, AGNES_ERR_RANGE, AGNES_ERR_INTERNAL = range(6)
 STATUS_NAMES = {0: "OK", 1: "INVALID", 2: "NOMEM", 3: "DEVICE", 4: "RANGE", 5: "INTERNAL"}
 AGNES_INT32, AGNES_INT64, AGNES_FLOAT32, AGNES_FLOAT16, AGNES_BFLOAT16 = range(5)
+AGNES_SILU, AGNES_GELU = range(2)
 AGNES_MAX_LAYERS = 8
 AGNES_OPT_PROFILE = 1
 AGNES_OPT_GATHER_GROUPS = 2
@@ -34,7 +35,12 @@ EXPORTED = ["agnes_build_blocks", "agnes_build_blocks_staged", "agnes_build_bloc
             "agnes_embedding_grad_rows", "agnes_batch_embedding_lookup", "agnes_batch_embedding_grad_rows",
             "agnes_distill_bytes", "agnes_distill_loss", "agnes_distill_grad", "agnes_distill_loss_grad",
             "agnes_mx4_quantize", "agnes_mx4_dequantize", "agnes_mx4_product_bytes", "agnes_mx4_product",
-            "agnes_mx4_linear_bytes", "agnes_mx4_linear"]
+            "agnes_mx4_linear_bytes", "agnes_mx4_linear",
+            "agnes_policy_bytes", "agnes_policy_logprob", "agnes_policy_loss", "agnes_policy_grad",
+            "agnes_policy_loss_grad", "agnes_int8_quantize", "agnes_int8_dequantize", "agnes_int8_product_bytes",
+            "agnes_int8_product", "agnes_int8_linear_bytes", "agnes_int8_linear", "agnes_mx8_quantize",
+            "agnes_mx8_dequantize", "agnes_mx8_activation", "agnes_mx8_activation_grad",
+            "agnes_mx8_weight_grad_bytes", "agnes_mx8_weight_grad"]
 
 # void* alloc(uint64_t bytes, void* user); void release(void* ptr, uint64_t bytes, void* user)
 DEVICE_ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p)
@@ -104,6 +110,23 @@ class agnes_mx4(ctypes.Structure):
                 ("cols", ctypes.c_int64)]
 
 
+class agnes_policy(ctypes.Structure):
+    _fields_ = [("logits", agnes_matrix), ("actions", ctypes.c_void_p), ("index_dtype", ctypes.c_int),
+                ("advantage", ctypes.c_void_p), ("old_logp", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("temperature", ctypes.c_float), ("clip_low", ctypes.c_float),
+                ("clip_high", ctypes.c_float), ("kl", ctypes.c_float)]
+
+
+class agnes_int8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
+class agnes_mx8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
 class AgnesError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__("%s: %s" % (STATUS_NAMES.get(status, status), msg))
@@ -166,6 +189,7 @@ def lib():
     L.agnes_set_device_allocator.argtypes = [DEVICE_ALLOC_FN, DEVICE_FREE_FN, vp]
     mat, mx, dis, f32, u64p = (ctypes.POINTER(agnes_matrix), ctypes.POINTER(agnes_mx4),
                                ctypes.POINTER(agnes_distill), ctypes.c_float, ctypes.POINTER(u64))
+    pol, i8, m8 = ctypes.POINTER(agnes_policy), ctypes.POINTER(agnes_int8), ctypes.POINTER(agnes_mx8)
     for name, args in (
             ("agnes_embedding_lookup", [mat, vp, st, f32, mat, vp]),
             ("agnes_embedding_grad_bytes", [i64, i64, i64, u64p]),
@@ -182,7 +206,24 @@ def lib():
             ("agnes_mx4_product_bytes", [i64, i64, i64, u64p]),
             ("agnes_mx4_product", [mx, mx, vp, i32, mat, vp, u64, vp]),
             ("agnes_mx4_linear_bytes", [i64, i64, i64, u64p]),
-            ("agnes_mx4_linear", [mat, mx, vp, i32, mat, vp, u64, vp])):
+            ("agnes_mx4_linear", [mat, mx, vp, i32, mat, vp, u64, vp]),
+            ("agnes_policy_bytes", [i64, i64, u64p]),
+            ("agnes_policy_logprob", [pol, vp, vp, u64, vp]),
+            ("agnes_policy_loss", [pol, vp, vp, vp, vp, u64, vp]),
+            ("agnes_policy_grad", [pol, vp, mat, vp]),
+            ("agnes_policy_loss_grad", [pol, vp, vp, mat, vp, u64, vp]),
+            ("agnes_int8_quantize", [mat, i8, vp]),
+            ("agnes_int8_dequantize", [i8, mat, vp]),
+            ("agnes_int8_product_bytes", [i64, i64, i64, u64p]),
+            ("agnes_int8_product", [i8, i8, vp, i32, mat, vp, u64, vp]),
+            ("agnes_int8_linear_bytes", [i64, i64, i64, u64p]),
+            ("agnes_int8_linear", [mat, i8, vp, i32, mat, vp, u64, vp]),
+            ("agnes_mx8_quantize", [mat, m8, vp]),
+            ("agnes_mx8_dequantize", [m8, mat, vp]),
+            ("agnes_mx8_activation", [mat, ctypes.c_int, i32, mat, m8, vp]),
+            ("agnes_mx8_activation_grad", [m8, ctypes.c_int, i32, mat, mat, vp]),
+            ("agnes_mx8_weight_grad_bytes", [i64, i64, i64, u64p]),
+            ("agnes_mx8_weight_grad", [mat, m8, i32, mat, vp, vp, u64, vp])):
         getattr(L, name).restype = st
         getattr(L, name).argtypes = args
     L.agnes_free.restype = None
@@ -422,3 +463,83 @@ def agnes_mx4_linear(x: agnes_matrix, w: agnes_mx4, bias, relu: int, out: agnes_
                      workspace_bytes: int, stream: int = 0) -> None:
     check(lib().agnes_mx4_linear(ctypes.byref(x), ctypes.byref(w), bias, relu, ctypes.byref(out), workspace,
                                  workspace_bytes, stream))
+
+
+def agnes_policy_bytes(rows: int, classes: int) -> int:
+    return _bytes(lib().agnes_policy_bytes, rows, classes)
+
+
+def agnes_policy_logprob(p: agnes_policy, logp, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_policy_logprob(ctypes.byref(p), logp, workspace, workspace_bytes, stream))
+
+
+def agnes_policy_loss(p: agnes_policy, loss, logp, stats, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_policy_loss(ctypes.byref(p), loss, logp, stats, workspace, workspace_bytes, stream))
+
+
+def agnes_policy_grad(p: agnes_policy, stats, grad: agnes_matrix, stream: int = 0) -> None:
+    check(lib().agnes_policy_grad(ctypes.byref(p), stats, ctypes.byref(grad), stream))
+
+
+def agnes_policy_loss_grad(p: agnes_policy, loss, logp, grad: agnes_matrix, workspace, workspace_bytes: int,
+                           stream: int = 0) -> None:
+    check(lib().agnes_policy_loss_grad(ctypes.byref(p), loss, logp, ctypes.byref(grad), workspace, workspace_bytes,
+                                       stream))
+
+
+def agnes_int8_quantize(x: agnes_matrix, q: agnes_int8, stream: int = 0) -> None:
+    check(lib().agnes_int8_quantize(ctypes.byref(x), ctypes.byref(q), stream))
+
+
+def agnes_int8_dequantize(q: agnes_int8, x: agnes_matrix, stream: int = 0) -> None:
+    check(lib().agnes_int8_dequantize(ctypes.byref(q), ctypes.byref(x), stream))
+
+
+def agnes_int8_product_bytes(M: int, N: int, K: int) -> int:
+    return _bytes(lib().agnes_int8_product_bytes, M, N, K)
+
+
+def agnes_int8_product(x: agnes_int8, w: agnes_int8, bias, relu: int, out: agnes_matrix, workspace,
+                       workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_int8_product(ctypes.byref(x), ctypes.byref(w), bias, relu, ctypes.byref(out), workspace,
+                                   workspace_bytes, stream))
+
+
+def agnes_int8_linear_bytes(M: int, N: int, K: int) -> int:
+    return _bytes(lib().agnes_int8_linear_bytes, M, N, K)
+
+
+def agnes_int8_linear(x: agnes_matrix, w: agnes_int8, bias, relu: int, out: agnes_matrix, workspace,
+                      workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_int8_linear(ctypes.byref(x), ctypes.byref(w), bias, relu, ctypes.byref(out), workspace,
+                                  workspace_bytes, stream))
+
+
+def agnes_mx8_quantize(x: agnes_matrix, q: agnes_mx8, stream: int = 0) -> None:
+    check(lib().agnes_mx8_quantize(ctypes.byref(x), ctypes.byref(q), stream))
+
+
+def agnes_mx8_dequantize(q: agnes_mx8, x: agnes_matrix, stream: int = 0) -> None:
+    check(lib().agnes_mx8_dequantize(ctypes.byref(q), ctypes.byref(x), stream))
+
+
+def agnes_mx8_activation(x: agnes_matrix, act: int, gated: int, y: agnes_matrix, kept: agnes_mx8 | None,
+                         stream: int = 0) -> None:
+    check(lib().agnes_mx8_activation(ctypes.byref(x), act, gated, ctypes.byref(y),
+                                     None if kept is None else ctypes.byref(kept), stream))
+
+
+def agnes_mx8_activation_grad(kept: agnes_mx8, act: int, gated: int, grad_y: agnes_matrix, grad_x: agnes_matrix,
+                              stream: int = 0) -> None:
+    check(lib().agnes_mx8_activation_grad(ctypes.byref(kept), act, gated, ctypes.byref(grad_y), ctypes.byref(grad_x),
+                                          stream))
+
+
+def agnes_mx8_weight_grad_bytes(M: int, N: int, K: int) -> int:
+    return _bytes(lib().agnes_mx8_weight_grad_bytes, M, N, K)
+
+
+def agnes_mx8_weight_grad(grad_out: agnes_matrix, kept: agnes_mx8, accumulate: int, grad_weight: agnes_matrix,
+                          grad_bias, workspace, workspace_bytes: int, stream: int = 0) -> None:
+    check(lib().agnes_mx8_weight_grad(ctypes.byref(grad_out), ctypes.byref(kept), accumulate,
+                                      ctypes.byref(grad_weight), grad_bias, workspace, workspace_bytes, stream))

@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libagnes.san.so" if SANITIZE else "libagnes.so")
 if SANITIZE:
     BUILD = os.path.join(HERE, "_build_san")
 SOURCES = ["prims.hip", "store.hip", "pipeline.hip", "bucket.hip", "bitmap.hip", "sage.hip", "embed.hip",
-           "distill.hip", "mx4.hip", "api.hip"]
+           "distill.hip", "mx4.hip", "policy.hip", "int8.hip", "mx8.hip", "api.hip"]
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.environ.get("HIPCC", os.path.join(ROCM, "bin", "hipcc"))
 ARCH = "gfx950"

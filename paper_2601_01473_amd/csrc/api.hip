@@ -522,6 +522,107 @@ agnes_status agnes_mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const f
     });
 }
 
+agnes_status agnes_policy_bytes(int64_t rows, int64_t classes, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = policy_bytes(rows, classes);
+    });
+}
+
+agnes_status agnes_policy_logprob(const agnes_policy* p, float* logp, void* workspace, uint64_t workspace_bytes,
+                                  void* hip_stream) {
+    return guarded([&] { policy_logprob(p, logp, workspace, workspace_bytes, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_policy_loss(const agnes_policy* p, float* loss, float* logp, float* stats, void* workspace,
+                               uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        policy_loss(p, loss, logp, stats, nullptr, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_policy_grad(const agnes_policy* p, const float* stats, const agnes_matrix* grad, void* hip_stream) {
+    return guarded([&] { policy_grad(p, stats, grad, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_policy_loss_grad(const agnes_policy* p, float* loss, float* logp, const agnes_matrix* grad,
+                                    void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        AGNES_REQUIRE(grad, AGNES_ERR_INVALID, "grad must not be NULL");
+        policy_loss(p, loss, logp, nullptr, grad, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_int8_quantize(const agnes_matrix* x, const agnes_int8* q, void* hip_stream) {
+    return guarded([&] { int8_quantize(x, q, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_int8_dequantize(const agnes_int8* q, const agnes_matrix* x, void* hip_stream) {
+    return guarded([&] { int8_dequantize(q, x, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_int8_product_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = int8_product_bytes(M, N, K);
+    });
+}
+
+agnes_status agnes_int8_product(const agnes_int8* x, const agnes_int8* w, const float* bias, int32_t relu,
+                                const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        int8_product(x, w, bias, relu != 0, out, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_int8_linear_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = int8_linear_bytes(M, N, K);
+    });
+}
+
+agnes_status agnes_int8_linear(const agnes_matrix* x, const agnes_int8* w, const float* bias, int32_t relu,
+                               const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        int8_linear(x, w, bias, relu != 0, out, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    });
+}
+
+agnes_status agnes_mx8_quantize(const agnes_matrix* x, const agnes_mx8* q, void* hip_stream) {
+    return guarded([&] { mx8_quantize(x, q, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_mx8_dequantize(const agnes_mx8* q, const agnes_matrix* x, void* hip_stream) {
+    return guarded([&] { mx8_dequantize(q, x, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_mx8_activation(const agnes_matrix* x, agnes_act act, int32_t gated, const agnes_matrix* y,
+                                  const agnes_mx8* kept, void* hip_stream) {
+    return guarded([&] { mx8_activation(x, act, gated != 0, y, kept, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int32_t gated, const agnes_matrix* grad_y,
+                                       const agnes_matrix* grad_x, void* hip_stream) {
+    return guarded([&] { mx8_activation_grad(kept, act, gated != 0, grad_y, grad_x, (hipStream_t)hip_stream); });
+}
+
+agnes_status agnes_mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes) {
+    return guarded([&] {
+        AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
+        *bytes = mx8_weight_grad_bytes(M, N, K);
+    });
+}
+
+agnes_status agnes_mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, int32_t accumulate,
+                                   const agnes_matrix* grad_weight, float* grad_bias, void* workspace,
+                                   uint64_t workspace_bytes, void* hip_stream) {
+    return guarded([&] {
+        mx8_weight_grad(grad_out, kept, accumulate != 0, grad_weight, grad_bias, workspace, workspace_bytes,
+                        (hipStream_t)hip_stream);
+    });
+}
+
 void agnes_free(void* handle) {
     if (!handle) return;
     uint32_t magic = *static_cast<uint32_t*>(handle);

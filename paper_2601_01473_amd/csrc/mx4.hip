@@ -56,34 +56,12 @@ __device__ __forceinline__ uint32_t top_bits(const float (&x)[8]) {
     return top;
 }
 
-// Eight elements from column c of a row on, zeros behind its end.
-template <typename T> __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, float (&x)[8]) {
-    if (c + 8 <= cols) {
-        Vec<T, 8>::load(row + c, x);
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; q++) x[q] = c + q < cols ? to_float(row[c + q]) : 0.f;
-    }
-}
-
 // ----------------------------------------------------------------- quantisation
 
 // A piece is 8 elements, a block four pieces in adjacent lanes.  Pieces are
 // numbered row after row; a workgroup takes kPieces rounds of 256, all loads
 // first.  Bound by memory: 65536 x 1024 bfloat16 to codes 40 us (4.3 TB/s), and
 // back 27 us (6.4 TB/s).
-constexpr int kPieces = 4;
-
-struct PieceAt {
-    int64_t row;
-    int32_t piece;
-};
-// Piece i of rows of `per_row` pieces; base: the workgroup's first piece.
-__device__ __forceinline__ PieceAt piece_at(int64_t base_row, uint32_t base_piece, uint32_t off, uint32_t per_row) {
-    const uint32_t x = base_piece + off;           // both below 2^30
-    return {base_row + x / per_row, (int32_t)(x % per_row)};
-}
-
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_mx4_quantize(const T* __restrict__ x, int64_t stride, int64_t pieces,
                                                          int64_t cols, uint32_t per_row, uint8_t* __restrict__ codes,
@@ -188,21 +166,8 @@ __device__ __forceinline__ float finish(float y, float bias, bool relu) {
     return relu && y < 0.f ? 0.f : y;
 }
 
-template <auto N> struct Const { static constexpr auto value = N; };
-template <int N, int I = 0, typename F> __device__ __forceinline__ void static_for(F&& f) {
-    if constexpr (I < N) {
-        f(Const<I>{});
-        static_for<N, I + 1>(f);
-    }
-}
-
 // Sixteen zero bytes: blocks behind the last one of a row.
 static __device__ const uint4 k_mx4_zero = {0u, 0u, 0u, 0u};
-
-constexpr int kVmcnt0 = 0x0F70;                    // s_waitcnt vmcnt(0) and nothing else
-
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
 
 // A workgroup of WM x WN waves computes a tile of out, a wave 16 F x 16 G of it,
 // in steps of 256 k: 128 bytes per row, a whole cache line.  (8192^3: 293 us, 3.75
@@ -611,19 +576,6 @@ static void check_mx4(const agnes_mx4* q, const char* name) {
     if (q->rows == 0 || q->cols == 0) return;
     AGNES_REQUIRE(q->codes && q->scales, AGNES_ERR_INVALID, n + ": codes and scales must not be NULL");
     AGNES_REQUIRE(((uintptr_t)q->codes & 15) == 0, AGNES_ERR_INVALID, n + ": codes must be 16-byte aligned");
-}
-
-// Calls launch(first row, pieces, workgroups) for parts of `rows` rows of
-// per_row <= 2^28 pieces, each of at most kLaunchGroups workgroups: a launch
-// holds fewer than 2^32 threads.
-constexpr int64_t kLaunchGroups = 1 << 22;
-template <typename F> static void launch_pieces(int64_t rows, int64_t per_row, F&& launch) {
-    constexpr int64_t kGroup = kBlock * kPieces;
-    const int64_t most = kLaunchGroups * kGroup / per_row;
-    for (int64_t r = 0; r < rows; r += most) {
-        const int64_t n = std::min(most, rows - r), pieces = n * per_row;
-        launch(r, pieces, (unsigned)((pieces + kGroup - 1) / kGroup));
-    }
 }
 
 void mx4_quantize(const agnes_matrix* x, const agnes_mx4* q, hipStream_t st) {

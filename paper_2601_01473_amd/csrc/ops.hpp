@@ -1,7 +1,9 @@
-// What the operator kernels (embed.hip, distill.hip, mx4.hip) share: element
-// types, vector accesses at element alignment, argument checks and the host
+// What the operator kernels (embed.hip, distill.hip, mx4.hip, policy.hip,
+// int8.hip, mx8.hip) share: element types, vector accesses at element alignment, argument checks and the host
 // entry points that api.hip wraps.
 #pragma once
+
+#include <algorithm>
 
 #include "device.hpp"
 #include "runtime.hpp"
@@ -80,6 +82,48 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// ----------------------------------------------------------------- pieces of rows
+
+// Eight elements from column c of a row on, zeros behind its end.
+template <typename T> __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, float (&x)[8]) {
+    if (c + 8 <= cols) {
+        Vec<T, 8>::load(row + c, x);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; q++) x[q] = c + q < cols ? to_float(row[c + q]) : 0.f;
+    }
+}
+
+// Pieces of 8 elements are numbered row after row; a workgroup takes kPieces
+// rounds of kBlock of them.
+constexpr int kPieces = 4;
+
+struct PieceAt {
+    int64_t row;
+    int32_t piece;
+};
+// Piece i of rows of `per_row` pieces; base: the workgroup's first piece.
+__device__ __forceinline__ PieceAt piece_at(int64_t base_row, uint32_t base_piece, uint32_t off, uint32_t per_row) {
+    const uint32_t x = base_piece + off;           // both below 2^30
+    return {base_row + x / per_row, (int32_t)(x % per_row)};
+}
+
+// ----------------------------------------------------------------- tiles
+
+// f(Const<0>{}), f(Const<1>{}), ..: indices that are constants.
+template <auto N> struct Const { static constexpr auto value = N; };
+template <int N, int I = 0, typename F> __device__ __forceinline__ void static_for(F&& f) {
+    if constexpr (I < N) {
+        f(Const<I>{});
+        static_for<N, I + 1>(f);
+    }
+}
+
+constexpr int kVmcnt0 = 0x0F70;                    // s_waitcnt vmcnt(0) and nothing else
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
 // ----------------------------------------------------------------- host side
 
 inline size_t elem_size(agnes_dtype t) { return t == AGNES_FLOAT32 ? 4 : 2; }
@@ -100,6 +144,19 @@ template <typename F> void with_float(agnes_dtype t, F&& f) {
 template <typename F> void with_index(agnes_dtype t, F&& f) {
     if (t == AGNES_INT64) f(int64_t{});
     else f(int32_t{});
+}
+
+// Calls launch(first row, pieces, workgroups) for parts of `rows` rows of
+// per_row <= 2^28 pieces, each of at most kLaunchGroups workgroups: a launch
+// holds fewer than 2^32 threads.
+constexpr int64_t kLaunchGroups = 1 << 22;
+template <typename F> void launch_pieces(int64_t rows, int64_t per_row, F&& launch) {
+    constexpr int64_t kGroup = kBlock * kPieces;
+    const int64_t most = kLaunchGroups * kGroup / per_row;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = std::min(most, rows - r), pieces = n * per_row;
+        launch(r, pieces, (unsigned)((pieces + kGroup - 1) / kGroup));
+    }
 }
 
 void check_matrix(const agnes_matrix* m, bool output, const char* name);
@@ -145,5 +202,30 @@ void mx4_product(const agnes_mx4* x, const agnes_mx4* w, const float* bias, bool
 uint64_t mx4_linear_bytes(int64_t M, int64_t N, int64_t K);
 void mx4_linear(const agnes_matrix* x, const agnes_mx4* w, const float* bias, bool relu, const agnes_matrix* out,
                 void* ws, uint64_t ws_bytes, hipStream_t st);
+
+uint64_t policy_bytes(int64_t rows, int64_t classes);
+void policy_logprob(const agnes_policy* p, float* logp, void* ws, uint64_t ws_bytes, hipStream_t st);
+void policy_loss(const agnes_policy* p, float* loss, float* logp, float* stats, const agnes_matrix* grad, void* ws,
+                 uint64_t ws_bytes, hipStream_t st);
+void policy_grad(const agnes_policy* p, const float* stats, const agnes_matrix* grad, hipStream_t st);
+
+void int8_quantize(const agnes_matrix* x, const agnes_int8* q, hipStream_t st);
+void int8_dequantize(const agnes_int8* q, const agnes_matrix* x, hipStream_t st);
+uint64_t int8_product_bytes(int64_t M, int64_t N, int64_t K);
+void int8_product(const agnes_int8* x, const agnes_int8* w, const float* bias, bool relu, const agnes_matrix* out,
+                  void* ws, uint64_t ws_bytes, hipStream_t st);
+uint64_t int8_linear_bytes(int64_t M, int64_t N, int64_t K);
+void int8_linear(const agnes_matrix* x, const agnes_int8* w, const float* bias, bool relu, const agnes_matrix* out,
+                 void* ws, uint64_t ws_bytes, hipStream_t st);
+
+void mx8_quantize(const agnes_matrix* x, const agnes_mx8* q, hipStream_t st);
+void mx8_dequantize(const agnes_mx8* q, const agnes_matrix* x, hipStream_t st);
+void mx8_activation(const agnes_matrix* x, agnes_act act, bool gated, const agnes_matrix* y, const agnes_mx8* kept,
+                    hipStream_t st);
+void mx8_activation_grad(const agnes_mx8* kept, agnes_act act, bool gated, const agnes_matrix* grad_y,
+                         const agnes_matrix* grad_x, hipStream_t st);
+uint64_t mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K);
+void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool accumulate,
+                     const agnes_matrix* grad_weight, float* grad_bias, void* ws, uint64_t ws_bytes, hipStream_t st);
 
 }  // namespace agnes

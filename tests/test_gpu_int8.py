@@ -1,0 +1,198 @@
+"""8-bit rows and products on the GPU against their definition in 64 bits (tests/more_operators_ref.py)."""
+import pytest
+import torch
+
+from tests import more_operators_ref as ref
+from tests.operators_ref import FLOATS, within
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def ag():
+    import paper_2601_01473_amd as m
+    return m
+
+
+def rows_of(R, K, dtype=F32, seed=1):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(R, K, generator=g) * torch.exp(2 * torch.randn(R, 1, generator=g))).to(dtype).cuda()
+
+
+def same(q, codes, scales):
+    assert torch.equal(q.codes.cpu(), codes)
+    assert torch.equal(q.scales.cpu().nan_to_num(nan=-1.0), scales.nan_to_num(nan=-1.0))
+
+
+@pytest.mark.parametrize("R,K", [(1, 1), (3, 15), (2, 16), (5, 17), (70, 63), (4, 1003), (2, 4096), (3, 8192), (2, 20001),
+                                 (1, 70000), (1000, 33), (300, 2050)])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_quantised_rows_and_back(ag, R, K, dtype):
+    x = rows_of(R, K, dtype)
+    codes, scales = ref.int8(x)
+    q = ag.int8_quantize(x)
+    same(q, codes, scales)
+    values = ref.int8_values(codes, scales, K)
+    for t in FLOATS:
+        within(ag.int8_dequantize(q, t), values, 0.0 * values, "values")
+
+
+def test_ties_and_neighbours(ag):
+    """Quotients at halves and next to them: scales whose reciprocal is rounded, elements at (k + 1/2) scale and one
+    unit in the last place to either side."""
+    g = torch.Generator().manual_seed(3)
+    top = torch.exp(3 * torch.randn(200, generator=g)).float()
+    top[:40] = torch.exp2(torch.arange(40).float() - 20) * 127      # scales that are powers of two: exact ties
+    s = (top.double() * ref.f32(1 / 127)).float()
+    k = torch.randint(-126, 126, (200, 120), generator=g).double()
+    mid = ((k + 0.5) * s.double().unsqueeze(1)).float()
+    x = torch.cat([top.unsqueeze(1), mid, torch.nextafter(mid, torch.tensor(float("inf"))),
+                   torch.nextafter(mid, torch.tensor(float("-inf")))], 1)
+    codes, scales = ref.int8(x)
+    same(ag.int8_quantize(x.cuda()), codes, scales)
+
+
+def test_extreme_rows(ag):
+    x = torch.zeros(16, 50)
+    tiny = 2.0 ** -149
+    x[1, 3] = tiny                                          # the scale is 0
+    x[2] = tiny * torch.arange(50)                          # the scale is a subnormal number or 0
+    x[3] = tiny * 127 * torch.arange(-25, 25)
+    x[4] = tiny * 190 * torch.sign(torch.arange(50) - 25.0)  # a quotient above 127
+    x[5] = 2.0 ** -126 * torch.linspace(-1, 1, 50)
+    x[6] = 2.0 ** -100 * torch.linspace(-127, 127, 50)
+    x[7] = torch.finfo(F32).max * torch.linspace(-1, 1, 50)
+    x[8] = torch.finfo(F32).min
+    x[9, 7], x[10, 49], x[11, 0] = float("nan"), float("inf"), float("-inf")
+    x[12] = -0.0
+    x[13, 0], x[13, 1] = 127.0, 0.5                         # ties to the even code
+    x[14, 0], x[14, 1], x[14, 2] = 127.0, 1.5, -2.5
+    x[15] = torch.linspace(2.0 ** -119, 2.0 ** -92, 50)
+    codes, scales = ref.int8(x)
+    q = ag.int8_quantize(x.cuda())
+    same(q, codes, scales)
+    values = ref.int8_values(codes, scales, 50)
+    within(ag.int8_dequantize(q), values, 0.0 * values)
+    lowest = torch.full((2, 40), torch.finfo(BF16).min, dtype=BF16, device="cuda")
+    same(ag.int8_quantize(lowest), *ref.int8(lowest))
+
+
+def test_strided_rows_and_untouched_memory(ag):
+    wide = torch.randn(9, 100, device="cuda")
+    x = wide[:, 7:70]
+    same(ag.int8_quantize(x), *ref.int8(x))
+    one = wide[:1, :63].expand(9, 63)
+    same(ag.int8_quantize(one), *ref.int8(one))
+    assert ag.int8_quantize(x[:0]).codes.shape == (0, 64)
+    q = ag.int8_quantize(torch.zeros(3, 0, device="cuda"))
+    assert q.codes.shape == (3, 0) and bool((q.scales == 0).all())
+    assert ag.int8_dequantize(q).shape == (3, 0)
+
+
+def check_linear(ag, M, N, K, dtype, out, bias, relu, seed=1):
+    x, w = rows_of(M, K, dtype, seed), rows_of(N, K, F32, seed + 1) / max(K, 1) ** 0.5
+    b = torch.randn(N, device="cuda") if bias else None
+    q = ag.int8_quantize(w)
+    codes, scales = ref.int8(x)
+    y, err = ref.int8_product(codes, scales, q.codes, q.scales, K, b, relu)
+    got = ag.int8_linear(x, q, b, relu=relu, dtype=out)
+    within(got, y, err, "linear %d %d %d" % (M, N, K))
+    got2 = ag.int8_linear(ag.int8_quantize(x), q, b, relu=relu, dtype=out)
+    assert torch.equal(got, got2)
+    return got
+
+
+SIZES = [(1, 1, 1), (1, 16, 64), (1, 1000, 4096), (2, 17, 33), (5, 300, 1000), (16, 64, 128), (17, 100, 2000),
+         (31, 47, 16), (32, 130, 4099), (33, 257, 1024), (61, 515, 2051), (64, 64, 64), (65, 1000, 700), (127, 129, 256),
+         (200, 300, 129), (256, 256, 512), (300, 513, 1024), (700, 600, 96), (1, 40000, 48), (3000, 7, 300), (9, 5, 131071),
+         (2100, 2200, 272)]
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (F16, F32), (BF16, F16)])
+def test_products(ag, M, N, K, dtype, out):
+    check_linear(ag, M, N, K, dtype, out, bias=True, relu=False)
+    check_linear(ag, M, N, K, dtype, out, bias=False, relu=True, seed=5)
+
+
+@pytest.mark.parametrize("K", [100, 300])
+def test_tiles_of_every_kind_over_few_steps(ag, K):
+    for M, N in ((5000, 4900), (3000, 3001), (1100, 1000), (40, 9000), (24, 20000)):
+        check_linear(ag, M, N, K, BF16, BF16, bias=True, relu=False)
+
+
+def test_largest_sums(ag):
+    """All codes 127, and the codes of -128 that no quantisation makes: 2^14 K stays below 2^31."""
+    K = (1 << 17) - 1
+    x = torch.ones(3, K, dtype=BF16, device="cuda")
+    w = ag.int8_quantize(torch.ones(20, K, device="cuda"))
+    got = ag.int8_linear(x, w, dtype=F32)
+    codes, scales = ref.int8(x[:1])
+    y, err = ref.int8_product(codes.expand(3, -1), scales.expand(3), w.codes, w.scales, K, None, False)
+    within(got, y, err)
+    low = ag.Int8(torch.full((20, K + 1), -128, dtype=torch.int8, device="cuda"), torch.ones(20, device="cuda"), K)
+    low.codes[:, K:] = 0
+    got = ag.int8_linear(low, low)
+    assert bool((got == 2.0 ** 14 * K).all())
+
+
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_undefined_rows_stay_in_their_rows(ag, M):
+    x, w = rows_of(M, 200), rows_of(90, 200, seed=2)
+    x[0, 5] = float("nan")
+    w[7, 3] = float("inf")
+    got = ag.int8_linear(x, ag.int8_quantize(w), relu=True)
+    bad = torch.zeros(M, 90, dtype=torch.bool)
+    bad[0] = True
+    bad[:, 7] = True
+    assert torch.equal(torch.isnan(got.cpu()), bad)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 50, 80), (40, 70, 500), (300, 290, 200), (600, 700, 1000)])
+def test_strides_and_untouched_memory(ag, M, N, K):
+    wide = torch.randn(M, K + 11, device="cuda", dtype=BF16)
+    x = wide[:, 3:3 + K]
+    w = ag.int8_quantize(rows_of(N, K))
+    want = ag.int8_linear(x.contiguous(), w)
+    out = torch.full((M + 2, N + 5), 3.0, dtype=BF16, device="cuda")
+    ag.int8_linear(x, w, out=out[1:M + 1, 2:2 + N])
+    assert torch.equal(out[1:M + 1, 2:2 + N], want)
+    out[1:M + 1, 2:2 + N] = 3.0
+    assert bool((out == 3).all())
+    one = x[:1].expand(M, K)
+    assert torch.equal(ag.int8_linear(one, w), want[:1].expand(M, N))
+
+
+def test_empty_products(ag):
+    w = ag.int8_quantize(rows_of(4, 32))
+    assert ag.int8_linear(torch.zeros(0, 32, device="cuda"), w).shape == (0, 4)
+    none = ag.int8_quantize(torch.zeros(4, 0, device="cuda"))
+    b = torch.tensor([1.0, -2.0, 0.0, 3.0], device="cuda")
+    got = ag.int8_linear(torch.zeros(3, 0, device="cuda"), none, b, relu=True)
+    assert got.tolist() == [[1.0, 0.0, 0.0, 3.0]] * 3
+    assert ag.int8_linear(torch.zeros(3, 32, device="cuda"), ag.int8_quantize(torch.zeros(0, 32, device="cuda"))).shape == (3, 0)
+
+
+def test_another_stream_and_replayed_graph(ag):
+    cases = [(1, 500, 1000), (40, 300, 4000), (700, 900, 512)]
+    xs = [rows_of(M, K, BF16) for M, N, K in cases]
+    ws = [ag.int8_quantize(rows_of(N, K, seed=2)) for M, N, K in cases]
+    want = [ag.int8_linear(x, w) for x, w in zip(xs, ws)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = [ag.int8_linear(x, w, stream=s) for x, w in zip(xs, ws)]
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = [ag.int8_linear(x, w) for x, w in zip(xs, ws)]
+    for seed in (11, 12, 13):
+        for x, (M, N, K) in zip(xs, cases):
+            x.copy_(rows_of(M, K, BF16, seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        for o, x, w in zip(outs, xs, ws):
+            assert torch.equal(o, ag.int8_linear(x, w))
