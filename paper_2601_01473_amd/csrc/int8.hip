@@ -209,9 +209,15 @@ static __device__ const uint4 k_int8_zero = {0u, 0u, 0u, 0u};
 // it, in steps of 64 k: one multiplication deep.  Codes go from memory straight
 // to one of four images in LDS, three steps ahead of their use; a wave reads a
 // step's operands into registers while it multiplies the step before.  An
-// image: row after row, 4 chunks each, chunk p of row r at place p ^ (r / 4 % 4):
-// the 16 rows that a wave reads at once then lie in different banks.
+// image: row after row, 4 chunks each, chunk p of row r at place p ^ (-(r / 4) % 4).
+// LDS serves lanes 0-3, 12-15 and 20-27 of a wave together, and so on: these 16
+// then lie in different banks.
+//
+// 8192^3: 431 us, 2550 TOPS, the matrix cores busy two thirds of the cycles, at a
+// clock that falls as they get busier (1.85 GHz): with 32 x 32 x 32
+// multiplications as many cycles take 493 us.
 constexpr int kStepChunks = 4, kImages = 4;
+__device__ __forceinline__ int turn(int r) { return -(r / 4) & 3; }
 
 // The weight's or x's rows of a step, a chunk per thread and round.  from[i]: the
 // row of the thread's i-th chunk, at the chunk that it fetches in step 0.
@@ -221,20 +227,17 @@ template <int THREADS, int ROWS> struct Int8Side {
     int chunk;                                     // within a step; the same for all rounds
     __device__ __forceinline__ Int8Side(const int8_t* codes, int64_t row0, int64_t rows, int chunks) {
         const int t = threadIdx.x, r = t / kStepChunks;
-        chunk = t % kStepChunks ^ r / 4 % 4;       // rounds differ by a multiple of 16 rows
+        chunk = t % kStepChunks ^ turn(r);         // rounds differ by a multiple of 16 rows
 #pragma unroll
         for (int i = 0; i < ROUNDS; i++)           // rows behind the last repeat it: they are not stored
             from[i] = codes + min(row0 + r + i * (THREADS / kStepChunks), rows - 1) * ((int64_t)chunks * kChunk) +
                       chunk * kChunk;
     }
-    __device__ __forceinline__ void fetch(int step, int end, char* image) const {
-        const bool there = step * kStepChunks + chunk < end;
+    template <int I> __device__ __forceinline__ void fetch(int step, int end, char* image) const {
+        const int8_t* p = step * kStepChunks + chunk < end ? from[I] + (int64_t)step * (kStepChunks * kChunk)
+                                                          : (const int8_t*)&k_int8_zero;
         char* const to = image + threadIdx.x / kWave * kWave * kChunk;
-#pragma unroll
-        for (int i = 0; i < ROUNDS; i++) {
-            const int8_t* p = there ? from[i] + (int64_t)step * (kStepChunks * kChunk) : (const int8_t*)&k_int8_zero;
-            __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(to + i * THREADS * kChunk), 16, 0, 0);
-        }
+        __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(to + I * THREADS * kChunk), 16, 0, 0);
     }
 };
 
@@ -271,13 +274,17 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_int8_gemm(Int8Args a) {
     const int all = (a.chunks + kStepChunks - 1) / kStepChunks, share = (all + gridDim.y - 1) / gridDim.y;
     const int first = min(all, share * (int)blockIdx.y), steps = min(all, first + share) - first;
     const int end = min(a.chunks, (first + steps) * kStepChunks);
+    constexpr int XROUNDS = Int8Side<THREADS, ROWS>::ROUNDS;
+    auto fetch_one = [&](auto image, auto n, int s) {
+        constexpr int I = decltype(n)::value;
+        if constexpr (I < XROUNDS) xside.template fetch<I>(first + s, end, xat(image));
+        else wside.template fetch<I - XROUNDS>(first + s, end, wat(image));
+    };
     auto fetch = [&](auto image, int s) {
-        xside.fetch(first + s, end, xat(image));
-        wside.fetch(first + s, end, wat(image));
-        __builtin_amdgcn_sched_barrier(0);         // on their way before the multiplications begin
+        static_for<FETCHES>([&](auto n) { fetch_one(image, n, s); });
     };
     i32x4 x[2][F], w[G];
-    const int place = (lane / 16 ^ lane / 4 % 4) * kChunk;
+    const int place = (lane / 16 ^ turn(lane % 16)) * kChunk;
     const int xr = (wm * 16 * F + lane % 16) * ROW + place, wr = (wn * 16 * G + lane % 16) * ROW + place;
     auto read_x = [&](auto s, auto i) {
         constexpr int S = decltype(s)::value, I = decltype(i)::value;
@@ -308,7 +315,6 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_int8_gemm(Int8Args a) {
     auto step = [&](auto image, int s) {
         constexpr int S = decltype(image)::value;
         arrived(Const<1>{});
-        fetch(Const<S + 3>{}, s + 3);
         static_for<G>([&](auto cj) {
             constexpr int J = decltype(cj)::value;
             static_for<F>([&](auto i) {
@@ -319,6 +325,12 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_int8_gemm(Int8Args a) {
                 acc[I][J] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[J], x[S % 2][I], acc[I][J], 0, 0, 0);
             });
             read_w(Const<S + 1>{}, cj);
+            // fetches spread over the columns: at the step's start all waves would
+            // queue for the address units before their first multiplication
+            // (8192^3: 460 us, 431 so)
+            static_for<FETCHES>([&](auto n) {
+                if constexpr (decltype(n)::value * G / FETCHES == J) fetch_one(Const<S + 3>{}, n, s + 3);
+            });
             __builtin_amdgcn_sched_barrier(0);
         });
     };
