@@ -763,7 +763,8 @@ agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int
  * it, so that every product is exact; sums are float32, in an order that the sizes alone
  * decide, and grad_weight is rounded once.  accumulate != 0: the sums are added
  * (in float32) to what grad_weight and grad_bias hold.  M = 0 gives zeros.
- * M, N, K < 2^31; errors: INVALID, RANGE (more than 2^23 - 8 tiles of 256 x 256 elements of grad_weight). */
+ * M, N < 2^31, K <= 2^25.  Errors: INVALID, RANGE (more than 2^23 - 8 tiles of
+ * 256 x 256, or of 128 x 128, elements of grad_weight). */
 agnes_status agnes_mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
 agnes_status agnes_mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, int32_t accumulate,
                                    const agnes_matrix* grad_weight, float* grad_bias, void* workspace,

@@ -236,7 +236,7 @@ template <int THREADS, int ROWS> struct Int8Side {
     template <int I> __device__ __forceinline__ void fetch(int step, int end, char* image) const {
         const int8_t* p = step * kStepChunks + chunk < end ? from[I] + (int64_t)step * (kStepChunks * kChunk)
                                                           : (const int8_t*)&k_int8_zero;
-        char* const to = image + threadIdx.x / kWave * kWave * kChunk;
+        char* const to = image + __builtin_amdgcn_readfirstlane(wave_id()) * (kWave * kChunk);
         __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(to + I * THREADS * kChunk), 16, 0, 0);
     }
 };
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_int8_gemm(Int8Args a) {
     // adds no wait of its own for it.
     __shared__ __attribute__((aligned(1024))) char x0[ROWS * ROW], x1[ROWS * ROW], x2[ROWS * ROW], x3[ROWS * ROW];
     __shared__ __attribute__((aligned(1024))) char w0[COLS * ROW], w1[COLS * ROW], w2[COLS * ROW], w3[COLS * ROW];
-    const int lane = lane_id(), wave = wave_id(), wm = wave / WN, wn = wave % WN;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wm = wave / WN, wn = wave % WN;
     // XCD x takes a contiguous run of tiles, in strips of 8 tile rows: the tiles
     // that run at once on it share rows of both operands in its L2.
     const int64_t tm = (a.M + ROWS - 1) / ROWS, tn = (a.N + COLS - 1) / COLS, tiles = tm * tn;

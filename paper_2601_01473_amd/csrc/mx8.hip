@@ -181,28 +181,501 @@ __global__ __launch_bounds__(kBlock) void k_mx8_act_grad(const int8_t* __restric
 
 // ----------------------------------------------------------------- weight gradient
 
-// A thread per element of grad_weight; the first column's threads also sum the bias gradient.
-template <typename TG, typename TW>
-__global__ __launch_bounds__(kBlock) void k_mx8_wgrad(const TG* __restrict__ g, int64_t gstride,
-                                                      const int8_t* __restrict__ codes,
-                                                      const uint8_t* __restrict__ scales, int64_t blocks, int64_t M,
-                                                      int64_t N, int64_t K, bool accumulate, TW* __restrict__ dw,
-                                                      int64_t wstride, float* __restrict__ db) {
-    const int64_t step = (int64_t)gridDim.x * kBlock, total = N * K;
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < total; i += step) {
-        const int64_t n = i / K, k = i % K;
-        float sum = 0.f;
-        for (int64_t m = 0; m < M; m++)
-            sum = fmaf(to_float(g[m * gstride + n]),
-                       from_code(codes[m * blocks * kMx8Block + k], scales[m * blocks + k / kMx8Block]), sum);
-        TW* const at = dw + n * wstride + k;
-        *at = from_float<TW>(accumulate ? to_float(*at) + sum : sum);
+// out[n][k] = sum over rows m of g[m][n] x[m][k]: both operands have m as their
+// slow axis, and the multiplication wants 8 consecutive m per lane.  Both lie in
+// LDS as they lie in memory, row m after row, as bfloat16, and are read with
+// ds_read_tr16_b64, which transposes: of 16 lanes, lane i names 4 columns (8
+// bytes) of row i / 4, and receives column i of the four rows.
+//
+// v_mfma_f32_16x16x32_bf16: lane l holds 8 m of row l % 16 of either operand;
+// D[4 (l / 16) + r][l % 16].  x goes in first, so a lane holds four adjacent
+// columns of a row of out.
+//
+// A float16 or float32 gradient is cut into 2 or 3 bfloat16 that add up to it,
+// planes of LDS that all meet the same x.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct WgradArgs {
+    const void* g;
+    int64_t gstride, gplane;                       // elements between rows, and between the planes of a cut gradient
+    const int8_t* codes;
+    const uint8_t* scales;
+    int64_t M, N, K, blocks;                       // blocks per kept row
+    void* out;
+    int64_t stride;
+    bool accumulate, nt;
+    float* parts;                                  // [gridDim.y][N][K]: sums over parts of the rows instead of out, or NULL
+    const float* bias_sums;                        // [bias_parts][N], for the join
+    int bias_parts;
+    float* db;
+};
+
+// Rows of a matrix that are read a step (32 rows) at a time, as buffers: reads
+// behind a buffer bring zeros, so that rows behind the last one need no branch.
+// All of it is scalar.  Offsets stay below 2^31: kMaxPitch.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+constexpr uint32_t kNowhere = 0x80000000u;         // an offset behind every such buffer
+constexpr int64_t kMaxPitch = (int64_t)1 << 25;    // bytes
+// Values that are the same in all lanes, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+    return (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
+}
+struct Rows {
+    uint64_t at;                                   // the next step's first row, at the tile's first column
+    int left, pitch, skip;                         // rows from there on; bytes of a row, and before the tile's first column
+    __device__ __forceinline__ Rows(const void* p, int64_t rows, int64_t row_bytes, int64_t before)
+        : at(uniform((uint64_t)p)), left(uniform((int)rows)), pitch(uniform((int)row_bytes)), skip(uniform((int)before)) {}
+    __device__ __forceinline__ Buffer buffer(int row, uint64_t offset = 0) const {     // from that row of the step on
+        int n = max(left - row, 0);
+        asm("" : "+s"(n));                         // the two bounds would become one vector instruction
+        const int bytes = max(min(n, 32) * pitch - skip, 0);
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(at + offset + (uint64_t)row * (uint32_t)pitch), 0, bytes, 0x00020000);
     }
-    if (!db) return;
-    for (int64_t n = (int64_t)blockIdx.x * kBlock + threadIdx.x; n < N; n += step) {
-        float sum = 0.f;
-        for (int64_t m = 0; m < M; m++) sum += to_float(g[m * gstride + n]);
-        db[n] = accumulate ? db[n] + sum : sum;
+    __device__ __forceinline__ void advance() {
+        at += 32 * (uint64_t)(uint32_t)pitch;
+        left -= 32;
+    }
+};
+
+constexpr int kStepRows = 32, kImages = 4;         // rows m of a step; steps in LDS
+
+// An image: kStepRows rows of WIDTH bfloat16, in blocks of 1024 bytes (what a wave
+// fetches at once) with PAD bytes between them; chunk c (32 bytes) of row m of
+// its block at place c ^ key(m).  A wave reads one chunk of eight consecutive rows at
+// once: they lie in different banks.  Fewer key bits than an unpadded image
+// would need leave fewer addresses for a lane to hold.
+template <int WIDTH> struct Image {
+    static constexpr int ROW = WIDTH * 2, BLOCK_ROWS = 1024 / ROW, PAD = WIDTH == 256 ? 64 : WIDTH == 128 ? 128 : 0;
+    static constexpr int BLOCK = 1024 + PAD, BYTES = kStepRows / BLOCK_ROWS * BLOCK, KEYS = WIDTH == 256 ? 2 : 4;
+    static __device__ __forceinline__ int key(int m) { return WIDTH == 64 ? m / 2 % 4 : m % KEYS; }
+    static __device__ __forceinline__ int row(int m) { return m / BLOCK_ROWS * BLOCK + m % BLOCK_ROWS * ROW; }
+};
+
+// Two floats to bfloat16, which both are exactly.
+__device__ __forceinline__ uint32_t pack_exact(float a, float b) {
+    return __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xFFFF0000u);
+}
+
+// x as P bfloat16 that add up to it: its bits cut into eights.  Infinities and NaN are whole in the first.
+template <int P> __device__ __forceinline__ void cut(float x, float (&part)[P]) {
+    const uint32_t b = __float_as_uint(x);
+    const bool finite = (b & 0x7F800000u) != 0x7F800000u;
+    part[0] = __uint_as_float(finite || (b & 0x007FFFFFu) == 0 ? b & 0xFFFF0000u : 0x7FC00000u);
+    float rest = finite ? x - part[0] : 0.f;
+#pragma unroll
+    for (int p = 1; p < P; p++) {
+        part[p] = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
+        rest -= part[p];
+    }
+}
+
+template <typename TG> constexpr int kParts = sizeof(TG) == 4 ? 3 : std::is_same<TG, _Float16>::value ? 2 : 1;
+
+// Eight gradients, as loaded.
+template <typename TG> struct Eight {
+    typename Vec<TG, 8>::type v;
+};
+
+// A workgroup of WM x WN waves computes a tile of out, a wave 16 F rows (n) and
+// 16 G columns (k) of it, in steps of 32 m.  DIRECT: P planes of bfloat16 whose rows are
+// whole 16-byte pieces go from memory straight to LDS, three steps ahead; else
+// gradients of type TG pass through registers and are cut there.  The kept codes
+// pass through registers too, a step ahead of being converted and three of
+// their use.  A wave reads a step's operands into registers while it multiplies
+// the step before.
+template <typename TG, int P, typename TW, bool DIRECT, int WM, int WN, int F, int G>
+__global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
+    constexpr int THREADS = kWave * WM * WN, ROWS = WM * 16 * F, COLS = WN * 16 * G;
+    typedef Image<ROWS> GI;
+    typedef Image<COLS> XI;
+    static_assert(DIRECT ? std::is_same<TG, __bf16>::value : P == kParts<TG>, "");
+    // An object per image and operand: see k_int8_gemm's.
+    __shared__ __attribute__((aligned(1024))) char g0[P * GI::BYTES], g1[P * GI::BYTES], g2[P * GI::BYTES], g3[P * GI::BYTES];
+    __shared__ __attribute__((aligned(1024))) char x0[XI::BYTES], x1[XI::BYTES], x2[XI::BYTES], x3[XI::BYTES];
+    const int t = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wm = wave / WN, wn = wave % WN;
+    // XCD x takes a contiguous run of tiles, in strips of 8 tile rows.
+    const int64_t tm = (a.N + ROWS - 1) / ROWS, tn = (a.K + COLS - 1) / COLS, tiles = tm * tn;
+    const int64_t per = (tiles + kXcds - 1) / kXcds, id = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+    if ((int64_t)blockIdx.x / kXcds >= per || id >= tiles) return;
+    const int64_t strip = id / (8 * tn), high = min((int64_t)8, tm - strip * 8), in = id - strip * 8 * tn;
+    const int64_t n0 = (strip * 8 + in % high) * ROWS, k0 = in / high * COLS;
+
+    f32x4 acc[F][G];
+#pragma unroll
+    for (int i = 0; i < F; i++)
+#pragma unroll
+        for (int j = 0; j < G; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // This part's steps; fetches behind its end bring zeros, so that every step has equally many.
+    const int all = (int)((a.M + kStepRows - 1) / kStepRows), share = (all + gridDim.y - 1) / gridDim.y;
+    const int first = min(all, share * (int)blockIdx.y), steps = min(all, first + share) - first;
+    const int64_t row0 = (int64_t)first * kStepRows;
+    const int rows = (int)(min(a.M, row0 + (int64_t)steps * kStepRows) - row0);                   // of this part
+    auto gat = [&](auto s) -> char* { constexpr int S = decltype(s)::value % kImages; return S == 0 ? g0 : S == 1 ? g1 : S == 2 ? g2 : g3; };
+    auto xat = [&](auto s) -> char* { constexpr int S = decltype(s)::value % kImages; return S == 0 ? x0 : S == 1 ? x1 : S == 2 ? x2 : x3; };
+
+    // The gradient: pieces of 8 elements, THREADS per round.
+    constexpr int GPIECES = ROWS / 8, GROUNDS = kStepRows * GPIECES / THREADS, GSTEP = THREADS / GPIECES;   // rows per round
+    static_assert(GROUNDS >= 1 && GSTEP % GI::BLOCK_ROWS == 0, "rounds have the same places");
+    const int grow = t / GPIECES;
+    const int gpiece = DIRECT ? t % GPIECES ^ GI::key(grow) << 1 : t % GPIECES;       // by place in LDS, or by place in memory
+    const int64_t gn = n0 + gpiece * 8;
+    const TG* const gfrom = (const TG*)a.g + row0 * a.gstride + n0;
+    const uint32_t gplace = gn < a.N ? (uint32_t)(grow * (int)a.gstride + gpiece * 8) * 2 : kNowhere;
+    Rows grows(gfrom, rows, DIRECT ? a.gstride * 2 : 0, 0);
+    auto fetch_g = [&](auto image, auto round) {                                      // DIRECT; the last round advances
+        constexpr int Q = decltype(round)::value / GROUNDS, I = decltype(round)::value % GROUNDS;
+        const Buffer b = grows.buffer(I * GSTEP, Q * (uint64_t)a.gplane * 2);
+        if constexpr (decltype(round)::value == P * GROUNDS - 1) grows.advance();
+        char* const to = gat(image) + wave * GI::BLOCK;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_void*)(to + Q * GI::BYTES + I * (THREADS / kWave) * GI::BLOCK), 16, gplace, 0, 0, 0);
+    };
+    // Through registers: whole pieces, from a row's end where they would reach
+    // over it; the piece that the end cuts is loaded by elements.  Rows behind the last
+    // repeat it and are zeroed on their way to LDS.
+    Eight<TG> gnext[DIRECT ? 1 : GROUNDS];
+    int gleft = 0;                                 // of the loaded step's rows, those from this thread's first on
+    const int64_t gcol = max(min(gn, a.N - 8), (int64_t)0);
+    const bool gcut = gn < a.N && gn + 8 > a.N;
+    auto load_g = [&](int s) {
+        gleft = rows - s * kStepRows - grow;
+        if (rows <= 0) return;
+#pragma unroll
+        for (int i = 0; i < (DIRECT ? 0 : GROUNDS); i++) {
+            const int m = min(s * kStepRows + grow + i * GSTEP, rows - 1);
+            const TG* const p = (const TG*)a.g + (row0 + m) * a.gstride;
+            if (a.N >= 8) gnext[i].v = Vec<TG, 8>::raw(p + gcol);
+            if (gcut) {
+#pragma unroll
+                for (int q = 0; q < 8; q++) gnext[i].v[q] = gn + q < a.N ? p[gn + q] : (TG)0.f;
+            }
+        }
+    };
+    auto put_g = [&](auto image, const Eight<TG>(&e)[DIRECT ? 1 : GROUNDS]) {
+#pragma unroll
+        for (int i = 0; i < (DIRECT ? 0 : GROUNDS); i++) {
+            char* const to = gat(image) + GI::row(grow) + i * (GSTEP / GI::BLOCK_ROWS) * GI::BLOCK +
+                             (t % GPIECES ^ GI::key(grow) << 1) * 16;
+            u32x4 w[P];
+            const bool there = i * GSTEP < gleft;
+            if constexpr (P == 1) {
+                __builtin_memcpy(&w[0], &e[i].v, 16);
+                w[0] = there ? w[0] : u32x4{0u, 0u, 0u, 0u};
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    float lo[P], hi[P];
+                    cut<P>(there ? (float)e[i].v[2 * q] : 0.f, lo);
+                    cut<P>(there ? (float)e[i].v[2 * q + 1] : 0.f, hi);
+#pragma unroll
+                    for (int p = 0; p < P; p++) w[p][q] = pack_exact(lo[p], hi[p]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < P; p++) *(u32x4*)(to + p * GI::BYTES) = w[p];
+        }
+    };
+
+    // The kept rows: pieces of 16 codes, one per thread (in tiles of 64 the second half of the threads has none).
+    constexpr int XPIECES = COLS / 16, XTHREADS = kStepRows * XPIECES;
+    static_assert(XTHREADS <= THREADS, "one piece per thread");
+    const int xt = t % XTHREADS, xrow = xt / XPIECES, xpiece = xt % XPIECES;
+    const int64_t xb = (k0 + xpiece * 16) / kMx8Block;
+    const bool xin = xb < a.blocks;
+    const int64_t pitch = a.blocks * kMx8Block;
+    Rows crows(a.codes + row0 * pitch + k0, rows, pitch, k0);
+    Rows srows(a.scales + row0 * a.blocks + k0 / kMx8Block, rows, a.blocks, k0 / kMx8Block);
+    const uint32_t cplace = xin ? xrow * (uint32_t)pitch + xpiece * 16 : kNowhere;
+    const uint32_t splace = xin ? xrow * (uint32_t)a.blocks + xpiece * 16 / kMx8Block : kNowhere;
+    int xput = XI::row(xrow) + (xpiece ^ XI::key(xrow)) * 32;
+    struct Kept {
+        u32x4 c;
+        int scale;
+    };
+    Kept xring[2];
+    auto load_x = [&] {                            // a load for every thread: waits count them
+        const Buffer c = crows.buffer(0), e = srows.buffer(0);
+        crows.advance();
+        srows.advance();
+        return Kept{__builtin_amdgcn_raw_buffer_load_b128(c, cplace, 0, 0), __builtin_amdgcn_raw_buffer_load_b8(e, splace, 0, 0)};
+    };
+    // Pair N of the 8 pairs of codes; four of them are a store.
+    u32x4 xword;
+    auto put_x = [&](auto image, auto pair, const Kept& r) {
+        constexpr int N = decltype(pair)::value;
+        const uint32_t c = r.c[N / 2] >> (N % 2 * 16);
+        const float scale = r.scale == 255 ? __uint_as_float(0x7FC00000u) : ldexpf(1.f, r.scale - 133);
+        xword[N % 4] = pack_exact((float)(int8_t)c * scale, (float)(int8_t)(c >> 8) * scale);
+        if constexpr (N % 4 == 3)
+            if (XTHREADS == THREADS || t < XTHREADS) *(u32x4*)(xat(image) + xput + N / 4 * 16) = xword;
+    };
+
+    // Operands.  A lane's 8 m are 4 (lane / 16) + {0 .. 3} and those plus 16, in both operands.
+    const int mrow = lane / 4 % 4 + lane / 16 * 4;
+    int gr[GI::KEYS], xr[XI::KEYS];                // for tiles that differ in the key's bits
+#pragma unroll
+    for (int q = 0; q < GI::KEYS; q++) gr[q] = GI::row(mrow) + ((wm * F + q) ^ GI::key(mrow)) * 32 + lane % 4 * 8;
+#pragma unroll
+    for (int q = 0; q < XI::KEYS; q++) xr[q] = XI::row(mrow) + ((wn * G + q) ^ XI::key(mrow)) * 32 + lane % 4 * 8;
+    static_assert((F % GI::KEYS == 0 || F < GI::KEYS) && (G % XI::KEYS == 0 || G < XI::KEYS), "");
+    auto read = [&](const char* at, int half) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        union {
+            s16x4 s[2];
+            bf16x8 v;
+        } r;
+        r.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        r.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + half));
+        return r.v;
+    };
+    bf16x8 gv[P][F], xv[G];
+    auto read_g = [&](auto s, auto i) {
+        constexpr int I = decltype(i)::value;
+        static_for<P>([&](auto p) {
+            constexpr int Q = decltype(p)::value;
+            gv[Q][I] = read(gat(s) + Q * GI::BYTES + gr[I % GI::KEYS] + I / GI::KEYS * GI::KEYS * 32, GI::row(16));
+        });
+    };
+    auto read_x = [&](auto s, auto j) {
+        constexpr int J = decltype(j)::value;
+        xv[J] = read(xat(s) + xr[J % XI::KEYS] + J / XI::KEYS * XI::KEYS * 32, XI::row(16));
+    };
+    // A wave's fetches, but the last step's ones, and its own stores are in LDS; then all waves'.
+    constexpr int COUNTED = P * GROUNDS + 2;
+    auto arrived = [](auto later) {
+        if constexpr (DIRECT) __builtin_amdgcn_s_waitcnt(0x0070 | decltype(later)::value);
+        else __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0) alone
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    static_assert(!DIRECT || COUNTED < 16, "what a wait can count here");
+
+    // Step s, whose image is the constant, on its way to registers, and from there into LDS.
+    auto load = [&](auto image, int s) {
+        xring[decltype(image)::value % 2] = load_x();
+        if constexpr (!DIRECT) load_g(s);
+    };
+    auto put = [&](auto image, auto pair) {
+        if constexpr (!DIRECT && decltype(pair)::value == 0) put_g(image, gnext);
+        put_x(image, pair, xring[decltype(image)::value % 2]);
+    };
+    // Steps 0 .. 2 on their way, 0 and 1 in LDS.
+    if constexpr (DIRECT)
+        static_for<3>([&](auto i) {
+            static_for<P * GROUNDS>([&](auto r) { fetch_g(i, r); });
+        });
+    static_for<2>([&](auto i) {
+        load(i, decltype(i)::value);
+        static_for<8>([&](auto n) { put(i, n); });
+    });
+    load(Const<2>{}, 2);
+    arrived(Const<0>{});
+    static_for<F>([&](auto i) { read_g(Const<0>{}, i); });
+    static_for<G>([&](auto j) { read_x(Const<0>{}, j); });
+    // Step s: its operands are in registers.  Behind the barrier step s + 1 is in
+    // LDS, and nobody reads the images of the steps before s any more.
+    auto step = [&](auto image, int s) {
+        constexpr int S = decltype(image)::value;
+        arrived(Const<DIRECT ? COUNTED : 0>{});
+        // Addresses in an image are sums of these; kept over the loop for all
+        // images they would not fit the registers.
+#pragma unroll
+        for (int q = 0; q < GI::KEYS; q++) asm volatile("" : "+v"(gr[q]));
+#pragma unroll
+        for (int q = 0; q < XI::KEYS; q++) asm volatile("" : "+v"(xr[q]));
+        asm volatile("" : "+v"(xput));
+        static_for<F>([&](auto ci) {               // 16 rows of out
+            constexpr int I = decltype(ci)::value;
+            static_for<G>([&](auto cj) {
+                constexpr int J = decltype(cj)::value;
+                static_for<P>([&](auto p) {        // the smallest part first
+                    acc[I][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[J], gv[P - 1 - decltype(p)::value][I], acc[I][J], 0,
+                                                                       0, 0);
+                });
+                if constexpr (I == F - 1) read_x(Const<S + 1>{}, cj);
+            });
+            read_g(Const<S + 1>{}, ci);            // in the place of what has been multiplied
+            static_for<8>([&](auto n) {
+                if constexpr (decltype(n)::value * F / 8 == I) put(Const<S + 2>{}, n);
+            });
+            if constexpr (I == (F > 2 ? 1 : 0)) load(Const<S + 3>{}, s + 3);
+            if constexpr (DIRECT)
+                static_for<P * GROUNDS>([&](auto r) {          // behind the kept codes' loads
+                    constexpr int R = decltype(r)::value, AT = F > 2 ? 2 + R * (F - 2) / (P * GROUNDS) : 1;
+                    if constexpr (AT == I) fetch_g(Const<S + 3>{}, r);
+                });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    for (int s = 0; s < steps; s += kImages) {     // steps behind the last one multiply zeros
+        // Sums in accumulation registers: the compiler would let them wander
+        // through all 256 and spill operands.
+#pragma unroll
+        for (int i = 0; i < F; i++)
+#pragma unroll
+            for (int j = 0; j < G; j++) asm volatile("" : "+a"(acc[i][j]));
+        static_for<kImages>([&](auto i) { step(i, s + decltype(i)::value); });
+    }
+    __builtin_amdgcn_s_waitcnt(kVmcnt0);           // the last fetches, before LDS is used again
+    __syncthreads();
+
+    // Rows leave through LDS, each wave its own part in strips of 16 rows, as
+    // pieces along a row.
+    constexpr int E = 16 / (int)sizeof(TW), PITCH = 16 * G + 4;
+    constexpr int SHARE = (WM * WN + 3) / 4;       // waves per LDS object
+    static_assert(SHARE * 16 * PITCH * 4 <= GI::BYTES, "a strip per wave");
+    char* const part = wave / SHARE == 0 ? g0 : wave / SHARE == 1 ? g1 : wave / SHARE == 2 ? g2 : g3;
+    float* const strip_at = (float*)part + wave % SHARE * 16 * PITCH;
+    TW* const out = a.parts ? (TW*)a.parts + (int64_t)blockIdx.y * a.N * a.K : (TW*)a.out;      // parts: launched with TW = float
+    const int64_t ostride = a.parts ? a.K : a.stride;
+    const bool accumulate = !a.parts && a.accumulate;
+    const int64_t wn0 = n0 + wm * 16 * F, wk0 = k0 + wn * 16 * G;
+#pragma unroll
+    for (int i = 0; i < F; i++) {
+#pragma unroll
+        for (int j = 0; j < G; j++) *(f32x4*)(strip_at + lane % 16 * PITCH + j * 16 + lane / 16 * 4) = acc[i][j];
+        wave_sync();
+        constexpr int PER_ROW = 16 * G / E, ROUNDS = (16 * PER_ROW + kWave - 1) / kWave;
+#pragma unroll
+        for (int q = 0; q < ROUNDS; q++) {
+            const int at = q * kWave + lane, row = at / PER_ROW, c = at % PER_ROW * E;
+            const int64_t n = wn0 + i * 16 + row, k = wk0 + c;
+            if (row >= 16 || n >= a.N || k >= a.K) continue;
+            TW* const to = out + n * ostride + k;
+            float y[E];
+#pragma unroll
+            for (int e = 0; e < E; e++) y[e] = strip_at[row * PITCH + c + e];
+            if (k + E <= a.K) {
+                if (accumulate) {
+                    float old[E];
+                    Vec<TW, E>::load(to, old);
+#pragma unroll
+                    for (int e = 0; e < E; e++) y[e] += old[e];
+                }
+                Vec<TW, E>::store(to, y, a.nt);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; e++)
+                    if (k + e < a.K) to[e] = from_float<TW>(accumulate ? to_float(to[e]) + y[e] : y[e]);
+            }
+        }
+        wave_sync();
+    }
+}
+
+// out from the sum of the parts, in their order, by the first `groups`
+// workgroups; the bias gradient from its parts by the others.
+template <typename TW> __global__ __launch_bounds__(kBlock) void k_mx8_wgrad_join(WgradArgs a, int parts, int groups) {
+    if ((int)blockIdx.x >= groups) {
+        const int64_t n = (int64_t)(blockIdx.x - groups) * kBlock + threadIdx.x;
+        if (n >= a.N) return;
+        float s = 0.f;
+#pragma unroll 8
+        for (int p = 0; p < a.bias_parts; p++) s += a.bias_sums[(int64_t)p * a.N + n];
+        a.db[n] = a.accumulate ? a.db[n] + s : s;
+        return;
+    }
+    const int64_t total = a.N * a.K, step = (int64_t)groups * kBlock * 4;
+    for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4; i < total; i += step) {
+        const int count = (int)min((int64_t)4, total - i);
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        if (count == 4) {
+#pragma unroll 4
+            for (int p = 0; p < parts; p++) {
+                float v[4];
+                Vec<float, 4>::load(a.parts + p * total + i, v);
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] += v[e];
+            }
+        } else {
+            for (int p = 0; p < parts; p++)
+                for (int e = 0; e < count; e++) y[e] += a.parts[p * total + i + e];
+        }
+        const int64_t n = i / a.K, k = i % a.K;
+        if (k + 4 <= a.K) {                        // all in one row
+            TW* const to = (TW*)a.out + n * a.stride + k;
+            if (a.accumulate) {
+                float old[4];
+                Vec<TW, 4>::load(to, old);
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] += old[e];
+            }
+            Vec<TW, 4>::store(to, y);
+        } else {
+            for (int e = 0; e < count; e++) {
+                TW* const to = (TW*)a.out + (i + e) / a.K * a.stride + (i + e) % a.K;
+                *to = from_float<TW>(a.accumulate ? to_float(*to) + y[e] : y[e]);
+            }
+        }
+    }
+}
+
+// ----------------------------------------------------------------- columns of the gradient
+
+// One pass over g: its planes of bfloat16 with rows of whole pieces (P > 0), and
+// the sums of its columns over parts of the rows (sums not NULL).  A thread takes 8 columns
+// of every (kBlock / L)-th row of its workgroup's part; L threads side by side.
+template <typename TG, int P>
+__global__ __launch_bounds__(kBlock) void k_mx8_columns(const TG* __restrict__ g, int64_t gstride, int64_t M, int64_t N, int L,
+                                                        int64_t share, uint16_t* __restrict__ planes, int64_t pitch,
+                                                        float* __restrict__ sums) {
+    __shared__ float red[kBlock][8];
+    const int l = threadIdx.x / L, lanes = kBlock / L;
+    const int64_t n = ((int64_t)blockIdx.x * L + threadIdx.x % L) * 8, m0 = share * blockIdx.y, m1 = min(M, m0 + share);
+    constexpr int U = 4;
+    float s[8] = {};
+    if (n < N)
+        for (int64_t m = m0 + l; m < m1; m += U * lanes) {
+            float x[U][8];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (m + u * lanes < m1) {
+                    load8<TG>(g + (m + u * lanes) * gstride, n, N, x[u]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; q++) x[u][q] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+#pragma unroll
+                for (int q = 0; q < 8; q++) s[q] += x[u][q];
+                if constexpr (P > 0) {
+                    if (m + u * lanes >= m1) continue;
+                    u32x4 w[P];
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        float lo[P], hi[P];
+                        cut<P>(x[u][2 * q], lo);
+                        cut<P>(x[u][2 * q + 1], hi);
+#pragma unroll
+                        for (int p = 0; p < P; p++) w[p][q] = pack_exact(lo[p], hi[p]);
+                    }
+#pragma unroll
+                    for (int p = 0; p < P; p++) *(u32x4*)(planes + (p * M + m + u * lanes) * pitch + n) = w[p];
+                }
+            }
+        }
+    if (!sums) return;
+#pragma unroll
+    for (int q = 0; q < 8; q++) red[threadIdx.x][q] = s[q];
+    for (int d = lanes / 2; d; d /= 2) {           // a power of two of lanes
+        __syncthreads();
+        if (l < d) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) red[threadIdx.x][q] += red[threadIdx.x + d * L][q];
+        }
+    }
+    if (l == 0 && n < N) {
+#pragma unroll
+        for (int q = 0; q < 8; q++)
+            if (n + q < N) sums[(int64_t)blockIdx.y * N + n + q] = red[threadIdx.x][q];
     }
 }
 
@@ -302,10 +775,113 @@ void mx8_activation_grad(const agnes_mx8* kept, agnes_act act, bool gated, const
     });
 }
 
+constexpr int64_t kPartSteps = 4;                  // fewest steps of a part
+constexpr int64_t kColumnGrid = 1024;              // workgroups that a pass over the gradient's columns aims at
+constexpr int64_t kColumnRows = 64;                // fewest rows of its parts
+
+// How a gradient is computed, by sizes, by how many planes it has and by whether they go straight to LDS.
+struct WgradPlan {
+    int rows, parts;                               // of a tile; of M
+    int lanes;                                     // of the pass over columns: its threads side by side,
+    int64_t share;                                 // rows of its parts
+    int column_parts;
+};
+
+// The tile and the parts that are fastest by what their steps have measured (us per step of one
+// workgroup alone on its compute unit, and per step and workgroup of a full one; what a
+// workgroup needs before its first step and behind its last), with the joining of the parts at
+// 4 TB/s.  16384 x 4096 x 4096 bfloat16: tiles of 256, 128 and 64 take 495, 650 and 1700
+// us; 65536 x 256 x 1024: 88, 68 and 96 us in their best parts; 8192 x 512 x 512: 42, 25 and 26 us.
+static WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t K, int planes, bool straight) {
+    WgradPlan p{64, 1, 1, 1, 1};
+    const int64_t steps = (M + kStepRows - 1) / kStepRows;
+    auto tiles = [&](int64_t r) { return ((N + r - 1) / r) * ((K + r - 1) / r); };
+    struct Tile {
+        int rows;
+        double alone[3], full[3], ends;            // of 1, 2, 3 planes
+    };
+    static const Tile kTiles[] = {{256, {1.0, 0, 0}, {1.0, 0, 0}, 10},
+                                  {128, {0.49, 0.65, 0.89}, {0.33, 0.65, 0.89}, 10},
+                                  {64, {0.28, 0.42, 0.6}, {0.21, 0.32, 0.48}, 4}};
+    double best = 0;
+    for (const Tile& t : kTiles) {
+        if ((t.rows == 256 && planes > 1) || (t.rows > 64 && !straight)) continue;
+        for (int64_t grid : {1, 256, 512, 1024}) {
+            const int64_t parts = std::max<int64_t>(1, std::min(grid / std::max<int64_t>(1, tiles(t.rows)), steps / kPartSteps));
+            const double each = (double)((steps + parts - 1) / parts), groups = (double)(tiles(t.rows) * parts);
+            const double us = t.ends + std::max(each * t.alone[planes - 1], std::ceil(groups / 256) * each * t.full[planes - 1]) +
+                              (parts > 1 ? 6 + (double)(parts * N * K) * 8 / 4e6 : 0);
+            if (best == 0 || us < best) {
+                best = us;
+                p.rows = t.rows;
+                p.parts = (int)parts;
+            }
+        }
+    }
+    AGNES_REQUIRE(tiles(p.rows) <= (1 << 23) - kXcds, AGNES_ERR_RANGE, "the gradient has too many tiles");
+    const int64_t pieces = (N + 7) / 8;
+    while (p.lanes < 32 && p.lanes < pieces) p.lanes *= 2;
+    const int64_t across = (pieces + p.lanes - 1) / p.lanes;
+    if (across > 0) {
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((kColumnGrid + across - 1) / across, M / kColumnRows));
+        p.share = std::max<int64_t>(1, (M + want - 1) / want);
+        p.column_parts = (int)std::max<int64_t>(1, (M + p.share - 1) / p.share);
+    }
+    return p;
+}
+
+// Gradients that cannot go straight to LDS are cut into planes by a pass of
+// their own, where there is work enough for it: otherwise every tile cuts them
+// again, and rows that start at odd addresses are read slowly by every tile.  (us, with that pass / cut in tiles:
+// 16384 x 4095 x 4096 bfloat16 580 / 2600, 60000 x 47 x 256 float32 78 / 91, 8192 x 515 x 512
+// 58 / 70, 2048 x 512 x 512 27 / 23, 2048 x 512 x 128 23 / 18.)
+static bool make_planes(int64_t M, int64_t N, int64_t K) { return M * N >= (1 << 21) || (K >= 1024 && M >= 256); }
+
+static int64_t plane_pitch(int64_t N) { return (N + 7) / 8 * 8; }
+
+// The largest need of the ways in which gradients of any type reach their tiles.
 uint64_t mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K) {
     for (int64_t v : {M, N, K})
         AGNES_REQUIRE(v >= 0 && v < ((int64_t)1 << 31), AGNES_ERR_INVALID, "M, N and K must be in [0, 2^31)");
-    return 0;
+    AGNES_REQUIRE(K <= kMaxPitch, AGNES_ERR_INVALID, "K must be at most 2^25");
+    uint64_t most = 0;
+    for (int planes : {1, 2, 3, -1, -2, -3}) {     // < 0: cut in tiles
+        const WgradPlan p = plan_wgrad(M, N, K, std::abs(planes), planes > 0);
+        Carve c(nullptr);
+        if (p.parts > 1) c.take<float>(p.parts * N * K);
+        c.take<float>(p.column_parts * N);
+        if (planes > 0 && make_planes(M, N, K)) c.take<uint16_t>(planes * M * plane_pitch(N));
+        most = std::max<uint64_t>(most, c.used);
+    }
+    return most;
+}
+
+template <typename TG, int P, typename TW, bool DIRECT, int WM, int WN, int F, int G>
+static void launch_tiles(const WgradArgs& a, int parts, hipStream_t st) {
+    constexpr int R = WM * 16 * F, C = WN * 16 * G;
+    const int64_t tiles = ((a.N + R - 1) / R) * ((a.K + C - 1) / C);
+    const unsigned grid = (unsigned)((tiles + kXcds - 1) / kXcds * kXcds);
+    AGNES_LAUNCH((k_mx8_wgrad<TG, P, TW, DIRECT, WM, WN, F, G>), dim3(grid, (unsigned)parts), dim3(kWave * WM * WN), 0, st, a);
+}
+
+// TG: float, _Float16 or __bf16 through registers, or P planes straight to LDS.
+template <typename TG, int P, typename TW, bool DIRECT>
+static void launch_wgrad(const WgradArgs& a, const WgradPlan& p, hipStream_t st) {
+    if constexpr (DIRECT && P == 1) {
+        if (p.rows == 256) return launch_tiles<TG, P, TW, DIRECT, 2, 4, 8, 4>(a, p.parts, st);
+    }
+    if constexpr (DIRECT) {
+        if (p.rows == 128) return launch_tiles<TG, P, TW, DIRECT, 2, 2, 4, 4>(a, p.parts, st);
+    }
+    launch_tiles<TG, P, TW, DIRECT, 2, 2, 2, 2>(a, p.parts, st);
+}
+
+template <typename TG, int P>
+static void launch_columns(const agnes_matrix* g, const WgradPlan& p, uint16_t* planes, float* sums, hipStream_t st) {
+    const int64_t pieces = (g->cols + 7) / 8;
+    AGNES_LAUNCH((k_mx8_columns<TG, P>), dim3((unsigned)((pieces + p.lanes - 1) / p.lanes), (unsigned)p.column_parts),
+                 dim3(kBlock), 0, st, (const TG*)g->data, g->stride, g->rows, g->cols, p.lanes, p.share, planes,
+                 plane_pitch(g->cols), sums);
 }
 
 void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool accumulate,
@@ -320,11 +896,55 @@ void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool a
     check_workspace(ws, ws_bytes, mx8_weight_grad_bytes(M, N, K));
     if (N == 0) return;
     with_float(grad_out->dtype, [&](auto tg) {
+        typedef decltype(tg) TG;
+        constexpr int P = kParts<TG>;
+        // bfloat16 rows of whole 16-byte pieces, within a buffer's reach, need no planes
+        const bool direct = P == 1 && ((uintptr_t)grad_out->data & 15) == 0 && grad_out->stride % 8 == 0 && N % 8 == 0 &&
+                            grad_out->stride >= N && grad_out->stride * 2 <= kMaxPitch;
+        const bool planes = !direct && make_planes(M, N, K) && plane_pitch(N) * 2 <= kMaxPitch;
+        const WgradPlan p = plan_wgrad(M, N, K, P, planes || direct);
+        Carve c(ws);
+        WgradArgs a{};
+        a.g = grad_out->data;
+        a.gstride = grad_out->stride;
+        a.codes = kept->codes;
+        a.scales = kept->scales;
+        a.M = M;
+        a.N = N;
+        a.K = K;
+        a.blocks = blocks_of(K);
+        a.out = grad_weight->data;
+        a.stride = grad_weight->stride;
+        a.accumulate = accumulate;
+        a.nt = !accumulate && N * K * (int64_t)elem_size(grad_weight->dtype) > kStreamBytes;
+        if (p.parts > 1) a.parts = c.take<float>(p.parts * N * K);
+        float* const sums = grad_bias ? p.column_parts > 1 ? c.take<float>(p.column_parts * N) : grad_bias : nullptr;
+        const bool join_bias = grad_bias && (p.column_parts > 1 || accumulate);
+        float* const first = join_bias && p.column_parts == 1 ? c.take<float>(N) : sums;
+        if (planes) {
+            uint16_t* const to = c.take<uint16_t>(P * M * plane_pitch(N));
+            launch_columns<TG, P>(grad_out, p, to, first, st);
+            a.g = to;
+            a.gstride = plane_pitch(N);
+            a.gplane = M * plane_pitch(N);
+        } else if (grad_bias) {
+            launch_columns<TG, 0>(grad_out, p, nullptr, first, st);
+        }
+        a.bias_sums = first;
+        a.bias_parts = p.column_parts;
+        a.db = grad_bias;
+        auto tiles = [&](auto tw) {
+            typedef decltype(tw) TW;
+            if (planes || direct) launch_wgrad<__bf16, P, TW, true>(a, p, st);
+            else launch_wgrad<TG, P, TW, false>(a, p, st);
+        };
+        if (K > 0 && p.parts > 1) tiles(float{});
         with_float(grad_weight->dtype, [&](auto tw) {
-            AGNES_LAUNCH((k_mx8_wgrad<decltype(tg), decltype(tw)>), dim3(grid_for(std::max<int64_t>(N * K, N), 4096)),
-                         dim3(kBlock), 0, st, (const decltype(tg)*)grad_out->data, grad_out->stride, kept->codes,
-                         kept->scales, blocks_of(K), M, N, K, accumulate, (decltype(tw)*)grad_weight->data,
-                         grad_weight->stride, grad_bias);
+            if (K > 0 && p.parts == 1) tiles(tw);
+            const int groups = K > 0 && p.parts > 1 ? (int)grid_for((N * K + 3) / 4, 4096) : 0;
+            const int more = join_bias ? (int)((N + kBlock - 1) / kBlock) : 0;
+            if (groups + more > 0)
+                AGNES_LAUNCH((k_mx8_wgrad_join<decltype(tw)>), dim3(groups + more), dim3(kBlock), 0, st, a, p.parts, groups);
         });
     });
 }
