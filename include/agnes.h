@@ -613,8 +613,8 @@ agnes_status agnes_distill_loss_grad(const agnes_distill* d, float* loss, const 
  *   clip_low in [0, 1], clip_high >= 0, kl >= 0, all finite.
  * agnes_policy_logprob: logp [rows] alone (how old_logp and ref_logp are made);
  *   advantage, old_logp and ref_logp are not read and may be NULL.
- * agnes_policy_loss: loss [rows], logp [rows] and, unless NULL, stats [rows][2]:
- *   the row's largest logit m and sum exp((z - m) / T); zeros for a skipped row.
+ * agnes_policy_loss: loss [rows], logp [rows] and, unless NULL, stats [rows][3]:
+ *   the row's largest logit m, sum exp((z - m) / T) and the action's logit; zeros for a skipped row.
  * agnes_policy_grad: the gradient from those statistics, for the same
  *   descriptor (weights may differ in rows that were not skipped): as the
  *   backward pass of per-row losses, weight is the gradient that arrives.

@@ -8,8 +8,20 @@
 // Whether a row is clipped hangs on the last digits of logp, and exp d - d - 1
 // cancels where the policies are close, so what a row needs once is computed
 // in 64 bits; m, S and the gradient in 32.
+//
+// A row of logits is read once, stays in registers between its sum and its
+// gradient, and its gradient is written once.  Variants, by the number of
+// 16-byte pieces of a row:
+//   up to 256      some lanes of a wave per row (a whole wave from 33 pieces on)
+//   up to 16384    a workgroup of 256 to 1024 threads per row
+//   above, or above 1024 with too few rows to fill the chip: the row is split
+//     over workgroups; a first launch leaves each part's maximum and sum and the action's
+//     logit, a second one joins them and writes the gradient (a second read of
+//     the row).
+// The gradient from statistics is the second launch alone, or the lanes' kernel.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "logits.hpp"
 
@@ -30,8 +42,12 @@ struct PolicyArgs {
     bool nt;                       // gradient past the caches
     float temp, kl;                // T
     double low, high;              // 1 - clip_low, 1 + clip_high
-    float ct;                      // log2(e) / T: exp(x / T) = 2^(x ct)
+    float ct, ct_low;              // log2(e) / T = ct + ct_low, both positive: exp(x / T) = 2^(x ct + x ct_low)
 };
+
+// exp(d / T) for d <= 0.  A single factor's rounding would move all of a row's terms,
+// and with them its logp, one way; with positive parts -inf stays -inf.
+__device__ __forceinline__ float exp_t(const PolicyArgs& a, float d) { return pow2(fmaf(d, a.ct, d * a.ct_low)); }
 
 // What a row asks for, as loaded.
 struct Decision {
@@ -81,73 +97,338 @@ __device__ __forceinline__ void store_grad(const PolicyArgs& a, int64_t at, int 
     else store_typed<E>((__bf16*)a.grad + at, c, hi, x, a.nt);
 }
 
-// A workgroup per row, which it reads for the maximum, for the sum and for the gradient.
-template <typename T> __global__ __launch_bounds__(kBlock) void k_policy_row(PolicyArgs a) {
-    __shared__ float red[kWavesPerBlock];
+// Maximum and sum of part of a row, relative to that maximum (to 0 where it is -inf).
+struct Sum {
+    float m, s;
+};
+
+// Adds E logits (-inf where there are none), none above x.m.  A NaN or +inf
+// logit makes the sum NaN, and with it everything that follows.
+template <int E, typename Raw> __device__ __forceinline__ void add_piece(const PolicyArgs& a, Sum& x, const Raw& v) {
+    const float base = x.m == -INFINITY ? 0.f : x.m;
+#pragma unroll
+    for (int q = 0; q < E; q++) x.s += exp_t(a, (float)v[q] - base);
+}
+// Brings a sum to the maximum m of a larger part.
+__device__ __forceinline__ void rebase(const PolicyArgs& a, Sum& x, float m) {
+    if (m == -INFINITY) return;                    // the sum is 0 (or NaN)
+    x.s *= exp_t(a, x.m - m);
+    x.m = m;
+}
+__device__ __forceinline__ Sum lanes_join(const PolicyArgs& a, Sum x) {
+    rebase(a, x, lanes_max(x.m, kWave));
+    x.s = lanes_sum(x.s, kWave);
+    return x;
+}
+
+// The gradient of logits [c, c + E): k = g / S.
+template <int E, typename Raw>
+__device__ __forceinline__ void grad_piece(const PolicyArgs& a, const Raw& v, int c, float m, float k, float g, int y, float (&x)[E]) {
+#pragma unroll
+    for (int q = 0; q < E; q++) {
+        x[q] = -k * exp_t(a, (float)v[q] - m);
+        if (c + q == y) x[q] += g;
+    }
+}
+
+__device__ __forceinline__ void store_row(const PolicyArgs& a, int64_t r, const Outcome& o, float m, float s, float zy) {
+    if (a.loss) a.loss[r] = o.loss;
+    if (a.logp) a.logp[r] = o.logp;
+    if (a.stats) {
+        a.stats[3 * r] = m;
+        a.stats[3 * r + 1] = s;
+        a.stats[3 * r + 2] = zy;
+    }
+}
+
+// ----------------------------------------------------------------- lanes of a wave per row
+
+// L lanes per row, P pieces per lane; a group takes several rows and loads the
+// next one before the present one's arithmetic.
+constexpr int kLanesMin = 8;
+constexpr int kLaneGroups = 2048;                // workgroups, about what the chip holds at once
+
+template <typename T, int P> struct LaneRow {
+    typename Vec<T, 16 / (int)sizeof(T)>::type v[P];
+    Decision d;
+};
+
+template <typename T, int P> __global__ __launch_bounds__(kBlock) void k_policy_lanes(PolicyArgs a, int L) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const int groups = kBlock / L, g = threadIdx.x / L, gl = threadIdx.x % L;
+    const int64_t step = (int64_t)gridDim.x * groups;
+    int64_t r = (int64_t)blockIdx.x * groups + g;
+    auto load = [&](int64_t i) {
+        LaneRow<T, P> x;
+        const T* zr = (const T*)a.z + i * a.zstride;
+#pragma unroll
+        for (int p = 0; p < P; p++) x.v[p] = logits_piece<T, E>(zr, (gl + p * L) * E, a.C);
+        x.d = load_decision(a, i);
+        return x;
+    };
+    LaneRow<T, P> next;
+    if (r < a.rows) next = load(r);
+    for (; r < a.rows; r += step) {                         // per group; nothing below crosses a group
+        LaneRow<T, P> x = next;
+        if (r + step < a.rows) next = load(r + step);
+        const int64_t at = r * a.gstride;
+        if (skipped(a, x.d)) {
+            if (gl == 0) store_row(a, r, Outcome{0.f, 0.f, 0.f}, 0.f, 0.f, 0.f);
+            if (a.grad) {
+                const float zero[E] = {};
+#pragma unroll
+                for (int p = 0; p < P; p++) store_grad<E>(a, at, (gl + p * L) * E, a.C, zero);
+            }
+            continue;
+        }
+        const int y = (int)x.d.y;
+        Sum s{-INFINITY, 0.f};
+        float zy;
+        if (a.stats_in) {
+            s = Sum{a.stats_in[3 * r], a.stats_in[3 * r + 1]};
+            zy = a.stats_in[3 * r + 2];
+        } else {
+            uint32_t named = 0;                             // the action's logit, in the lane that holds it
+#pragma unroll
+            for (int p = 0; p < P; p++)
+#pragma unroll
+                for (int e = 0; e < E; e++) {
+                    const float z = (float)x.v[p][e];
+                    s.m = fmaxf(s.m, z);
+                    if ((gl + p * L) * E + e == y) named = __float_as_uint(z);
+                }
+            s.m = lanes_max(s.m, L);
+#pragma unroll
+            for (int p = 0; p < P; p++) {
+                keep_packed(x.v[p]);
+                add_piece<E>(a, s, x.v[p]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            s.s = lanes_sum(s.s, L);
+            zy = lanes_reduce(__uint_as_float(named), L, [](float u, float v) {
+                return __uint_as_float(__float_as_uint(u) | __float_as_uint(v));
+            });
+        }
+        const Outcome o = outcome(a, x.d, s.m, s.s, zy);
+        if (gl == 0) store_row(a, r, o, s.m, s.s, zy);
+        if (!a.grad) continue;
+        const float k = o.g == 0.f ? 0.f : o.g / s.s;
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            float w[E] = {};
+            keep_packed(x.v[p]);
+            if (o.g != 0.f) grad_piece<E>(a, x.v[p], (gl + p * L) * E, s.m, k, o.g, y, w);
+            store_grad<E>(a, at, (gl + p * L) * E, a.C, w);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+// ----------------------------------------------------------------- a workgroup per row
+
+template <typename T, int THREADS, int P>
+__global__ __launch_bounds__(THREADS, THREADS == 1024 && P == 8 ? 8 : 4) void k_policy_block(PolicyArgs a) {
+    constexpr int E = 16 / (int)sizeof(T), WAVES = THREADS / kWave;
+    typedef typename Vec<T, E>::type Raw;
+    __shared__ Sum red[WAVES];
+    __shared__ float named;
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
     const int64_t r = blockIdx.x;
     const T* zr = (const T*)a.z + r * a.zstride;
+    const int64_t at = r * a.gstride;
     const Decision d = load_decision(a, r);
-    const int tid = threadIdx.x;
     if (skipped(a, d)) {
-        if (tid == 0) {
-            if (a.loss) a.loss[r] = 0.f;
-            if (a.logp) a.logp[r] = 0.f;
-            if (a.stats) a.stats[2 * r] = a.stats[2 * r + 1] = 0.f;
+        if (tid == 0) store_row(a, r, Outcome{0.f, 0.f, 0.f}, 0.f, 0.f, 0.f);
+        if (a.grad) {
+            const float zero[E] = {};
+            for (int c = tid * E; c < a.C; c += THREADS * E) store_grad<E>(a, at, c, a.C, zero);
         }
-        if (a.grad)
-            for (int64_t c = tid; c < a.C; c += kBlock) store_any(a.grad, a.gtype, r * a.gstride + c, 0.f);
         return;
     }
-    const float zy = to_float(zr[d.y]);
-    float m = -INFINITY, s = 0.f;
-    if (a.stats_in) {
-        m = a.stats_in[2 * r];
-        s = a.stats_in[2 * r + 1];
-        __syncthreads();                         // zy is read before the gradient is stored
-    } else {
-        for (int64_t c = tid; c < a.C; c += kBlock) m = fmaxf(m, to_float(zr[c]));
-        m = lanes_max(m, kWave);
-        if (lane_id() == 0) red[wave_id()] = m;
-        __syncthreads();
-        for (int w = 0; w < kWavesPerBlock; w++) m = fmaxf(m, red[w]);
-        __syncthreads();
-        const float base = m == -INFINITY ? 0.f : m;
-        for (int64_t c = tid; c < a.C; c += kBlock) s += pow2((to_float(zr[c]) - base) * a.ct);
-        s = lanes_sum(s, kWave);
-        if (lane_id() == 0) red[wave_id()] = s;
-        __syncthreads();
-        s = 0.f;
-        for (int w = 0; w < kWavesPerBlock; w++) s += red[w];
-    }
-    const Outcome o = outcome(a, d, m, s, zy);
-    if (tid == 0) {
-        if (a.loss) a.loss[r] = o.loss;
-        if (a.logp) a.logp[r] = o.logp;
-        if (a.stats) {
-            a.stats[2 * r] = m;
-            a.stats[2 * r + 1] = s;
+    Raw v[P];
+#pragma unroll
+    for (int i = 0; i < P; i++)
+        if (i * THREADS * E < a.C) v[i] = logits_piece<T, E>(zr, (tid + i * THREADS) * E, a.C);
+    if (tid == 0) named = to_float(zr[d.y]);       // read before anything is stored, also where grad is over the logits
+    Sum s{-INFINITY, 0.f};
+#pragma unroll
+    for (int i = 0; i < P; i++)
+        if (i * THREADS * E < a.C) {
+#pragma unroll
+            for (int x = 0; x < E; x++) s.m = fmaxf(s.m, (float)v[i][x]);
         }
-    }
+    s.m = lanes_max(s.m, kWave);
+#pragma unroll
+    for (int i = 0; i < P; i++)
+        if (i * THREADS * E < a.C) {               // no work for rounds that lie behind the row
+            keep_packed(v[i]);
+            add_piece<E>(a, s, v[i]);
+            __builtin_amdgcn_sched_barrier(0);     // one piece's values at a time: registers decide the occupancy
+        }
+    s.s = lanes_sum(s.s, kWave);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    s = lane < WAVES ? red[lane] : Sum{-INFINITY, 0.f};
+    s = lanes_join(a, s);
+    const Outcome o = outcome(a, d, s.m, s.s, named);
+    if (tid == 0) store_row(a, r, o, s.m, s.s, named);
     if (!a.grad) return;
-    const float k = o.g == 0.f ? 0.f : o.g / s;
-    for (int64_t c = tid; c < a.C; c += kBlock) {
-        float x = 0.f;
-        if (o.g != 0.f) {
-            x = -k * pow2((to_float(zr[c]) - m) * a.ct);
-            if (c == d.y) x += o.g;
+    const float k = o.g == 0.f ? 0.f : o.g / s.s;
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+        if (i * THREADS * E < a.C) {
+            const int c = (tid + i * THREADS) * E;
+            float x[E] = {};
+            keep_packed(v[i]);
+            if (o.g != 0.f) grad_piece<E>(a, v[i], c, s.m, k, o.g, (int)d.y, x);
+            store_grad<E>(a, at, c, a.C, x);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        store_any(a.grad, a.gtype, r * a.gstride + c, x);
+    }
+}
+
+// ----------------------------------------------------------------- a row over several workgroups
+
+// Part of a row: its maximum and sum, and the action's logit if it lies in it (else 0).
+struct Part {
+    float m, s, zy, pad;
+};
+
+constexpr int kPartThreads = 256;
+
+// blockIdx: (part, row).  A part is `span` logits, a multiple of a piece.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_policy_part(PolicyArgs a, int64_t span, Part* __restrict__ parts) {
+    constexpr int E = 16 / (int)sizeof(T), U = 4;
+    typedef typename Vec<T, E>::type Raw;
+    __shared__ Sum red[kPartThreads / kWave];
+    const int tid = threadIdx.x, lane = lane_id(), wave = wave_id();
+    const int64_t r = blockIdx.y;
+    const T* zr = (const T*)a.z + r * a.zstride;
+    const Decision d = load_decision(a, r);
+    if (skipped(a, d)) return;                     // the second launch skips the row too
+    const int lo = (int)(blockIdx.x * span), hi = (int)min((int64_t)a.C, lo + span);
+    Sum s{-INFINITY, 0.f};
+    for (int c0 = lo; c0 < hi; c0 += kPartThreads * E * U) {
+        Raw v[U];
+#pragma unroll
+        for (int i = 0; i < U; i++) v[i] = logits_piece<T, E>(zr, c0 + (tid + i * kPartThreads) * E, hi);
+        float m = s.m;
+#pragma unroll
+        for (int i = 0; i < U; i++)
+#pragma unroll
+            for (int x = 0; x < E; x++) m = fmaxf(m, (float)v[i][x]);
+        rebase(a, s, m);
+#pragma unroll
+        for (int i = 0; i < U; i++) add_piece<E>(a, s, v[i]);
+    }
+    s = lanes_join(a, s);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    if (wave != 0) return;
+    s = lane < kPartThreads / kWave ? red[lane] : Sum{-INFINITY, 0.f};
+    s = lanes_join(a, s);
+    if (lane == 0) {
+        const float zy = d.y >= lo && d.y < hi ? to_float(zr[d.y]) : 0.f;
+        parts[r * gridDim.x + blockIdx.x] = Part{s.m, s.s, zy, 0.f};
+    }
+}
+
+// The row's sum from its parts (or from stats_in), then the loss, by the first
+// workgroup, and the gradient of [lo, hi).  The action's logit comes with them:
+// where grad is over the logits another workgroup may have written there.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_policy_apply(PolicyArgs a, int64_t span, int nparts, const Part* __restrict__ parts) {
+    constexpr int E = 16 / (int)sizeof(T), U = 4;
+    typedef typename Vec<T, E>::type Raw;
+    const int tid = threadIdx.x, lane = lane_id();
+    const int64_t r = blockIdx.y;
+    const T* zr = (const T*)a.z + r * a.zstride;
+    const int64_t at = r * a.gstride;
+    const int lo = (int)(blockIdx.x * span), hi = (int)min((int64_t)a.C, lo + span);
+    const bool first = blockIdx.x == 0;
+    const Decision d = load_decision(a, r);
+    if (skipped(a, d)) {
+        if (first && tid == 0) store_row(a, r, Outcome{0.f, 0.f, 0.f}, 0.f, 0.f, 0.f);
+        if (a.grad) {
+            const float zero[E] = {};
+            for (int c = lo + tid * E; c < hi; c += kPartThreads * E) store_grad<E>(a, at, c, hi, zero);
+        }
+        return;
+    }
+    Raw v[U];
+    if (a.grad) {                                  // on their way while the parts are joined
+#pragma unroll
+        for (int i = 0; i < U; i++) v[i] = logits_piece<T, E>(zr, lo + (tid + i * kPartThreads) * E, hi);
+    }
+    Sum s{-INFINITY, 0.f};
+    float zy = 0.f;
+    if (a.stats_in) {
+        s = Sum{a.stats_in[3 * r], a.stats_in[3 * r + 1]};
+        zy = a.stats_in[3 * r + 2];
+    } else {
+        const Part* p = parts + r * nparts;
+        for (int i = lane; i < nparts; i += kWave) s.m = fmaxf(s.m, p[i].m);
+        s.m = lanes_max(s.m, kWave);
+        for (int i = lane; i < nparts; i += kWave) {
+            Sum x{p[i].m, p[i].s};
+            rebase(a, x, s.m);
+            s.s += x.s;
+        }
+        s.s = lanes_sum(s.s, kWave);
+        zy = p[d.y / span].zy;
+    }
+    const Outcome o = outcome(a, d, s.m, s.s, zy);
+    if (first && tid == 0) store_row(a, r, o, s.m, s.s, zy);
+    if (!a.grad) return;
+    const float k = o.g == 0.f ? 0.f : o.g / s.s;
+    for (int c0 = lo; c0 < hi; c0 += kPartThreads * E * U) {
+        if (c0 != lo) {
+#pragma unroll
+            for (int i = 0; i < U; i++) v[i] = logits_piece<T, E>(zr, c0 + (tid + i * kPartThreads) * E, hi);
+        }
+#pragma unroll
+        for (int i = 0; i < U; i++) {
+            const int c = c0 + (tid + i * kPartThreads) * E;
+            float x[E] = {};
+            if (o.g != 0.f) grad_piece<E>(a, v[i], c, s.m, k, o.g, (int)d.y, x);
+            store_grad<E>(a, at, c, hi, x);
+        }
     }
 }
 
 // ----------------------------------------------------------------- host
 
+constexpr int64_t kLanePieces = 4 * kWave;       // a wave's rows
+constexpr int64_t kSplitPieces = 1024;           // rows that may be split
+constexpr int64_t kBlockPieces = 16 * 1024;      // a workgroup's rows
+constexpr int64_t kSplitRows = 512;              // fewer rows leave too many compute units idle
+constexpr int64_t kSplitGroups = 1024;           // workgroups that a split aims at
 constexpr int64_t kLaunchRows = 1 << 21;         // rows per launch of a workgroup each: a launch holds fewer than 2^32 threads
+
+// Parts of a row of C logits of `size` bytes, or 1 and span 0: not split.  A
+// part has at least one round of its workgroup.
+static int parts_of(int64_t rows, int64_t C, int64_t size, int64_t& span) {
+    const int64_t E = 16 / size, pieces = (C + E - 1) / E, round = (int64_t)kPartThreads * E;
+    span = 0;
+    const bool many = pieces > kBlockPieces;
+    if (!many && (pieces <= kSplitPieces || rows >= kSplitRows)) return 1;
+    const int64_t want = std::max<int64_t>((kSplitGroups + rows - 1) / rows, many ? 2 : 1);
+    const int64_t rounds = std::max<int64_t>(1, (C + round * want - 1) / (round * want));
+    span = rounds * round;
+    return (int)((C + span - 1) / span);
+}
 
 uint64_t policy_bytes(int64_t rows, int64_t classes) {
     AGNES_REQUIRE(rows >= 0 && classes >= 0 && rows < ((int64_t)1 << 31) && classes < ((int64_t)1 << 31),
                   AGNES_ERR_INVALID, "rows and classes must be in [0, 2^31)");
-    return 0;
+    if (rows == 0 || classes == 0) return 0;
+    int64_t span = 0, most = 0;
+    for (int64_t size : {2, 4}) {                // either size of logits
+        const int n = parts_of(rows, classes, size, span);
+        if (span) most = std::max<int64_t>(most, rows * n * (int64_t)sizeof(Part));
+    }
+    return (uint64_t)most;
 }
 
 static PolicyArgs check_policy(const agnes_policy* p, bool alone, const agnes_matrix* grad) {
@@ -196,7 +477,10 @@ static PolicyArgs check_policy(const agnes_policy* p, bool alone, const agnes_ma
     a.rows = rows;
     a.C = (int32_t)C;
     a.temp = p->temperature;
-    a.ct = kLog2e / p->temperature;
+    const double ct = M_LOG2E / (double)p->temperature;
+    a.ct = (float)ct;
+    if (a.ct > ct) a.ct = std::nextafter(a.ct, 0.f);
+    a.ct_low = std::max((float)(ct - a.ct), std::numeric_limits<float>::denorm_min());
     return a;
 }
 
@@ -207,19 +491,57 @@ template <typename T> static PolicyArgs rows_from(const PolicyArgs& a, int64_t r
     b.actions = (const char*)a.actions + r * (a.wide ? 8 : 4);
     for (const float** p : {&b.advantage, &b.old_logp, &b.ref_logp, &b.weight})
         if (*p) *p += r;
-    if (a.stats_in) b.stats_in = a.stats_in + 2 * r;
+    if (a.stats_in) b.stats_in = a.stats_in + 3 * r;
     if (a.loss) b.loss = a.loss + r;
     if (a.logp) b.logp = a.logp + r;
-    if (a.stats) b.stats = a.stats + 2 * r;
+    if (a.stats) b.stats = a.stats + 3 * r;
     if (a.grad) b.grad = (char*)a.grad + r * a.gstride * (int64_t)elem_size(a.gtype);
     b.rows = n;
     return b;
 }
 
 template <typename T> static void launch(const PolicyArgs& a, void* ws, hipStream_t st) {
-    for (int64_t r = 0; r < a.rows; r += kLaunchRows) {
-        const int64_t n = std::min(kLaunchRows, a.rows - r);
-        AGNES_LAUNCH(k_policy_row<T>, dim3((unsigned)n), dim3(kBlock), 0, st, rows_from<T>(a, r, n));
+    constexpr int E = 16 / (int)sizeof(T);
+    const int64_t pieces = (a.C + E - 1) / E, rows = a.rows;
+    if (pieces <= kLanePieces) {
+        int L = kLanesMin;
+        while (L * 4 < pieces) L *= 2;
+        const int per = kBlock / L;
+        const dim3 grid((unsigned)std::min<int64_t>((rows + per - 1) / per, kLaneGroups));
+        if (pieces <= L) AGNES_LAUNCH((k_policy_lanes<T, 1>), grid, dim3(kBlock), 0, st, a, L);
+        else if (pieces <= 2 * L) AGNES_LAUNCH((k_policy_lanes<T, 2>), grid, dim3(kBlock), 0, st, a, L);
+        else AGNES_LAUNCH((k_policy_lanes<T, 4>), grid, dim3(kBlock), 0, st, a, L);
+        return;
+    }
+    int64_t span = 0;
+    int parts = parts_of(rows, a.C, sizeof(T), span);
+    if (a.stats_in && span == 0) {               // the gradient alone needs no sums: parts of any length do
+        span = 4 * kPartThreads * E;
+        parts = (int)((a.C + span - 1) / span);
+    }
+    if (span) {
+        // blockIdx.y holds at most 65535 rows
+        for (int64_t r = 0; r < rows; r += 65535) {
+            const int64_t n = std::min<int64_t>(65535, rows - r);
+            const PolicyArgs b = rows_from<T>(a, r, n);
+            Part* p = (Part*)ws + r * parts;
+            const dim3 grid((unsigned)parts, (unsigned)n);
+            if (!a.stats_in) AGNES_LAUNCH((k_policy_part<T>), grid, dim3(kPartThreads), 0, st, b, span, p);
+            // without a gradient only a row's first part has anything to do
+            AGNES_LAUNCH((k_policy_apply<T>), dim3(a.grad ? (unsigned)parts : 1u, (unsigned)n), dim3(kPartThreads), 0, st, b,
+                         span, parts, (const Part*)p);
+        }
+        return;
+    }
+    for (int64_t r = 0; r < rows; r += kLaunchRows) {
+        const int64_t n = std::min(kLaunchRows, rows - r);
+        const PolicyArgs b = rows_from<T>(a, r, n);
+        const dim3 grid((unsigned)n);
+        if (pieces <= 4 * 256) AGNES_LAUNCH((k_policy_block<T, 256, 4>), grid, dim3(256), 0, st, b);
+        else if (pieces <= 8 * 256) AGNES_LAUNCH((k_policy_block<T, 256, 8>), grid, dim3(256), 0, st, b);
+        else if (pieces <= 8 * 512) AGNES_LAUNCH((k_policy_block<T, 512, 8>), grid, dim3(512), 0, st, b);
+        else if (pieces <= 8 * 1024) AGNES_LAUNCH((k_policy_block<T, 1024, 8>), grid, dim3(1024), 0, st, b);
+        else AGNES_LAUNCH((k_policy_block<T, 1024, 16>), grid, dim3(1024), 0, st, b);
     }
 }
 

@@ -324,13 +324,13 @@ def policy_loss(logits, actions, advantage, old_logp, ref_logp=None, weight=None
     """Per-row clipped policy loss (agnes_policy_loss): logits [rows, C], actions
     [rows], advantage, old_logp and (with kl > 0) ref_logp float32 [rows],
     weight float32 [rows].  Returns (loss, logp float32 [rows], stats float32
-    [rows, 2]); policy_grad takes the statistics."""
+    [rows, 3]); policy_grad takes the statistics."""
     p = _policy(logits, actions, advantage, old_logp, ref_logp, weight, temperature, clip_low, clip_high, kl)
     with _on(stream, logits, actions, advantage, old_logp, ref_logp, weight):
         rows = p.logits.rows
         loss = logits.new_empty(rows, dtype=torch.float32)
         logp = logits.new_empty(rows, dtype=torch.float32)
-        stats = logits.new_empty((rows, 2), dtype=torch.float32)
+        stats = logits.new_empty((rows, 3), dtype=torch.float32)
         need = _policy_bytes(rows, p.logits.cols)
         ws = _workspace(logits, need)
         B.agnes_policy_loss(p, loss.data_ptr(), logp.data_ptr(), stats.data_ptr(), _ptr(ws), need, _handle(stream))
@@ -344,8 +344,8 @@ def policy_grad(logits, actions, advantage, old_logp, stats, ref_logp=None, weig
     gradient that arrives.  out may be the logits themselves."""
     p = _policy(logits, actions, advantage, old_logp, ref_logp, weight, temperature, clip_low, clip_high, kl)
     _device(stats, "stats")
-    if stats.dtype != torch.float32 or tuple(stats.shape) != (p.logits.rows, 2) or not stats.is_contiguous():
-        raise ValueError("stats must be policy_loss's statistics, contiguous float32 [rows, 2]")
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (p.logits.rows, 3) or not stats.is_contiguous():
+        raise ValueError("stats must be policy_loss's statistics, contiguous float32 [rows, 3]")
     with _on(stream, logits, actions, advantage, old_logp, stats, ref_logp, weight, out):
         out, o = _grad_like(logits, out)
         B.agnes_policy_grad(p, stats.data_ptr(), o, _handle(stream))
