@@ -129,53 +129,149 @@ __global__ __launch_bounds__(kBlock) void k_mx8_dequantize(const int8_t* __restr
 
 // ----------------------------------------------------------------- activations
 
-// act(x) and act'(x).
+// act(x) and act'(x).  SiLU: with e = exp(-x) and p = 1 / (1 + e), x p and p (1 +
+// x e p), which has no difference of near numbers.  GELU: Phi(|x|) = 1 - (a1 t + .. +
+// a5 t^5) exp(-x^2 / 2) / 2 with t = 1 / (1 + b |x| / sqrt 2) (Abramowitz and Stegun 7.1.26: erf
+// within 1.5e-7); its exponential is the density's too, so the pair costs one
+// exponential and one reciprocal.
 template <agnes_act ACT> __device__ __forceinline__ void activation(float x, float& value, float& slope) {
+    constexpr float kLog2e = 1.44269504088896340736f;
     if (ACT == AGNES_SILU) {
-        const float e = expf(-x), p = 1.f / (1.f + e);
+        const float e = __builtin_amdgcn_exp2f(x * -kLog2e), p = __builtin_amdgcn_rcpf(1.f + e);
         value = x * p;
-        const float rest = x < -40.f ? 1.f : e * p;             // 1 - p, without a difference
+        const float rest = x < -40.f ? 1.f : e * p;             // 1 - p
         slope = p * (1.f + x * rest);
     } else {
-        const float phi = 0.5f * erfcf(x * -0.70710678118654752440f);
+        const float e = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752440f, 1.f));
+        float q = fmaf(1.061405429f, t, -1.453152027f);
+        q = fmaf(q, t, 1.421413741f);
+        q = fmaf(q, t, -0.284496736f);
+        q = fmaf(q, t, 0.254829592f);
+        q *= 0.5f * t * e;
+        const float phi = x < 0.f ? q : 1.f - q;
         value = x * phi;
-        slope = phi + x * (0.39894228040143267794f * expf(-0.5f * x * x));
+        slope = fmaf(x * 0.39894228040143267794f, e, phi);
     }
 }
 
-template <typename T, typename TY, agnes_act ACT>
-__global__ __launch_bounds__(kBlock) void k_mx8_act(const T* __restrict__ x, int64_t stride, int64_t rows, int64_t F,
-                                                    bool gated, TY* __restrict__ y, int64_t ystride) {
-    const int64_t step = (int64_t)gridDim.x * kBlock, n = rows * F;
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += step) {
-        const int64_t r = i / F, c = i % F;
-        float v, s;
-        activation<ACT>(to_float(x[r * stride + c]), v, s);
-        if (gated) v *= to_float(x[r * stride + F + c]);
-        y[r * ystride + c] = from_float<TY>(v);
+// Forward: a piece is 8 columns of y; x's blocks are four adjacent lanes, in
+// either half of a gated row too if the halves are whole blocks.  KEEP: 8-bit
+// codes of x as well.
+template <typename T, typename TY, agnes_act ACT, bool GATED, bool KEEP>
+__global__ __launch_bounds__(kBlock) void k_mx8_act(const T* __restrict__ x, int64_t stride, int64_t pieces, int64_t F,
+                                                    uint32_t per_row, int8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ scales, int64_t blocks, TY* __restrict__ y,
+                                                    int64_t ystride, bool nt) {
+    constexpr int HALVES = GATED ? 2 : 1, U = kPieces / HALVES;
+    const int64_t base = (int64_t)blockIdx.x * (kBlock * U);
+    const int64_t base_row = base / per_row;
+    const uint32_t base_piece = (uint32_t)(base % per_row);
+    float v[U][HALVES][8];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const uint32_t off = u * kBlock + threadIdx.x;
+        if (base + off < pieces) {
+            const PieceAt p = piece_at(base_row, base_piece, off, per_row);
+#pragma unroll
+            for (int h = 0; h < HALVES; h++) load8<T>(x + p.row * stride + h * F, (int64_t)p.piece * 8, F, v[u][h]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const uint32_t off = u * kBlock + threadIdx.x;
+        if (base + off >= pieces) continue;        // whole blocks: with KEEP pieces is a multiple of 4
+        const PieceAt p = piece_at(base_row, base_piece, off, per_row);
+        const int64_t c = (int64_t)p.piece * 8;
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int h = 0; h < HALVES; h++) {
+                const int scale = scale_code(block_top(v[u][h]));
+                const int64_t at = p.row * blocks * kMx8Block + h * F + c;
+                *(uint2*)(codes + at) = to_codes(v[u][h], scale);
+                if (threadIdx.x % 4 == 0) scales[at / kMx8Block] = (uint8_t)scale;
+            }
+        }
+        float o[8];
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            float slope;
+            activation<ACT>(v[u][0][q], o[q], slope);
+            if constexpr (GATED) o[q] *= v[u][1][q];
+        }
+        store8<TY>(y + p.row * ystride, c, F, o, nt);
     }
 }
 
-template <typename TG, typename TX, agnes_act ACT>
+// Eight kept values from column c of a row on, in whatever blocks they lie; zeros from column `cols` on.
+__device__ __forceinline__ void load_kept(const int8_t* codes, const uint8_t* scales, int64_t c, int64_t cols, float (&x)[8]) {
+    typedef uint2 __attribute__((aligned(1))) u64_bytes;
+    uint2 w = {0u, 0u};
+    if (c + 8 <= cols) {
+        w = *(const u64_bytes*)(codes + c);
+    } else {
+        for (int q = 0; q < 8 && c + q < cols; q++) {
+            const uint32_t b = (uint32_t)(uint8_t)codes[c + q] << (q % 4 * 8);
+            if (q < 4) w.x |= b;
+            else w.y |= b;
+        }
+    }
+    const int64_t first = c / kMx8Block, last = min(c + 7, cols - 1) / kMx8Block;
+    const int lo = scales[first], hi = scales[last], turn = (int)((first + 1) * kMx8Block - c);
+#pragma unroll
+    for (int q = 0; q < 8; q++) x[q] = from_code((int8_t)((q < 4 ? w.x : w.y) >> (q % 4 * 8)), q < turn ? lo : hi);
+}
+
+// Backward: a piece is 8 columns of grad_y.  WHOLE: the halves of a gated row are whole blocks.
+template <typename TG, typename TX, agnes_act ACT, bool GATED, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_mx8_act_grad(const int8_t* __restrict__ codes,
                                                          const uint8_t* __restrict__ scales, int64_t blocks,
-                                                         int64_t rows, int64_t F, bool gated, const TG* __restrict__ gy,
-                                                         int64_t gystride, TX* __restrict__ gx, int64_t gxstride) {
-    const int64_t step = (int64_t)gridDim.x * kBlock, n = rows * F;
-    auto kept = [&](int64_t r, int64_t c) {
-        return from_code(codes[r * blocks * kMx8Block + c], scales[r * blocks + c / kMx8Block]);
-    };
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += step) {
-        const int64_t r = i / F, c = i % F;
-        const float g = to_float(gy[r * gystride + c]);
-        float v, s;
-        activation<ACT>(kept(r, c), v, s);
-        if (gated) {
-            gx[r * gxstride + c] = from_float<TX>(g * kept(r, F + c) * s);
-            gx[r * gxstride + F + c] = from_float<TX>(g * v);
-        } else {
-            gx[r * gxstride + c] = from_float<TX>(g * s);
+                                                         int64_t pieces, int64_t F, uint32_t per_row,
+                                                         const TG* __restrict__ gy, int64_t gystride, TX* __restrict__ gx,
+                                                         int64_t gxstride, bool nt) {
+    constexpr int HALVES = GATED ? 2 : 1, U = kPieces / HALVES;
+    const int64_t base = (int64_t)blockIdx.x * (kBlock * U);
+    const int64_t base_row = base / per_row;
+    const uint32_t base_piece = (uint32_t)(base % per_row);
+    uint2 w[U][HALVES];
+    int s[U][HALVES];
+    float g[U][8];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const uint32_t off = u * kBlock + threadIdx.x;
+        if (base + off < pieces) {
+            const PieceAt p = piece_at(base_row, base_piece, off, per_row);
+            const int64_t at = p.row * blocks * kMx8Block + (int64_t)p.piece * 8;
+#pragma unroll
+            for (int h = 0; h < (WHOLE ? HALVES : 1); h++) {
+                w[u][h] = *(const uint2*)(codes + at + h * F);
+                s[u][h] = scales[(at + h * F) / kMx8Block];
+            }
+            load8<TG>(gy + p.row * gystride, (int64_t)p.piece * 8, F, g[u]);
         }
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const uint32_t off = u * kBlock + threadIdx.x;
+        if (base + off >= pieces) continue;
+        const PieceAt p = piece_at(base_row, base_piece, off, per_row);
+        const int64_t c = (int64_t)p.piece * 8;
+        float a[8], b[8], o[8];
+        from_codes(w[u][0], s[u][0], a);
+        if constexpr (GATED) {
+            if constexpr (WHOLE) from_codes(w[u][HALVES - 1], s[u][HALVES - 1], b);
+            else load_kept(codes + p.row * blocks * kMx8Block, scales + p.row * blocks, F + c, 2 * F, b);
+        }
+        TX* const row = gx + p.row * gxstride;
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            float value, slope;
+            activation<ACT>(a[q], value, slope);
+            o[q] = GATED ? g[u][q] * b[q] * slope : g[u][q] * slope;
+            b[q] = g[u][q] * value;
+        }
+        store8<TX>(row, c, F, o, nt);
+        if constexpr (GATED) store8<TX>(row + F, c, F, b, nt);
     }
 }
 
@@ -727,6 +823,12 @@ template <typename F> static void with_act(agnes_act act, F&& f) {
     if (act == AGNES_SILU) f(std::integral_constant<agnes_act, AGNES_SILU>{});
     else f(std::integral_constant<agnes_act, AGNES_GELU>{});
 }
+template <typename F> static void with_bools(bool a, bool b, F&& f) {
+    if (a && b) f(std::true_type{}, std::true_type{});
+    else if (a) f(std::true_type{}, std::false_type{});
+    else if (b) f(std::false_type{}, std::true_type{});
+    else f(std::false_type{}, std::false_type{});
+}
 static void check_act(agnes_act act) {
     AGNES_REQUIRE(act == AGNES_SILU || act == AGNES_GELU, AGNES_ERR_INVALID, "the activation must be AGNES_SILU or AGNES_GELU");
 }
@@ -738,14 +840,32 @@ void mx8_activation(const agnes_matrix* x, agnes_act act, bool gated, const agne
     check_act(act);
     AGNES_REQUIRE(y->rows == x->rows && x->cols == (gated ? 2 : 1) * y->cols, AGNES_ERR_INVALID,
                   gated ? "y must have x's rows and half its columns" : "y must have x's shape");
-    if (kept) mx8_quantize(x, kept, st);
-    if (y->rows == 0 || y->cols == 0) return;
+    const int64_t R = y->rows, F = y->cols, blocks = blocks_of(x->cols);
+    // halves that meet inside a block: their codes by a pass of their own
+    const bool apart = kept && gated && F % kMx8Block != 0;
+    if (kept) {
+        check_mx8(kept, "kept");
+        AGNES_REQUIRE(kept->rows == x->rows && kept->cols == x->cols, AGNES_ERR_INVALID, "x and kept must have equal shapes");
+    }
+    if (R == 0 || F == 0) return;
+    if (apart) mx8_quantize(x, kept, st);
+    const bool keep = kept && !apart, nt = R * F * (int64_t)elem_size(y->dtype) > kStreamBytes;
+    const int64_t per_row = keep ? blocks_of(F) * 4 : (F + 7) / 8;
     with_float(x->dtype, [&](auto t) {
         with_float(y->dtype, [&](auto ty) {
             with_act(act, [&](auto a) {
-                AGNES_LAUNCH((k_mx8_act<decltype(t), decltype(ty), decltype(a)::value>),
-                             dim3(grid_for(y->rows * y->cols, 4096)), dim3(kBlock), 0, st, (const decltype(t)*)x->data,
-                             x->stride, y->rows, y->cols, gated, (decltype(ty)*)y->data, y->stride);
+                with_bools(gated, keep, [&](auto g, auto k) {
+                    typedef decltype(t) T;
+                    typedef decltype(ty) TY;
+                    constexpr int U = kPieces / (decltype(g)::value ? 2 : 1);
+                    launch_pieces<U>(R, per_row, [&](int64_t r, int64_t pieces, unsigned groups) {
+                        AGNES_LAUNCH((k_mx8_act<T, TY, decltype(a)::value, decltype(g)::value, decltype(k)::value>), dim3(groups),
+                                     dim3(kBlock), 0, st, (const T*)x->data + r * x->stride, x->stride, pieces, F,
+                                     (uint32_t)per_row, keep ? kept->codes + r * blocks * kMx8Block : nullptr,
+                                     keep ? kept->scales + r * blocks : nullptr, blocks, (TY*)y->data + r * y->stride,
+                                     y->stride, nt);
+                    });
+                });
             });
         });
     });
@@ -761,15 +881,24 @@ void mx8_activation_grad(const agnes_mx8* kept, agnes_act act, bool gated, const
                   "grad_x must have the kept rows' shape");
     AGNES_REQUIRE(grad_y->rows == kept->rows && kept->cols == (gated ? 2 : 1) * grad_y->cols, AGNES_ERR_INVALID,
                   gated ? "grad_y must have the kept rows and half their columns" : "grad_y must have the kept rows' shape");
-    if (grad_y->rows == 0 || grad_y->cols == 0) return;
+    const int64_t R = grad_y->rows, F = grad_y->cols, blocks = blocks_of(kept->cols), per_row = (F + 7) / 8;
+    if (R == 0 || F == 0) return;
+    const bool whole = !gated || F % kMx8Block == 0, nt = R * kept->cols * (int64_t)elem_size(grad_x->dtype) > kStreamBytes;
     with_float(grad_y->dtype, [&](auto tg) {
         with_float(grad_x->dtype, [&](auto tx) {
             with_act(act, [&](auto a) {
-                AGNES_LAUNCH((k_mx8_act_grad<decltype(tg), decltype(tx), decltype(a)::value>),
-                             dim3(grid_for(grad_y->rows * grad_y->cols, 4096)), dim3(kBlock), 0, st, kept->codes,
-                             kept->scales, blocks_of(kept->cols), grad_y->rows, grad_y->cols, gated,
-                             (const decltype(tg)*)grad_y->data, grad_y->stride, (decltype(tx)*)grad_x->data,
-                             grad_x->stride);
+                with_bools(gated, whole, [&](auto g, auto w) {
+                    typedef decltype(tg) TG;
+                    typedef decltype(tx) TX;
+                    constexpr int U = kPieces / (decltype(g)::value ? 2 : 1);
+                    launch_pieces<U>(R, per_row, [&](int64_t r, int64_t pieces, unsigned groups) {
+                        AGNES_LAUNCH((k_mx8_act_grad<TG, TX, decltype(a)::value, decltype(g)::value, decltype(w)::value>),
+                                     dim3(groups), dim3(kBlock), 0, st, kept->codes + r * blocks * kMx8Block,
+                                     kept->scales + r * blocks, blocks, pieces, F, (uint32_t)per_row,
+                                     (const TG*)grad_y->data + r * grad_y->stride, grad_y->stride,
+                                     (TX*)grad_x->data + r * grad_x->stride, grad_x->stride, nt);
+                    });
+                });
             });
         });
     });

@@ -147,11 +147,11 @@ template <typename F> void with_index(agnes_dtype t, F&& f) {
 }
 
 // Calls launch(first row, pieces, workgroups) for parts of `rows` rows of
-// per_row <= 2^28 pieces, each of at most kLaunchGroups workgroups: a launch
-// holds fewer than 2^32 threads.
+// per_row <= 2^28 pieces, each of at most kLaunchGroups workgroups, which take U
+// rounds of kBlock pieces: a launch holds fewer than 2^32 threads.
 constexpr int64_t kLaunchGroups = 1 << 22;
-template <typename F> void launch_pieces(int64_t rows, int64_t per_row, F&& launch) {
-    constexpr int64_t kGroup = kBlock * kPieces;
+template <int U = kPieces, typename F> void launch_pieces(int64_t rows, int64_t per_row, F&& launch) {
+    constexpr int64_t kGroup = kBlock * U;
     const int64_t most = kLaunchGroups * kGroup / per_row;
     for (int64_t r = 0; r < rows; r += most) {
         const int64_t n = std::min(most, rows - r), pieces = n * per_row;
