@@ -337,7 +337,7 @@ struct Rows {
     }
 };
 
-constexpr int kStepRows = 32, kImages = 4;         // rows m of a step; steps in LDS
+constexpr int kStepRows = 32, kImages = 3;         // rows m of a step; steps in LDS
 
 // An image: kStepRows rows of WIDTH bfloat16, in blocks of 1024 bytes (what a wave
 // fetches at once) with PAD bytes between them; chunk c (32 bytes) of row m of
@@ -390,8 +390,8 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     typedef Image<COLS> XI;
     static_assert(DIRECT ? std::is_same<TG, __bf16>::value : P == kParts<TG>, "");
     // An object per image and operand: see k_int8_gemm's.
-    __shared__ __attribute__((aligned(1024))) char g0[P * GI::BYTES], g1[P * GI::BYTES], g2[P * GI::BYTES], g3[P * GI::BYTES];
-    __shared__ __attribute__((aligned(1024))) char x0[XI::BYTES], x1[XI::BYTES], x2[XI::BYTES], x3[XI::BYTES];
+    __shared__ __attribute__((aligned(1024))) char g0[P * GI::BYTES], g1[P * GI::BYTES], g2[P * GI::BYTES];
+    __shared__ __attribute__((aligned(1024))) char x0[XI::BYTES], x1[XI::BYTES], x2[XI::BYTES];
     const int t = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wm = wave / WN, wn = wave % WN;
     // XCD x takes a contiguous run of tiles, in strips of 8 tile rows.
     const int64_t tm = (a.N + ROWS - 1) / ROWS, tn = (a.K + COLS - 1) / COLS, tiles = tm * tn;
@@ -411,8 +411,8 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     const int first = min(all, share * (int)blockIdx.y), steps = min(all, first + share) - first;
     const int64_t row0 = (int64_t)first * kStepRows;
     const int rows = (int)(min(a.M, row0 + (int64_t)steps * kStepRows) - row0);                   // of this part
-    auto gat = [&](auto s) -> char* { constexpr int S = decltype(s)::value % kImages; return S == 0 ? g0 : S == 1 ? g1 : S == 2 ? g2 : g3; };
-    auto xat = [&](auto s) -> char* { constexpr int S = decltype(s)::value % kImages; return S == 0 ? x0 : S == 1 ? x1 : S == 2 ? x2 : x3; };
+    auto gat = [&](auto s) -> char* { constexpr int S = decltype(s)::value % kImages; return S == 0 ? g0 : S == 1 ? g1 : g2; };
+    auto xat = [&](auto s) -> char* { constexpr int S = decltype(s)::value % kImages; return S == 0 ? x0 : S == 1 ? x1 : x2; };
 
     // The gradient: pieces of 8 elements, THREADS per round.
     constexpr int GPIECES = ROWS / 8, GROUNDS = kStepRows * GPIECES / THREADS, GSTEP = THREADS / GPIECES;   // rows per round
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
         u32x4 c;
         int scale;
     };
-    Kept xring[2];
+    Kept xring[kImages];
     auto load_x = [&] {                            // a load for every thread: waits count them
         const Buffer c = crows.buffer(0), e = srows.buffer(0);
         crows.advance();
@@ -554,12 +554,12 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
 
     // Step s, whose image is the constant, on its way to registers, and from there into LDS.
     auto load = [&](auto image, int s) {
-        xring[decltype(image)::value % 2] = load_x();
+        xring[decltype(image)::value % kImages] = load_x();
         if constexpr (!DIRECT) load_g(s);
     };
     auto put = [&](auto image, auto pair) {
         if constexpr (!DIRECT && decltype(pair)::value == 0) put_g(image, gnext);
-        put_x(image, pair, xring[decltype(image)::value % 2]);
+        put_x(image, pair, xring[decltype(image)::value % kImages]);
     };
     // Steps 0 .. 2 on their way, 0 and 1 in LDS.
     if constexpr (DIRECT)
@@ -575,7 +575,8 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     static_for<F>([&](auto i) { read_g(Const<0>{}, i); });
     static_for<G>([&](auto j) { read_x(Const<0>{}, j); });
     // Step s: its operands are in registers.  Behind the barrier step s + 1 is in
-    // LDS, and nobody reads the images of the steps before s any more.
+    // LDS, and nobody reads the images of step s and before any more (a wave waits
+    // for its reads before the barrier), so step s + 3 may take that of step s.
     auto step = [&](auto image, int s) {
         constexpr int S = decltype(image)::value;
         arrived(Const<DIRECT ? COUNTED : 0>{});
@@ -625,8 +626,8 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     // pieces along a row.
     constexpr int E = 16 / (int)sizeof(TW), PITCH = 16 * G + 4;
     constexpr int SHARE = (WM * WN + 3) / 4;       // waves per LDS object
-    static_assert(SHARE * 16 * PITCH * 4 <= GI::BYTES, "a strip per wave");
-    char* const part = wave / SHARE == 0 ? g0 : wave / SHARE == 1 ? g1 : wave / SHARE == 2 ? g2 : g3;
+    static_assert(SHARE * 16 * PITCH * 4 <= P * GI::BYTES && SHARE * 16 * PITCH * 4 <= XI::BYTES, "a strip per wave");
+    char* const part = wave / SHARE == 0 ? g0 : wave / SHARE == 1 ? g1 : wave / SHARE == 2 ? g2 : x0;
     float* const strip_at = (float*)part + wave % SHARE * 16 * PITCH;
     TW* const out = a.parts ? (TW*)a.parts + (int64_t)blockIdx.y * a.N * a.K : (TW*)a.out;      // parts: launched with TW = float
     const int64_t ostride = a.parts ? a.K : a.stride;
@@ -910,44 +911,49 @@ constexpr int64_t kColumnRows = 64;                // fewest rows of its parts
 
 // How a gradient is computed, by sizes, by how many planes it has and by whether they go straight to LDS.
 struct WgradPlan {
-    int rows, parts;                               // of a tile; of M
+    int rows, cols, parts;                         // of a tile; of M
     int lanes;                                     // of the pass over columns: its threads side by side,
     int64_t share;                                 // rows of its parts
     int column_parts;
 };
 
-// The tile and the parts that are fastest by what their steps have measured (us per step of one
-// workgroup alone on its compute unit, and per step and workgroup of a full one; what a
-// workgroup needs before its first step and behind its last), with the joining of the parts at
-// 4 TB/s.  16384 x 4096 x 4096 bfloat16: tiles of 256, 128 and 64 take 495, 650 and 1700
-// us; 65536 x 256 x 1024: 88, 68 and 96 us in their best parts; 8192 x 512 x 512: 42, 25 and 26 us.
+// The tile and the parts that are fastest by what their steps have measured (us
+// per step of one workgroup alone on its compute unit, and per step and
+// workgroup of a full one; and what a workgroup needs before its first step and
+// behind its last), with the joining of the parts at 4 TB/s.
+// 16384 x 4096 x 4096: bfloat16 in tiles of 256, 128 and 64 takes 490, 680 and 1800
+// us; float16 in tiles of 128 x 256, 128 and 64 takes 960, 1305 and 2960 us, float32
+// 1370, 1815 and 3775 us.  65536 x 256 x 1024 bfloat16: 88, 70 and 96 us in each tile's best
+// parts; 8192 x 512 x 512: 42, 23 and 26 us.
 static WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t K, int planes, bool straight) {
-    WgradPlan p{64, 1, 1, 1, 1};
+    WgradPlan p{64, 64, 1, 1, 1, 1};
     const int64_t steps = (M + kStepRows - 1) / kStepRows;
-    auto tiles = [&](int64_t r) { return ((N + r - 1) / r) * ((K + r - 1) / r); };
+    auto tiles = [&](int64_t r, int64_t c) { return ((N + r - 1) / r) * ((K + c - 1) / c); };
     struct Tile {
-        int rows;
+        int rows, cols;
         double alone[3], full[3], ends;            // of 1, 2, 3 planes
     };
-    static const Tile kTiles[] = {{256, {1.0, 0, 0}, {1.0, 0, 0}, 10},
-                                  {128, {0.49, 0.65, 0.89}, {0.33, 0.65, 0.89}, 10},
-                                  {64, {0.28, 0.42, 0.6}, {0.21, 0.32, 0.48}, 4}};
+    static const Tile kTiles[] = {{256, 256, {1.0, 0, 0}, {1.0, 0, 0}, 10},
+                                  {128, 256, {0, 0.92, 1.25}, {0, 0.92, 1.25}, 10},
+                                  {128, 128, {0.49, 0.63, 0.86}, {0.33, 0.63, 0.86}, 10},
+                                  {64, 64, {0.28, 0.42, 0.6}, {0.21, 0.32, 0.46}, 4}};
     double best = 0;
     for (const Tile& t : kTiles) {
-        if ((t.rows == 256 && planes > 1) || (t.rows > 64 && !straight)) continue;
+        if (t.full[planes - 1] == 0 || (t.rows > 64 && !straight)) continue;
         for (int64_t grid : {1, 256, 512, 1024}) {
-            const int64_t parts = std::max<int64_t>(1, std::min(grid / std::max<int64_t>(1, tiles(t.rows)), steps / kPartSteps));
-            const double each = (double)((steps + parts - 1) / parts), groups = (double)(tiles(t.rows) * parts);
+            const int64_t parts = std::max<int64_t>(1, std::min(grid / std::max<int64_t>(1, tiles(t.rows, t.cols)), steps / kPartSteps));
+            const double each = (double)((steps + parts - 1) / parts), groups = (double)(tiles(t.rows, t.cols) * parts);
             const double us = t.ends + std::max(each * t.alone[planes - 1], std::ceil(groups / 256) * each * t.full[planes - 1]) +
                               (parts > 1 ? 6 + (double)(parts * N * K) * 8 / 4e6 : 0);
             if (best == 0 || us < best) {
                 best = us;
                 p.rows = t.rows;
+                p.cols = t.cols;
                 p.parts = (int)parts;
             }
         }
     }
-    AGNES_REQUIRE(tiles(p.rows) <= (1 << 23) - kXcds, AGNES_ERR_RANGE, "the gradient has too many tiles");
+    AGNES_REQUIRE(tiles(p.rows, p.cols) <= (1 << 23) - kXcds, AGNES_ERR_RANGE, "the gradient has too many tiles");
     const int64_t pieces = (N + 7) / 8;
     while (p.lanes < 32 && p.lanes < pieces) p.lanes *= 2;
     const int64_t across = (pieces + p.lanes - 1) / p.lanes;
@@ -998,6 +1004,9 @@ template <typename TG, int P, typename TW, bool DIRECT>
 static void launch_wgrad(const WgradArgs& a, const WgradPlan& p, hipStream_t st) {
     if constexpr (DIRECT && P == 1) {
         if (p.rows == 256) return launch_tiles<TG, P, TW, DIRECT, 2, 4, 8, 4>(a, p.parts, st);
+    }
+    if constexpr (DIRECT && P > 1) {
+        if (p.cols == 256) return launch_tiles<TG, P, TW, DIRECT, 2, 4, 4, 4>(a, p.parts, st);
     }
     if constexpr (DIRECT) {
         if (p.rows == 128) return launch_tiles<TG, P, TW, DIRECT, 2, 2, 4, 4>(a, p.parts, st);
