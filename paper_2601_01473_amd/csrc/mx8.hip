@@ -666,16 +666,27 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     }
 }
 
+constexpr int kJoinCols = 16;
+
 // out from the sum of the parts, in their order, by the first `groups`
 // workgroups; the bias gradient from its parts by the others.
 template <typename TW> __global__ __launch_bounds__(kBlock) void k_mx8_wgrad_join(WgradArgs a, int parts, int groups) {
-    if ((int)blockIdx.x >= groups) {
-        const int64_t n = (int64_t)(blockIdx.x - groups) * kBlock + threadIdx.x;
-        if (n >= a.N) return;
+    __shared__ float red[kBlock];
+    if ((int)blockIdx.x >= groups) {               // kJoinCols columns, the other threads' share of the parts each
+        constexpr int LANES = kBlock / kJoinCols;
+        const int l = threadIdx.x / kJoinCols;
+        const int64_t n = (int64_t)(blockIdx.x - groups) * kJoinCols + threadIdx.x % kJoinCols;
         float s = 0.f;
+        if (n < a.N) {
 #pragma unroll 8
-        for (int p = 0; p < a.bias_parts; p++) s += a.bias_sums[(int64_t)p * a.N + n];
-        a.db[n] = a.accumulate ? a.db[n] + s : s;
+            for (int p = l; p < a.bias_parts; p += LANES) s += a.bias_sums[(int64_t)p * a.N + n];
+        }
+        red[threadIdx.x] = s;
+        for (int d = LANES / 2; d; d /= 2) {
+            __syncthreads();
+            if (l < d) red[threadIdx.x] += red[threadIdx.x + d * kJoinCols];
+        }
+        if (l == 0 && n < a.N) a.db[n] = a.accumulate ? a.db[n] + red[threadIdx.x] : red[threadIdx.x];
         return;
     }
     const int64_t total = a.N * a.K, step = (int64_t)groups * kBlock * 4;
@@ -1080,7 +1091,7 @@ void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool a
         with_float(grad_weight->dtype, [&](auto tw) {
             if (K > 0 && p.parts == 1) tiles(tw);
             const int groups = K > 0 && p.parts > 1 ? (int)grid_for((N * K + 3) / 4, 4096) : 0;
-            const int more = join_bias ? (int)((N + kBlock - 1) / kBlock) : 0;
+            const int more = join_bias ? (int)((N + kJoinCols - 1) / kJoinCols) : 0;
             if (groups + more > 0)
                 AGNES_LAUNCH((k_mx8_wgrad_join<decltype(tw)>), dim3(groups + more), dim3(kBlock), 0, st, a, p.parts, groups);
         });
