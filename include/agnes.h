@@ -764,7 +764,7 @@ agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int
  * decide, and grad_weight is rounded once.  accumulate != 0: the sums are added
  * (in float32) to what grad_weight and grad_bias hold.  M = 0 gives zeros.
  * M, N < 2^31, K <= 2^25.  Errors: INVALID, RANGE (more than 2^23 - 8 tiles of
- * 256 x 256, or of 128 x 128, elements of grad_weight). */
+ * 64 x 64 elements of grad_weight). */
 agnes_status agnes_mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
 agnes_status agnes_mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, int32_t accumulate,
                                    const agnes_matrix* grad_weight, float* grad_bias, void* workspace,

@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     const int gpiece = DIRECT ? t % GPIECES ^ GI::key(grow) << 1 : t % GPIECES;       // by place in LDS, or by place in memory
     const int64_t gn = n0 + gpiece * 8;
     const TG* const gfrom = (const TG*)a.g + row0 * a.gstride + n0;
-    const uint32_t gplace = gn < a.N ? (uint32_t)(grow * (int)a.gstride + gpiece * 8) * 2 : kNowhere;
+    const uint32_t gplace = DIRECT && gn < a.N ? (grow * (uint32_t)a.gstride + gpiece * 8) * 2 : kNowhere;
     Rows grows(gfrom, rows, DIRECT ? a.gstride * 2 : 0, 0);
     auto fetch_g = [&](auto image, auto round) {                                      // DIRECT; the last round advances
         constexpr int Q = decltype(round)::value / GROUNDS, I = decltype(round)::value % GROUNDS;

@@ -196,3 +196,21 @@ def test_another_stream_and_replayed_graph(ag):
         torch.cuda.synchronize()
         for o, x, w in zip(outs, xs, ws):
             assert torch.equal(o, ag.int8_linear(x, w))
+
+
+@pytest.mark.parametrize("M", [17, 40, 300])
+def test_no_columns_and_many_rows(ag, M):
+    """K = 0 through every kernel: the bias alone."""
+    none = ag.int8_quantize(torch.zeros(70, 0, device="cuda"))
+    b = torch.randn(70, device="cuda")
+    got = ag.int8_linear(torch.zeros(M, 0, device="cuda"), none, b)
+    assert torch.equal(got, b.expand(M, 70))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 20, 300), (5, 33, 90), (20, 50, 200), (200, 130, 100)])
+def test_codes_behind_a_weight_s_last_column_do_not_matter(ag, M, N, K):
+    """Rows that the call quantises itself have zeros there."""
+    x, q = rows_of(M, K, BF16), ag.int8_quantize(rows_of(N, K))
+    want = ag.int8_linear(x, q)
+    q.codes[:, K:] = 77
+    assert torch.equal(ag.int8_linear(x, q), want)

@@ -311,3 +311,44 @@ def test_another_stream_and_replayed_graph(ag):
         torch.cuda.synchronize()
         for a, b in zip(outs, step()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("M,N,K", [(70000, 31, 64), (2100, 1001, 40), (300, 130, 1100), (4200, 515, 300)])
+def test_gradients_cut_by_a_pass_of_their_own(ag, dtype, M, N, K):
+    """Enough work for it, or a wide layer: rows at odd addresses, a last piece that the row's end cuts, and padding
+    columns of the planes that hold no row's values."""
+    check_wgrad(ag, M, N, K, dtype, F32)
+    wide = rows_of(M, N + 3, dtype, seed=9)
+    kept = ag.mx8_quantize(rows_of(M, K, seed=10))
+    want = ag.mx8_weight_grad(wide[:, 1:1 + N].contiguous(), kept, bias=True, dtype=F32)
+    got = ag.mx8_weight_grad(wide[:, 1:1 + N], kept, bias=True, dtype=F32)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N", [1, 3, 7, 8, 9])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_narrow_gradients(ag, N, dtype):
+    """Fewer columns than a piece of 8, at the end of their memory."""
+    for M, K in ((1, 40), (33, 100), (400, 1030)):
+        check_wgrad(ag, M, N, K, dtype, F32)
+
+
+def test_rows_of_a_part_that_has_none(ag):
+    """Parts are whole steps of 32 rows: the last parts may be empty, or hold one row; so may the bias gradient's."""
+    for M in (32 * 4 * 3 + 1, 32 * 40 + 1, 32 * 33, 65 * 32 + 31):
+        for N, K in ((8, 64), (47, 256)):
+            check_wgrad(ag, M, N, K, BF16, F32)
+
+
+def test_a_nan_in_the_last_row_stays_in_its_row(ag):
+    """Rows behind the last one are zeros, not copies of it."""
+    for dtype in FLOATS:
+        for M, N, K in ((33, 16, 64), (2000, 1050, 64), (65, 24, 96)):
+            g = torch.ones(M, N, dtype=dtype, device="cuda")
+            g[M - 1, 3] = float("inf")
+            got = ag.mx8_weight_grad(g, ag.mx8_quantize(torch.ones(M, K, device="cuda")), dtype=F32)
+            assert bool((got[3] == float("inf")).all())
+            got[3] = M
+            assert bool((got == M).all())

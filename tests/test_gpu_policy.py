@@ -267,3 +267,14 @@ def test_many_rows_of_each_kernel(ag):
         got = ag.policy_loss_grad(*big[:4], ref_logp=big[4], weight=big[5], kl=0.1)
         for a, b in zip(got, few):
             assert torch.equal(a, b.repeat(n, *[1] * (b.dim() - 1))[:rows])
+
+
+@pytest.mark.parametrize("C", [40, 3000, 100003])
+@pytest.mark.parametrize("T", [1e-3, 1e30])
+def test_extreme_temperatures(ag, C, T):
+    """Masked classes stay masked where the factor log2(e) / T has no smaller part left, or is large."""
+    z, y, A, old, away, w = make(5, C, F32, seed=15)
+    if T < 1:
+        y[:] = z.argmax(1)                                  # any other class has no probability left
+        old[:] = -0.1
+    check(ag, z, y, A, old, away, w, temperature=T, kl=0.0)

@@ -220,3 +220,14 @@ def test_tensors_of_the_wrong_kind_are_refused():
                  lambda: ag.policy_loss(x, i, v, v, temperature=0.0)):
         with pytest.raises(ag.AgnesError):
             call()
+
+
+def test_weight_gradients_of_too_many_tiles():
+    for N, K in (((1 << 31) - 1, 1024), (1 << 20, 1 << 16)):
+        with pytest.raises(B.AgnesError) as e:
+            B.agnes_mx8_weight_grad(mat(4, N), m8(4, K), 0, mat(N, K), None, P, BIG)
+        assert e.value.status == B.AGNES_ERR_RANGE, e.value
+        with pytest.raises(B.AgnesError) as e:
+            B.agnes_mx8_weight_grad_bytes(4, N, K)
+        assert e.value.status == B.AGNES_ERR_RANGE, e.value
+    refused(lambda: B.agnes_mx8_weight_grad_bytes(1, 1, (1 << 25) + 1), "2^25")
