@@ -433,40 +433,43 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     // Through registers: whole pieces, from a row's end where they would reach
     // over it; the piece that the end cuts is loaded by elements.  Rows behind the last
     // repeat it and are zeroed on their way to LDS.
-    Eight<TG> gnext[DIRECT ? 1 : GROUNDS];
-    int gleft = 0;                                 // of the loaded step's rows, those from this thread's first on
+    struct Loaded {
+        Eight<TG> e[DIRECT ? 1 : GROUNDS];
+        int left;                                  // of the step's rows, those from this thread's first on
+    };
+    Loaded gring[DIRECT ? 1 : kImages];
     const int64_t gcol = max(min(gn, a.N - 8), (int64_t)0);
     const bool gcut = gn < a.N && gn + 8 > a.N;
-    auto load_g = [&](int s) {
-        gleft = rows - s * kStepRows - grow;
+    auto load_g = [&](Loaded& to, int s) {
+        to.left = rows - s * kStepRows - grow;
         if (rows <= 0) return;
 #pragma unroll
         for (int i = 0; i < (DIRECT ? 0 : GROUNDS); i++) {
             const int m = min(s * kStepRows + grow + i * GSTEP, rows - 1);
             const TG* const p = (const TG*)a.g + (row0 + m) * a.gstride;
-            if (a.N >= 8) gnext[i].v = Vec<TG, 8>::raw(p + gcol);
+            if (a.N >= 8) to.e[i].v = Vec<TG, 8>::raw(p + gcol);
             if (gcut) {
 #pragma unroll
-                for (int q = 0; q < 8; q++) gnext[i].v[q] = gn + q < a.N ? p[gn + q] : (TG)0.f;
+                for (int q = 0; q < 8; q++) to.e[i].v[q] = gn + q < a.N ? p[gn + q] : (TG)0.f;
             }
         }
     };
-    auto put_g = [&](auto image, const Eight<TG>(&e)[DIRECT ? 1 : GROUNDS]) {
+    auto put_g = [&](auto image, const Loaded& from) {
 #pragma unroll
         for (int i = 0; i < (DIRECT ? 0 : GROUNDS); i++) {
             char* const to = gat(image) + GI::row(grow) + i * (GSTEP / GI::BLOCK_ROWS) * GI::BLOCK +
                              (t % GPIECES ^ GI::key(grow) << 1) * 16;
             u32x4 w[P];
-            const bool there = i * GSTEP < gleft;
+            const bool there = i * GSTEP < from.left;
             if constexpr (P == 1) {
-                __builtin_memcpy(&w[0], &e[i].v, 16);
+                __builtin_memcpy(&w[0], &from.e[i].v, 16);
                 w[0] = there ? w[0] : u32x4{0u, 0u, 0u, 0u};
             } else {
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
                     float lo[P], hi[P];
-                    cut<P>(there ? (float)e[i].v[2 * q] : 0.f, lo);
-                    cut<P>(there ? (float)e[i].v[2 * q + 1] : 0.f, hi);
+                    cut<P>(there ? (float)from.e[i].v[2 * q] : 0.f, lo);
+                    cut<P>(there ? (float)from.e[i].v[2 * q + 1] : 0.f, hi);
 #pragma unroll
                     for (int p = 0; p < P; p++) w[p][q] = pack_exact(lo[p], hi[p]);
                 }
@@ -555,10 +558,10 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     // Step s, whose image is the constant, on its way to registers, and from there into LDS.
     auto load = [&](auto image, int s) {
         xring[decltype(image)::value % kImages] = load_x();
-        if constexpr (!DIRECT) load_g(s);
+        if constexpr (!DIRECT) load_g(gring[decltype(image)::value % kImages], s);
     };
     auto put = [&](auto image, auto pair) {
-        if constexpr (!DIRECT && decltype(pair)::value == 0) put_g(image, gnext);
+        if constexpr (!DIRECT && decltype(pair)::value == 0) put_g(image, gring[decltype(image)::value % kImages]);
         put_x(image, pair, xring[decltype(image)::value % kImages]);
     };
     // Steps 0 .. 2 on their way, 0 and 1 in LDS.
@@ -566,11 +569,10 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
         static_for<3>([&](auto i) {
             static_for<P * GROUNDS>([&](auto r) { fetch_g(i, r); });
         });
+    static_for<3>([&](auto i) { load(i, decltype(i)::value); });
     static_for<2>([&](auto i) {
-        load(i, decltype(i)::value);
         static_for<8>([&](auto n) { put(i, n); });
     });
-    load(Const<2>{}, 2);
     arrived(Const<0>{});
     static_for<F>([&](auto i) { read_g(Const<0>{}, i); });
     static_for<G>([&](auto j) { read_x(Const<0>{}, j); });
