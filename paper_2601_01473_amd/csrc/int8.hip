@@ -5,6 +5,7 @@
 //   y[m][n] = (float)(sum_k a[m][k] b[n][k]) s_m t_n + bias[n]
 // The sum is a whole number below 2^31 for K < 2^17, so it is exact in any order.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "ops.hpp"
@@ -633,8 +634,8 @@ void int8_dequantize(const agnes_int8* q, const agnes_matrix* x, hipStream_t st)
 }
 
 constexpr int64_t kFullGrid = 256;                 // workgroups that fill the chip
-constexpr int64_t kPartGrid = 512;                 // and that parts of K aim at
-constexpr int64_t kPartSteps = 8;                  // fewest steps of a part
+constexpr int64_t kPartSteps = 4;                  // fewest steps of a part
+constexpr int64_t kNear = (int64_t)32 << 20;       // operands that the caches near the compute units hold
 
 static void check_sizes(int64_t M, int64_t N, int64_t K) {
     for (int64_t v : {M, N, K})
@@ -664,13 +665,36 @@ static Int8Plan plan_product(int64_t M, int64_t N, int64_t K) {
     const int64_t rounds = (N + 16 * kFullGrid - 1) / (16 * kFullGrid);
     if (M <= kFewTile || (M <= kFewRows && K <= kFewWork && M * K * rounds <= kFewWork))
         return fits({0, 1}, (N + 15) / 16);
-    auto tiles = [&](int64_t r) { return ((M + r - 1) / r) * ((N + r - 1) / r); };
-    for (int r : {256, 128})
-        if (tiles(r) >= kFullGrid) return fits({r, 1}, tiles(r));
-    // else small tiles, and K in parts of at least kPartSteps steps
-    const int64_t steps = chunks_of(K) / kStepChunks;
-    const int64_t parts = std::min<int64_t>(kPartGrid / tiles(64), steps / kPartSteps);
-    return {64, (int)std::max<int64_t>(1, parts)};
+    // The tile, and the parts of K, that are fastest by what steps have measured: us
+    // per step of one workgroup alone on its compute unit (its operands near, or far), and per
+    // step and workgroup of a full chip; what a workgroup needs before and behind its steps;
+    // the parts' sums at 3 TB/s.  us, tiles of 256 / 128 / 64: 256 x 4096 x 4096 42 / 24 / 12,
+    // 1024 x 4096 x 4096 45 / 28 / 40, 3000 x 4096 x 4096 52 / 74 / 109; 64 rows of 8192 x 8192 in 1, 2, 4
+    // and 8 parts 29, 22, 20 and 22; 64 rows of 1024 x 8192 in 1, 8 and 16 parts 16, 11 and 13.
+    struct Tile {
+        int rows;
+        double near, far, full, ends;
+    };
+    static const Tile kTiles[] = {{256, 0.68, 0.75, 0.9, 5}, {128, 0.42, 0.45, 0.36, 3}, {64, 0.115, 0.22, 0.15, 1.5}};
+    const double steps = (double)((chunks_of(K) + kStepChunks - 1) / kStepChunks);
+    const bool near = (M + N) * K <= kNear;
+    Int8Plan best{64, 1};
+    double least = 0;
+    for (const Tile& t : kTiles) {
+        const int64_t tiles = ((M + t.rows - 1) / t.rows) * ((N + t.rows - 1) / t.rows);
+        for (int64_t grid : {1, 256, 512, 1024}) {
+            const int64_t parts = t.rows > 64 ? 1 : std::max<int64_t>(1, std::min(grid / tiles, (int64_t)steps / kPartSteps));
+            const double each = std::ceil(steps / parts), groups = (double)(tiles * parts) / kFullGrid;
+            const double us = t.ends + std::max(each * (near ? t.near : t.far), (t.rows == 256 ? std::ceil(groups) : groups) *
+                                                                                   each * (groups < 0.75 ? 0 : t.full)) +
+                              (parts > 1 ? 6 + (double)(parts * M * N) * 8 / 3e6 : 0);
+            if (least == 0 || us < least) {
+                least = us;
+                best = {t.rows, (int)parts};
+            }
+        }
+    }
+    return fits(best, ((M + best.rows - 1) / best.rows) * ((N + best.rows - 1) / best.rows));
 }
 
 uint64_t int8_product_bytes(int64_t M, int64_t N, int64_t K) {
