@@ -154,3 +154,44 @@ def test_policy_nodes():
 def test_policy_nodes_two_runs_agree():
     from examples import policy_nodes
     assert policy_nodes.main(SMALL) == policy_nodes.main(SMALL)
+
+
+def test_offsets_beyond_32_bits(ag):
+    """Matrices of more than 2^31 elements: the last rows are what they are alone, and a sum over all rows has them.
+    (Few rows of logits take another kernel than many, which sums in another order, so these are held against the
+    definition.)"""
+    R, C, tail = 33000, 66000, 200
+    z = torch.randn(64, C, device="cuda", dtype=BF16).repeat(-(-R // 64), 1)[:R]
+    z[-tail:] = torch.randn(tail, C, device="cuda", dtype=BF16)
+    last = z[-tail:].clone()
+    y = torch.arange(R, device="cuda") % C
+    v = torch.linspace(-1, 1, R, device="cuda")
+    loss, logp, grad = ag.policy_loss_grad(z, y, v, -11 + v)
+    for rows in (slice(0, 2), slice(R - 2, R)):
+        L, eL, P, eP, G, eG = ref.policy(z[rows], y[rows], v[rows], -11 + v[rows])
+        within(loss[rows], L, eL, "loss")
+        within(logp[rows], P, eP, "logp")
+        within(grad[rows], G, eG, "gradient")
+    del loss, logp, grad
+    for quantize, dequantize in ((ag.int8_quantize, ag.int8_dequantize), (ag.mx8_quantize, ag.mx8_dequantize)):
+        q, want = quantize(z), quantize(last)
+        assert torch.equal(q.codes[-tail:], want.codes) and torch.equal(q.scales[-tail:], want.scales)
+        back = dequantize(q, BF16)
+        assert torch.equal(back[-tail:], dequantize(want, BF16))
+        del back
+    # q: the kept rows.  Gradients that are zero but in the last rows leave their sum alone.
+    g = torch.zeros(R, 8, device="cuda", dtype=BF16)
+    g[-tail:] = torch.randn(tail, 8, device="cuda", dtype=BF16)
+    v = ref.mx8_values(want.codes, want.scales, C)
+    for dtype in (BF16, F32):
+        W, eW, b, eb = ref.weight_grad(g[-tail:].to(dtype), v)
+        dw, db = ag.mx8_weight_grad(g.to(dtype), q, bias=True, dtype=F32)
+        # a sum over R rows, of which all but the last are zeros
+        within(dw, W, eW * 4)
+        within(db, b, eb * 4)
+    y, kept = ag.mx8_activation(z, "silu")
+    small, small_kept = ag.mx8_activation(last, "silu")
+    assert torch.equal(y[-tail:], small) and torch.equal(kept.codes[-tail:], small_kept.codes)
+    del y
+    dx = ag.mx8_activation_grad(z, kept, "silu")
+    assert torch.equal(dx[-tail:], ag.mx8_activation_grad(last, small_kept, "silu"))
