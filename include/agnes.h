@@ -50,7 +50,8 @@ typedef enum {
     AGNES_INT64 = 1,
     AGNES_FLOAT32 = 2,
     AGNES_FLOAT16 = 3,
-    AGNES_BFLOAT16 = 4
+    AGNES_BFLOAT16 = 4,
+    AGNES_DTYPE_END = 0x7FFFFFFF   /* no type: any int can be passed, and is refused */
 } agnes_dtype;
 
 typedef struct agnes_store agnes_store;   /* opaque: HBM-resident topology/feature blocks */
@@ -748,7 +749,11 @@ agnes_status agnes_mx8_dequantize(const agnes_mx8* q, const agnes_matrix* x, voi
  *   grad_y * act'(k), or with gated != 0  [grad_y * b * act'(a), grad_y * act(a)]
  *   for k = [a, b].  A block of NaN gives NaN.
  * All in float32, rounded once.  Types may differ.  Errors: INVALID. */
-typedef enum { AGNES_SILU = 0, AGNES_GELU = 1 } agnes_act;
+typedef enum {
+    AGNES_SILU = 0,
+    AGNES_GELU = 1,
+    AGNES_ACT_END = 0x7FFFFFFF   /* no activation, as AGNES_DTYPE_END */
+} agnes_act;
 
 agnes_status agnes_mx8_activation(const agnes_matrix* x, agnes_act act, int32_t gated, const agnes_matrix* y,
                                   const agnes_mx8* kept, void* hip_stream);

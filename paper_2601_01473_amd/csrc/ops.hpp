@@ -168,7 +168,7 @@ struct Carve {
     size_t used = 0;
     explicit Carve(void* p) : base((char*)p) {}
     template <typename T> T* take(int64_t n) {
-        T* p = (T*)(base + used);
+        T* p = (T*)((uintptr_t)base + used);     // base NULL: sizes alone
         used += ((size_t)n * sizeof(T) + 255) / 256 * 256;
         return p;
     }
