@@ -768,9 +768,11 @@ agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int
  * it, so that every product is exact; sums are float32, in an order that the sizes alone
  * decide, and grad_weight is rounded once.  accumulate != 0: the sums are added
  * (in float32) to what grad_weight and grad_bias hold.  M = 0 gives zeros.
+ * The workspace depends on grad_out's type and layout: its bytes are asked for with
+ * the same structure (grad_out's memory is not read).
  * M, N < 2^31, K <= 2^25.  Errors: INVALID, RANGE (more than 2^23 - 8 tiles of
  * 64 x 64 elements of grad_weight). */
-agnes_status agnes_mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
+agnes_status agnes_mx8_weight_grad_bytes(const agnes_matrix* grad_out, int64_t K, uint64_t* bytes);
 agnes_status agnes_mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, int32_t accumulate,
                                    const agnes_matrix* grad_weight, float* grad_bias, void* workspace,
                                    uint64_t workspace_bytes, void* hip_stream);

@@ -222,7 +222,7 @@ def lib():
             ("agnes_mx8_dequantize", [m8, mat, vp]),
             ("agnes_mx8_activation", [mat, ctypes.c_int, i32, mat, m8, vp]),
             ("agnes_mx8_activation_grad", [m8, ctypes.c_int, i32, mat, mat, vp]),
-            ("agnes_mx8_weight_grad_bytes", [i64, i64, i64, u64p]),
+            ("agnes_mx8_weight_grad_bytes", [mat, i64, u64p]),
             ("agnes_mx8_weight_grad", [mat, m8, i32, mat, vp, vp, u64, vp])):
         getattr(L, name).restype = st
         getattr(L, name).argtypes = args
@@ -535,8 +535,8 @@ def agnes_mx8_activation_grad(kept: agnes_mx8, act: int, gated: int, grad_y: agn
                                           stream))
 
 
-def agnes_mx8_weight_grad_bytes(M: int, N: int, K: int) -> int:
-    return _bytes(lib().agnes_mx8_weight_grad_bytes, M, N, K)
+def agnes_mx8_weight_grad_bytes(grad_out: agnes_matrix, K: int) -> int:
+    return _bytes(lib().agnes_mx8_weight_grad_bytes, ctypes.byref(grad_out), K)
 
 
 def agnes_mx8_weight_grad(grad_out: agnes_matrix, kept: agnes_mx8, accumulate: int, grad_weight: agnes_matrix,

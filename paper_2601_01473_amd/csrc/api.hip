@@ -607,10 +607,10 @@ agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int
     return guarded([&] { mx8_activation_grad(kept, act, gated != 0, grad_y, grad_x, (hipStream_t)hip_stream); });
 }
 
-agnes_status agnes_mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes) {
+agnes_status agnes_mx8_weight_grad_bytes(const agnes_matrix* grad_out, int64_t K, uint64_t* bytes) {
     return guarded([&] {
         AGNES_REQUIRE(bytes, AGNES_ERR_INVALID, "bytes must not be NULL");
-        *bytes = mx8_weight_grad_bytes(M, N, K);
+        *bytes = mx8_weight_grad_bytes(grad_out, K);
     });
 }
 

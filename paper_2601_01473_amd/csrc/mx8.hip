@@ -1009,7 +1009,6 @@ static WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t K, int planes, bool st
             }
         }
     }
-    AGNES_REQUIRE(tiles(p.rows, p.cols) <= (1 << 23) - kXcds, AGNES_ERR_RANGE, "the gradient has too many tiles");
     const int64_t pieces = (N + 7) / 8;
     while (p.lanes < 32 && p.lanes < pieces) p.lanes *= 2;
     const int64_t across = (pieces + p.lanes - 1) / p.lanes;
@@ -1031,21 +1030,40 @@ static bool make_planes(int64_t M, int64_t N, int64_t K) { return M * N >= (1 <<
 
 static int64_t plane_pitch(int64_t N) { return (N + 7) / 8 * 8; }
 
-// The largest need of the ways in which gradients of any type reach their tiles.
-uint64_t mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K) {
-    for (int64_t v : {M, N, K})
-        AGNES_REQUIRE(v >= 0 && v < ((int64_t)1 << 31), AGNES_ERR_INVALID, "M, N and K must be in [0, 2^31)");
-    AGNES_REQUIRE(K <= kMaxPitch, AGNES_ERR_INVALID, "K must be at most 2^25");
-    uint64_t most = 0;
-    for (int planes : {1, 2, 3, -1, -2, -3}) {     // < 0: cut in tiles
-        const WgradPlan p = plan_wgrad(M, N, K, std::abs(planes), planes > 0);
-        Carve c(nullptr);
-        if (p.parts > 1) c.take<float>(p.parts * N * K);
-        c.take<float>(p.column_parts * N);
-        if (planes > 0 && make_planes(M, N, K)) c.take<uint16_t>(planes * M * plane_pitch(N));
-        most = std::max<uint64_t>(most, c.used);
-    }
-    return most;
+// How a gradient reaches its tiles.
+struct WgradWay {
+    int planes;                                    // bfloat16 that add up to an element
+    bool direct, cut;                              // straight to LDS as it is; cut into planes first
+    bool straight() const { return direct || cut; }
+};
+static WgradWay way_of(const agnes_matrix* g, int64_t K) {
+    const int64_t M = g->rows, N = g->cols;
+    WgradWay w{g->dtype == AGNES_FLOAT32 ? 3 : g->dtype == AGNES_FLOAT16 ? 2 : 1, false, false};
+    // bfloat16 rows of whole 16-byte pieces, within a buffer's reach
+    w.direct = w.planes == 1 && ((uintptr_t)g->data & 15) == 0 && g->stride % 8 == 0 && N % 8 == 0 && g->stride >= N &&
+               g->stride * 2 <= kMaxPitch;
+    w.cut = !w.direct && make_planes(M, N, K) && plane_pitch(N) * 2 <= kMaxPitch;
+    return w;
+}
+
+static void check_wgrad(const agnes_matrix* grad_out, int64_t K) {
+    check_matrix(grad_out, false, "grad_out");
+    AGNES_REQUIRE(K >= 0 && K <= kMaxPitch, AGNES_ERR_INVALID, "K must be in [0, 2^25]");
+    // by the smallest tile, so that no gradient is refused for its type or layout
+    AGNES_REQUIRE((grad_out->cols + 63) / 64 * ((K + 63) / 64) <= (1 << 23) - kXcds, AGNES_ERR_RANGE,
+                  "the gradient has too many tiles");
+}
+
+uint64_t mx8_weight_grad_bytes(const agnes_matrix* grad_out, int64_t K) {
+    check_wgrad(grad_out, K);
+    const int64_t M = grad_out->rows, N = grad_out->cols;
+    const WgradWay w = way_of(grad_out, K);
+    const WgradPlan p = plan_wgrad(M, N, K, w.planes, w.straight());
+    Carve c(nullptr);
+    if (p.parts > 1) c.take<float>(p.parts * N * K);
+    c.take<float>(p.column_parts * N);
+    if (w.cut) c.take<uint16_t>(w.planes * M * plane_pitch(N));
+    return c.used;
 }
 
 template <typename TG, int P, typename TW, bool DIRECT, int WM, int WN, int F, int G>
@@ -1088,16 +1106,14 @@ void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool a
     AGNES_REQUIRE(grad_weight->rows == grad_out->cols && grad_weight->cols == kept->cols, AGNES_ERR_INVALID,
                   "grad_weight must have a row per column of grad_out and the kept rows' columns");
     const int64_t M = kept->rows, N = grad_out->cols, K = kept->cols;
-    check_workspace(ws, ws_bytes, mx8_weight_grad_bytes(M, N, K));
+    check_workspace(ws, ws_bytes, mx8_weight_grad_bytes(grad_out, K));      // checks K and the number of tiles too
     if (N == 0) return;
+    const WgradWay way = way_of(grad_out, K);
+    const bool direct = way.direct, planes = way.cut;
     with_float(grad_out->dtype, [&](auto tg) {
         typedef decltype(tg) TG;
         constexpr int P = kParts<TG>;
-        // bfloat16 rows of whole 16-byte pieces, within a buffer's reach, need no planes
-        const bool direct = P == 1 && ((uintptr_t)grad_out->data & 15) == 0 && grad_out->stride % 8 == 0 && N % 8 == 0 &&
-                            grad_out->stride >= N && grad_out->stride * 2 <= kMaxPitch;
-        const bool planes = !direct && make_planes(M, N, K) && plane_pitch(N) * 2 <= kMaxPitch;
-        const WgradPlan p = plan_wgrad(M, N, K, P, planes || direct);
+        const WgradPlan p = plan_wgrad(M, N, K, P, way.straight());
         Carve c(ws);
         WgradArgs a{};
         a.g = grad_out->data;

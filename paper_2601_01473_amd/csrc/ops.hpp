@@ -224,7 +224,7 @@ void mx8_activation(const agnes_matrix* x, agnes_act act, bool gated, const agne
                     hipStream_t st);
 void mx8_activation_grad(const agnes_mx8* kept, agnes_act act, bool gated, const agnes_matrix* grad_y,
                          const agnes_matrix* grad_x, hipStream_t st);
-uint64_t mx8_weight_grad_bytes(int64_t M, int64_t N, int64_t K);
+uint64_t mx8_weight_grad_bytes(const agnes_matrix* grad_out, int64_t K);
 void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool accumulate,
                      const agnes_matrix* grad_weight, float* grad_bias, void* ws, uint64_t ws_bytes, hipStream_t st);
 

@@ -124,7 +124,12 @@ _linear_bytes = functools.lru_cache(1024)(B.agnes_mx4_linear_bytes)
 _policy_bytes = functools.lru_cache(1024)(B.agnes_policy_bytes)
 _product8_bytes = functools.lru_cache(1024)(B.agnes_int8_product_bytes)
 _linear8_bytes = functools.lru_cache(1024)(B.agnes_int8_linear_bytes)
-_wgrad_bytes = functools.lru_cache(1024)(B.agnes_mx8_weight_grad_bytes)
+
+
+@functools.lru_cache(1024)
+def _wgrad_bytes(rows: int, cols: int, stride: int, code: int, misaligned: int, K: int) -> int:
+    """By layout: an address stands for all that are as far from a multiple of 16 bytes."""
+    return B.agnes_mx8_weight_grad_bytes(B.agnes_matrix(4096 + misaligned, rows, cols, stride, code), K)
 
 
 def _workspace(like: torch.Tensor, nbytes: int):
@@ -607,7 +612,7 @@ def mx8_weight_grad(grad_out: torch.Tensor, kept: Mx8, bias: bool = False, dtype
             if not bias or bias_out.dtype != torch.float32 or tuple(bias_out.shape) != (m.cols,) or \
                     not bias_out.is_contiguous():
                 raise ValueError("bias_out must be contiguous float32 [N], with bias")
-        need = _wgrad_bytes(m.rows, m.cols, d.cols)
+        need = _wgrad_bytes(m.rows, m.cols, m.stride, m.dtype, g.data_ptr() % 16, d.cols)
         ws = _workspace(g, need)
         B.agnes_mx8_weight_grad(m, d, 1 if accumulate else 0, o, _ptr(bias_out), _ptr(ws), need, _handle(stream))
     return (out, bias_out) if bias else out

@@ -1,5 +1,7 @@
 """What the 8-bit operators and the policy loss refuse, on the host: every bad argument is an error before any device
 work (the device pointers here are never read).  The wrappers' refusals of tensors need CUDA tensors and are marked so."""
+import ctypes
+
 import pytest
 import torch
 
@@ -42,9 +44,10 @@ def test_null_structures():
     assert lib.agnes_mx8_activation(None, 0, 0, None, None, None) == 1
     assert lib.agnes_mx8_activation_grad(None, 0, 0, None, None, None) == 1
     assert lib.agnes_mx8_weight_grad(None, None, 0, None, None, None, 0, None) == 1
-    for f, n in ((lib.agnes_int8_product_bytes, 3), (lib.agnes_int8_linear_bytes, 3), (lib.agnes_mx8_weight_grad_bytes, 3),
-                 (lib.agnes_policy_bytes, 2)):
+    for f, n in ((lib.agnes_int8_product_bytes, 3), (lib.agnes_int8_linear_bytes, 3), (lib.agnes_policy_bytes, 2)):
         assert f(*[1] * n, None) == B.AGNES_ERR_INVALID
+    assert lib.agnes_mx8_weight_grad_bytes(ctypes.byref(mat()), 8, None) == B.AGNES_ERR_INVALID
+    assert lib.agnes_mx8_weight_grad_bytes(None, 8, ctypes.byref(ctypes.c_uint64())) == B.AGNES_ERR_INVALID
 
 
 def pol(z=None, actions=P, index=B.AGNES_INT32, A=P, old=P, ref=None, weight=None, T=1.0, low=0.2, high=0.2, kl=0.0):
@@ -168,12 +171,23 @@ def test_weight_grad_arguments():
     refused(lambda: call(o=mat(9, 63)), "grad_weight")
     refused(lambda: call(o=mat(9, 64, stride=63)), "stride")
     refused(lambda: call(q=m8(scales=None)), "kept")
-    refused(lambda: B.agnes_mx8_weight_grad_bytes(1, -1, 1))
-    refused(lambda: B.agnes_mx8_weight_grad_bytes(1 << 31, 1, 1))
-    need = B.agnes_mx8_weight_grad_bytes(1 << 16, 9, 64)
-    if need:
-        refused(lambda: call(mat(1 << 16, 9), m8(1 << 16), n=need - 1), "workspace")
-        refused(lambda: call(mat(1 << 16, 9), m8(1 << 16), ws=None), "workspace")
+    refused(lambda: B.agnes_mx8_weight_grad_bytes(mat(1, -1), 1), "grad_out")
+    refused(lambda: B.agnes_mx8_weight_grad_bytes(mat(1 << 31, 1), 1), "grad_out")
+    refused(lambda: B.agnes_mx8_weight_grad_bytes(mat(1, 1), -1), "K")
+    for g in (mat(1 << 16, 9), mat(1 << 16, 9, dtype=B.AGNES_BFLOAT16), mat(1 << 16, 64)):
+        need = B.agnes_mx8_weight_grad_bytes(g, 64)
+        out = mat(g.cols, 64)
+        refused(lambda: call(g, m8(1 << 16), out, n=need - 1), "workspace")
+        refused(lambda: call(g, m8(1 << 16), out, ws=None), "workspace")
+
+
+def test_weight_gradients_in_bfloat16_need_no_second_copy():
+    """Only gradients that cannot be read as they are need memory of their own size."""
+    size = 16384 * 4096 * 2
+    assert B.agnes_mx8_weight_grad_bytes(mat(16384, 4096, dtype=B.AGNES_BFLOAT16), 4096) < size // 8
+    assert B.agnes_mx8_weight_grad_bytes(mat(16384, 4096, stride=4097, dtype=B.AGNES_BFLOAT16), 4096) >= size
+    assert B.agnes_mx8_weight_grad_bytes(mat(16384, 4096, dtype=B.AGNES_BFLOAT16, data=P + 2), 4096) >= size
+    assert B.agnes_mx8_weight_grad_bytes(mat(16384, 4096), 4096) >= 3 * size
 
 
 def test_host_tensors_are_refused():
@@ -228,6 +242,6 @@ def test_weight_gradients_of_too_many_tiles():
             B.agnes_mx8_weight_grad(mat(4, N), m8(4, K), 0, mat(N, K), None, P, BIG)
         assert e.value.status == B.AGNES_ERR_RANGE, e.value
         with pytest.raises(B.AgnesError) as e:
-            B.agnes_mx8_weight_grad_bytes(4, N, K)
+            B.agnes_mx8_weight_grad_bytes(mat(4, N), K)
         assert e.value.status == B.AGNES_ERR_RANGE, e.value
-    refused(lambda: B.agnes_mx8_weight_grad_bytes(1, 1, (1 << 25) + 1), "2^25")
+    refused(lambda: B.agnes_mx8_weight_grad_bytes(mat(1, 1), (1 << 25) + 1), "2^25")
