@@ -708,8 +708,8 @@ agnes_status agnes_int8_dequantize(const agnes_int8* q, const agnes_matrix* x, v
  * bias: float32 [N] or NULL.  agnes_int8_linear quantises its float rows x
  * first; w is laid out once by agnes_int8_quantize (a scale for each output
  * column).  M, N < 2^31, K < 2^17.  Errors: INVALID, RANGE (more than 2^23 - 8
- * tiles, which are 16 columns of out for up to 32 rows of x, and 256 x 256
- * elements of out for many; nothing is enqueued then). */
+ * tiles, which are 16 columns of out for up to 16 rows of x, and 256 x 256
+ * elements of out for more; nothing is enqueued then). */
 agnes_status agnes_int8_product_bytes(int64_t M, int64_t N, int64_t K, uint64_t* bytes);
 agnes_status agnes_int8_product(const agnes_int8* x, const agnes_int8* w, const float* bias, int32_t relu,
                                 const agnes_matrix* out, void* workspace, uint64_t workspace_bytes, void* hip_stream);

@@ -662,17 +662,18 @@ struct Int8Plan {
     int parts;                                     // of K
 };
 
-// Refuses what one launch cannot hold (2^32 threads), so that callers do before
-// they enqueue anything: a tile has at most 512 threads, and their number is
-// rounded up to one for each XCD.
+// Refuses what no launch can hold (2^32 threads), so that callers do before they
+// enqueue anything: a tile has at most 512 threads, and their number is rounded up
+// to one for each XCD.
 static Int8Plan plan_product(int64_t M, int64_t N, int64_t K) {
-    auto fits = [](Int8Plan p, int64_t tiles) {
-        AGNES_REQUIRE(tiles <= (1 << 23) - kXcds, AGNES_ERR_RANGE, "the product has too many tiles");
-        return p;
-    };
-    const int64_t rounds = (N + 16 * kFullGrid - 1) / (16 * kFullGrid);
-    if (M <= kFewTile || (M <= kFewRows && K <= kFewWork && M * K * rounds <= kFewWork))
-        return fits({0, 1}, (N + 15) / 16);
+    constexpr int64_t kMostTiles = (1 << 23) - kXcds;
+    auto require = [](bool fits) { AGNES_REQUIRE(fits, AGNES_ERR_RANGE, "the product has too many tiles"); };
+    const int64_t columns = (N + 15) / 16, rounds = (N + 16 * kFullGrid - 1) / (16 * kFullGrid);
+    if (M <= kFewTile) {
+        require(columns <= kMostTiles);
+        return {0, 1};
+    }
+    if (M <= kFewRows && K <= kFewWork && M * K * rounds <= kFewWork && columns <= kMostTiles) return {0, 1};
     // The tile, and the parts of K, that are fastest by what steps have measured: us
     // per step of one workgroup alone on its compute unit (its operands near, or far), and per
     // step and workgroup of a full chip; what a workgroup needs before and behind its steps;
@@ -690,6 +691,7 @@ static Int8Plan plan_product(int64_t M, int64_t N, int64_t K) {
     double least = 0;
     for (const Tile& t : kTiles) {
         const int64_t tiles = ((M + t.rows - 1) / t.rows) * ((N + t.rows - 1) / t.rows);
+        if (tiles > kMostTiles) continue;
         for (int64_t grid : {1, 256, 512, 1024}) {
             const int64_t parts = t.rows > 64 ? 1 : std::max<int64_t>(1, std::min(grid / tiles, (int64_t)steps / kPartSteps));
             const double each = std::ceil(steps / parts), groups = (double)(tiles * parts) / kFullGrid;
@@ -702,7 +704,8 @@ static Int8Plan plan_product(int64_t M, int64_t N, int64_t K) {
             }
         }
     }
-    return fits(best, ((M + best.rows - 1) / best.rows) * ((N + best.rows - 1) / best.rows));
+    require(least > 0);
+    return best;
 }
 
 uint64_t int8_product_bytes(int64_t M, int64_t N, int64_t K) {
