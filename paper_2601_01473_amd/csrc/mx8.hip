@@ -754,22 +754,25 @@ template <int E> __device__ __forceinline__ void join_lanes(float (*red)[4], flo
     for (int e = 0; e < E; e++) y[e] = red[threadIdx.x][e];
 }
 
-// out from the sum of the parts, in an order that the sizes alone decide, by the
-// first `groups` workgroups, `lanes` threads for every four elements; the bias
-// gradient from its parts by the others.  (9 x 150 in 341 parts, by one thread each: 150 us.)
+// out from the sum of the parts, always in the same order, by the first `groups`
+// workgroups, `lanes` threads for every four elements; the bias gradient from its
+// parts by the others, 16 columns at a time.  (9 x 150 in 341 parts, by one thread each: 150 us.)
 template <typename TW> __global__ __launch_bounds__(kBlock) void k_mx8_wgrad_join(WgradArgs a, int parts, int groups, int lanes) {
     __shared__ float red[kBlock][4];
     if ((int)blockIdx.x >= groups) {
         constexpr int LANES = kBlock / kJoinCols;
         const int l = threadIdx.x / kJoinCols;
-        const int64_t n = (int64_t)(blockIdx.x - groups) * kJoinCols + threadIdx.x % kJoinCols;
-        float s[1] = {0.f};
-        if (n < a.N) {
+        for (int64_t n0 = (int64_t)(blockIdx.x - groups) * kJoinCols; n0 < a.N; n0 += (int64_t)(gridDim.x - groups) * kJoinCols) {
+            const int64_t n = n0 + threadIdx.x % kJoinCols;
+            float s[1] = {0.f};
+            if (n < a.N) {
 #pragma unroll 8
-            for (int p = l; p < a.bias_parts; p += LANES) s[0] += a.bias_sums[(int64_t)p * a.N + n];
+                for (int p = l; p < a.bias_parts; p += LANES) s[0] += a.bias_sums[(int64_t)p * a.N + n];
+            }
+            join_lanes(red, s, LANES);
+            if (l == 0 && n < a.N) a.db[n] = a.accumulate ? a.db[n] + s[0] : s[0];
+            __syncthreads();                       // red is used again
         }
-        join_lanes(red, s, LANES);
-        if (l == 0 && n < a.N) a.db[n] = a.accumulate ? a.db[n] + s[0] : s[0];
         return;
     }
     const int side = kBlock / lanes, l = threadIdx.x / side;
@@ -1201,7 +1204,7 @@ void mx8_weight_grad(const agnes_matrix* grad_out, const agnes_mx8* kept, bool a
             const int64_t fours = (N * K + 3) / 4;
             const int groups = K == 0 || p.parts == 1 ? 0
                                : lanes > 1 ? (int)((fours * lanes + kBlock - 1) / kBlock) : (int)grid_for(fours, 4096);
-            const int more = join_bias ? (int)((N + kJoinCols - 1) / kJoinCols) : 0;
+            const int more = join_bias ? (int)std::min<int64_t>((N + kJoinCols - 1) / kJoinCols, kLaunchGroups) : 0;
             if (groups + more > 0)
                 AGNES_LAUNCH((k_mx8_wgrad_join<decltype(tw)>), dim3(groups + more), dim3(kBlock), 0, st, a, p.parts, groups,
                              lanes);
