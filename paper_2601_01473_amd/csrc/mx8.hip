@@ -404,7 +404,10 @@ __device__ __forceinline__ uint32_t pack_exact(float a, float b) {
     return __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xFFFF0000u);
 }
 
-// x as P bfloat16 that add up to it: its bits cut into eights.  Infinities and NaN are whole in the first.
+// x as P bfloat16 that add up to it: its bits cut into eights.  Infinities and NaN are
+// whole in the first.  What a float32 has below 2^-133, the smallest bfloat16, is left
+// out: nothing from 2^-110 on up.  (The parts are summed in one accumulator and
+// meet the same x, so none of them can be scaled up by itself.)
 template <int P> __device__ __forceinline__ void cut(float x, float (&part)[P]) {
     const uint32_t b = __float_as_uint(x);
     const bool finite = (b & 0x7F800000u) != 0x7F800000u;
