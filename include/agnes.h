@@ -770,8 +770,9 @@ agnes_status agnes_mx8_activation_grad(const agnes_mx8* kept, agnes_act act, int
  * grad_out enters as one, two or three bfloat16 (bfloat16, float16, float32) that add up to
  * it, so that every product is exact; but a float32 gradient's digits below 2^-133, the
  * smallest bfloat16, are left out (one of 2^-110 or more has none).  Sums are float32, in
- * an order that the sizes alone decide, and grad_weight is rounded once.  accumulate != 0: the sums are added
- * (in float32) to what grad_weight and grad_bias hold.  M = 0 gives zeros.
+ * an order that the sizes and grad_out's type and layout (stride, alignment to 16 bytes)
+ * decide, and grad_weight is rounded once.  accumulate != 0: the sums are added (in
+ * float32) to what grad_weight and grad_bias hold.  M = 0 gives zeros.
  * The workspace depends on grad_out's type and layout: its bytes are asked for with
  * the same structure (grad_out's memory is not read).
  * M, N < 2^31, K <= 2^25.  Errors: INVALID, RANGE (more than 2^23 - 8 tiles of
