@@ -51,13 +51,6 @@ __device__ __forceinline__ int to_code(float x, const Scale& s) {
 
 // ----------------------------------------------------------------- quantisation
 
-// A row's largest magnitude as bits; NaN above infinity above all finite values.
-__device__ __forceinline__ uint32_t top_bits(const float (&x)[8]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int q = 0; q < 8; q++) top = max(top, __float_as_uint(x[q]) & 0x7FFFFFFFu);
-    return top;
-}
 __device__ __forceinline__ uint32_t lanes_top(uint32_t top, int L) {
     // as numbers without a sign they are ordered as float32 are, but NaN
     return __float_as_uint(lanes_reduce(__uint_as_float(top), L, [](float a, float b) {
@@ -446,7 +439,7 @@ __global__ __launch_bounds__(kBlock) void k_int8_join(Int8Args a, int parts) {
 // LDS.  S is the type of x's elements, up to 16 rows of which the workgroup
 // quantises into LDS first (a launch less), or int8_t: x is quantised already.
 // (One row of 4096 x 4096: 5.9 us quantised before, 7.4 us in all.)
-template <typename S> struct FewRows {
+template <typename S> struct Int8Rows {
     const S* x;
     int64_t stride;                                // of float rows
     int64_t cols;
@@ -454,7 +447,7 @@ template <typename S> struct FewRows {
 constexpr int kFewDepth = 2;                       // steps whose weight is on its way
 
 template <typename S, typename T, int Q>
-__global__ __launch_bounds__(1024) void k_int8_few(Int8Args a, FewRows<S> f) {
+__global__ __launch_bounds__(1024) void k_int8_few(Int8Args a, Int8Rows<S> f) {
     constexpr bool QUANTISED = std::is_same<S, int8_t>::value;
     __shared__ i32x4 sums[16][Q][kWave];
     __shared__ uint32_t tops[16][16];
@@ -730,7 +723,7 @@ template <typename T, int WM, int WN, int F, int G> static void launch_tile(cons
     AGNES_LAUNCH((k_int8_gemm<T, WM, WN, F, G>), dim3(grid, (unsigned)parts), dim3(kWave * WM * WN), 0, st, a);
 }
 
-template <typename S, typename T> static void launch_few(const Int8Args& a, const FewRows<S>& f, hipStream_t st) {
+template <typename S, typename T> static void launch_few(const Int8Args& a, const Int8Rows<S>& f, hipStream_t st) {
     constexpr bool QUANTISED = std::is_same<S, int8_t>::value;
     const int64_t groups = (a.N + 15) / 16;
     // more waves where there are few workgroups, but a step for each
@@ -773,7 +766,7 @@ void int8_product(const agnes_int8* x, const agnes_int8* w, const float* bias, b
     }
     with_float(out->dtype, [&](auto t) {
         typedef decltype(t) T;
-        if (p.rows == 0) launch_few<int8_t, T>(a, FewRows<int8_t>{x->codes, 0, x->cols}, st);
+        if (p.rows == 0) launch_few<int8_t, T>(a, Int8Rows<int8_t>{x->codes, 0, x->cols}, st);
         else if (p.rows == 256) launch_tile<T, 2, 4, 8, 4>(a, 1, st);
         else if (p.rows == 128) launch_tile<T, 2, 2, 4, 4>(a, 1, st);
         else if (p.parts == 1) launch_tile<T, 2, 2, 2, 2>(a, 1, st);
@@ -798,7 +791,7 @@ void int8_linear(const agnes_matrix* x, const agnes_int8* w, const float* bias, 
         with_float(x->dtype, [&](auto ts) {
             with_float(out->dtype, [&](auto t) {
                 typedef decltype(ts) S;
-                launch_few<S, decltype(t)>(a, FewRows<S>{(const S*)x->data, x->stride, x->cols}, st);
+                launch_few<S, decltype(t)>(a, Int8Rows<S>{(const S*)x->data, x->stride, x->cols}, st);
             });
         });
         return;

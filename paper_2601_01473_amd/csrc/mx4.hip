@@ -49,13 +49,6 @@ __device__ __forceinline__ uint32_t to_codes(const float (&x)[8], int code) {
     return r & ~zero;                              // -0 as 0
 }
 
-__device__ __forceinline__ uint32_t top_bits(const float (&x)[8]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int q = 0; q < 8; q++) top = max(top, __float_as_uint(x[q]) & 0x7FFFFFFFu);
-    return top;
-}
-
 // ----------------------------------------------------------------- quantisation
 
 // A piece is 8 elements, a block four pieces in adjacent lanes.  Pieces are

@@ -20,7 +20,7 @@ static int64_t blocks_of(int64_t cols) { return (cols + kMx8Block - 1) / kMx8Blo
 
 // The scale code of a block whose largest magnitude has the float32 bits `top`:
 // their exponent (0 for subnormal numbers; 255 for infinities and NaN).
-__device__ __forceinline__ int scale_code(uint32_t top) { return (int)(top >> 23); }
+__device__ __forceinline__ int mx8_scale(uint32_t top) { return (int)(top >> 23); }
 
 // x in units of 1/64 of the scale; the scaling is exact (or far below 1).
 __device__ __forceinline__ int to_code(float x, int scale) {
@@ -28,7 +28,7 @@ __device__ __forceinline__ int to_code(float x, int scale) {
     return (int)fminf(fmaxf(q, -127.f), 127.f);
 }
 // The eight codes as bytes, the first in the low bits.
-__device__ __forceinline__ uint2 to_codes(const float (&x)[8], int scale) {
+__device__ __forceinline__ uint2 mx8_codes(const float (&x)[8], int scale) {
     uint2 w = {0u, 0u};
     if (scale == 255) return w;
 #pragma unroll
@@ -52,9 +52,7 @@ __device__ __forceinline__ void from_codes(uint2 w, int scale, float (&x)[8]) {
 
 // The largest magnitude of the four lanes that hold a block.
 __device__ __forceinline__ uint32_t block_top(const float (&x)[8]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int q = 0; q < 8; q++) top = max(top, __float_as_uint(x[q]) & 0x7FFFFFFFu);
+    uint32_t top = top_bits(x);
     top = max(top, __float_as_uint(lane_pair<1>(__uint_as_float(top))));
     return max(top, __float_as_uint(lane_pair<2>(__uint_as_float(top))));
 }
@@ -93,8 +91,8 @@ __global__ __launch_bounds__(kBlock) void k_mx8_quantize(const T* __restrict__ x
     for (int u = 0; u < kPieces; u++) {
         const int64_t i = base + u * kBlock + threadIdx.x;
         if (i >= pieces) continue;                 // whole blocks: pieces is a multiple of 4
-        const int scale = scale_code(block_top(v[u]));
-        *(uint2*)(codes + 8 * i) = to_codes(v[u], scale);
+        const int scale = mx8_scale(block_top(v[u]));
+        *(uint2*)(codes + 8 * i) = mx8_codes(v[u], scale);
         if (threadIdx.x % 4 == 0) scales[i / 4] = (uint8_t)scale;
     }
 }
@@ -233,9 +231,9 @@ __global__ __launch_bounds__(kBlock) void k_mx8_act(const T* __restrict__ x, int
         if constexpr (KEEP) {
 #pragma unroll
             for (int h = 0; h < HALVES; h++) {
-                const int scale = scale_code(block_top(v[u][h]));
+                const int scale = mx8_scale(block_top(v[u][h]));
                 const int64_t at = p.row * blocks * kMx8Block + h * F + c;
-                *(uint2*)(codes + at) = to_codes(v[u][h], scale);
+                *(uint2*)(codes + at) = mx8_codes(v[u][h], scale);
                 if (threadIdx.x % 4 == 0) scales[at / kMx8Block] = (uint8_t)scale;
             }
         }

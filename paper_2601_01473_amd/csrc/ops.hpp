@@ -94,6 +94,14 @@ template <typename T> __device__ __forceinline__ void load8(const T* row, int64_
     }
 }
 
+// The largest magnitude as bits: NaN above infinity above all finite values.
+__device__ __forceinline__ uint32_t top_bits(const float (&x)[8]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 8; q++) top = max(top, __float_as_uint(x[q]) & 0x7FFFFFFFu);
+    return top;
+}
+
 // Pieces of 8 elements are numbered row after row; a workgroup takes kPieces
 // rounds of kBlock of them.
 constexpr int kPieces = 4;

@@ -150,7 +150,7 @@ __device__ __forceinline__ void store_row(const PolicyArgs& a, int64_t r, const 
 constexpr int kLanesMin = 8;
 constexpr int kLaneGroups = 2048;                // workgroups, about what the chip holds at once
 
-template <typename T, int P> struct LaneRow {
+template <typename T, int P> struct PolicyRow {
     typename Vec<T, 16 / (int)sizeof(T)>::type v[P];
     Decision d;
 };
@@ -161,17 +161,17 @@ template <typename T, int P> __global__ __launch_bounds__(kBlock) void k_policy_
     const int64_t step = (int64_t)gridDim.x * groups;
     int64_t r = (int64_t)blockIdx.x * groups + g;
     auto load = [&](int64_t i) {
-        LaneRow<T, P> x;
+        PolicyRow<T, P> x;
         const T* zr = (const T*)a.z + i * a.zstride;
 #pragma unroll
         for (int p = 0; p < P; p++) x.v[p] = logits_piece<T, E>(zr, (gl + p * L) * E, a.C);
         x.d = load_decision(a, i);
         return x;
     };
-    LaneRow<T, P> next;
+    PolicyRow<T, P> next;
     if (r < a.rows) next = load(r);
     for (; r < a.rows; r += step) {                         // per group; nothing below crosses a group
-        LaneRow<T, P> x = next;
+        PolicyRow<T, P> x = next;
         if (r + step < a.rows) next = load(r + step);
         const int64_t at = r * a.gstride;
         if (skipped(a, x.d)) {
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 && P == 8 ? 8 : 4) void k_
 // ----------------------------------------------------------------- a row over several workgroups
 
 // Part of a row: its maximum and sum, and the action's logit if it lies in it (else 0).
-struct Part {
+struct PolicyPart {
     float m, s, zy, pad;
 };
 
@@ -300,7 +300,7 @@ constexpr int kPartThreads = 256;
 
 // blockIdx: (part, row).  A part is `span` logits, a multiple of a piece.
 template <typename T>
-__global__ __launch_bounds__(kPartThreads) void k_policy_part(PolicyArgs a, int64_t span, Part* __restrict__ parts) {
+__global__ __launch_bounds__(kPartThreads) void k_policy_part(PolicyArgs a, int64_t span, PolicyPart* __restrict__ parts) {
     constexpr int E = 16 / (int)sizeof(T), U = 4;
     typedef typename Vec<T, E>::type Raw;
     __shared__ Sum red[kPartThreads / kWave];
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part(PolicyArgs a, int6
     s = lanes_join(a, s);
     if (lane == 0) {
         const float zy = d.y >= lo && d.y < hi ? to_float(zr[d.y]) : 0.f;
-        parts[r * gridDim.x + blockIdx.x] = Part{s.m, s.s, zy, 0.f};
+        parts[r * gridDim.x + blockIdx.x] = PolicyPart{s.m, s.s, zy, 0.f};
     }
 }
 
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_part(PolicyArgs a, int6
 // workgroup, and the gradient of [lo, hi).  The action's logit comes with them:
 // where grad is over the logits another workgroup may have written there.
 template <typename T>
-__global__ __launch_bounds__(kPartThreads) void k_policy_apply(PolicyArgs a, int64_t span, int nparts, const Part* __restrict__ parts) {
+__global__ __launch_bounds__(kPartThreads) void k_policy_apply(PolicyArgs a, int64_t span, int nparts, const PolicyPart* __restrict__ parts) {
     constexpr int E = 16 / (int)sizeof(T), U = 4;
     typedef typename Vec<T, E>::type Raw;
     const int tid = threadIdx.x, lane = lane_id();
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(kPartThreads) void k_policy_apply(PolicyArgs a, int
         s = Sum{a.stats_in[3 * r], a.stats_in[3 * r + 1]};
         zy = a.stats_in[3 * r + 2];
     } else {
-        const Part* p = parts + r * nparts;
+        const PolicyPart* p = parts + r * nparts;
         for (int i = lane; i < nparts; i += kWave) s.m = fmaxf(s.m, p[i].m);
         s.m = lanes_max(s.m, kWave);
         for (int i = lane; i < nparts; i += kWave) {
@@ -428,7 +428,7 @@ uint64_t policy_bytes(int64_t rows, int64_t classes) {
     int64_t span = 0, most = 0;
     for (int64_t size : {2, 4}) {                // either size of logits
         const int n = parts_of(rows, classes, size, span);
-        if (span) most = std::max<int64_t>(most, rows * n * (int64_t)sizeof(Part));
+        if (span) most = std::max<int64_t>(most, rows * n * (int64_t)sizeof(PolicyPart));
     }
     return (uint64_t)most;
 }
@@ -526,12 +526,12 @@ template <typename T> static void launch(const PolicyArgs& a, void* ws, hipStrea
         for (int64_t r = 0; r < rows; r += 65535) {
             const int64_t n = std::min<int64_t>(65535, rows - r);
             const PolicyArgs b = rows_from<T>(a, r, n);
-            Part* p = (Part*)ws + r * parts;
+            PolicyPart* p = (PolicyPart*)ws + r * parts;
             const dim3 grid((unsigned)parts, (unsigned)n);
             if (!a.stats_in) AGNES_LAUNCH((k_policy_part<T>), grid, dim3(kPartThreads), 0, st, b, span, p);
             // without a gradient only a row's first part has anything to do
             AGNES_LAUNCH((k_policy_apply<T>), dim3(a.grad ? (unsigned)parts : 1u, (unsigned)n), dim3(kPartThreads), 0, st, b,
-                         span, parts, (const Part*)p);
+                         span, parts, (const PolicyPart*)p);
         }
         return;
     }
