@@ -208,9 +208,9 @@ static __device__ const uint4 k_int8_zero = {0u, 0u, 0u, 0u};
 // LDS serves lanes 0-3, 12-15 and 20-27 of a wave together, and so on: these 16
 // then lie in different banks.
 //
-// 8192^3: 431 us, 2550 TOPS, the matrix cores busy two thirds of the cycles, at a
-// clock that falls as they get busier (1.85 GHz): with 32 x 32 x 32
-// multiplications as many cycles take 493 us.  (Chunk p at place p ^ (r / 4 % 4), where
+// 8192^3: 431 us, 2550 TOPS (449 us on a slower card), the matrix cores busy two
+// thirds of the cycles, at a clock that falls as they get busier (1.85 GHz): with
+// 32 x 32 x 32 multiplications as many cycles take 493 us.  (Chunk p at place p ^ (r / 4 % 4), where
 // lanes meet in pairs: as many us, so LDS does not bound it.)
 constexpr int kStepChunks = 4, kImages = 4;
 __device__ __forceinline__ int turn(int r) { return -(r / 4) & 3; }
@@ -642,11 +642,12 @@ static void check_sizes(int64_t M, int64_t N, int64_t K) {
 
 // Which kernel computes M x N x K, by sizes alone.  k_int8_few reads x again for
 // every 16 columns of out, and a workgroup's steps follow each other, so more than one
-// 16-row tile pays only while rows x K x rounds of workgroups is small.  us,
+// 16-row tile pays only while rows x K x rounds of workgroups is small.  Up to 16
+// rows take it at any size: it is the faster one but for the largest layers.  us,
 // k_int8_few against tiles, of N x K: 16 rows of 4096 x 4096 7.0 / 9.6, of 1024 x 8192 9.7 / 12.0, of
 // 8192 x 8192 18.9 / 16.8; 17 rows of 4096 x 4096 7.7 / 9.8, of 8192 x 8192 20.9 / 16.8; 32 rows of 4096 x
 // 4096 9.0 / 9.9, of 2048 x 2048 5.9 / 6.7, of 8192 x 8192 25.9 / 17.5, of 1024 x 8192 13.1 / 12.5.
-constexpr int64_t kFewTile = 16;                   // rows of k_int8_few, whatever the sizes,
+constexpr int64_t kFewTile = 16;                   // rows of k_int8_few at any size (16 of 8192 x 8192: 2 us more than tiles),
 constexpr int64_t kFewRows = 32;                   // and at most, as long as
 constexpr int64_t kFewWork = 1 << 17;              // rows x K x rounds is no more than this
 constexpr int64_t kFewBytes = 40 << 10;            // LDS for rows that it quantises itself
